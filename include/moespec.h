@@ -334,6 +334,159 @@ moespec_status moespec_oracle_ranking(const moespec_desc *desc, const moespec_we
 #define MOESPEC_STREAM_READ_WORDS 256
 moespec_status moespec_stream_read(const void *buf, size_t bytes, uint32_t *checksum, void *hip_stream);
 
+/*
+ * ---- The other half of a verification step: tree attention, its cache, the norm between two blocks ----
+ *
+ * A draft tree is verified by attention blocks and MoE blocks in turn.  The calls below are the attention block's: attention of
+ * the drafted tokens over a cache of keys and values and over their own tree (moespec_tree_attention), the attention weight that
+ * every cached key received (moespec_cache_weights), the accepted path appended to the cache (moespec_cache_commit), a cache cut
+ * to a budget of entries by that weight (moespec_cache_evict: what the expert budget does to experts, done to cached
+ * keys), and the norms around a block fused with its gate, its scale and the residual stream (moespec_block_norm).
+ * The conventions at the head of this file apply, and:
+ *   Batch     A call serves n_seq sequences.  Sequence s owns the token rows tree_off[s] .. tree_off[s+1] - 1 (its tree, which may
+ *             be empty) and cache entries [s].  Rows of no sequence (padding behind the last one) are neither read nor written.
+ *   Cache     k_cache, v_cache [n_seq, n_kv_heads, capacity, head_dim] dtype; sequence s holds cache_len[s] entries, in order.
+ *             Entries from there on are not read.
+ *   Device data  Lengths, offsets and paths are device data and not checked on the host.  The kernels clamp them to what the
+ *             buffers hold (offsets to [0, n_tokens], a tree to max_tree rows, a length to max_len, or to capacity), so
+ *             that no value leads to an access outside of a buffer.
+ *   Sums      are in fp32, in an order that depends on the arguments alone.
+ */
+
+/* Shape of one attention layer.  Host struct. */
+typedef struct {
+  int32_t n_heads;    /* H query heads                                                        */
+  int32_t n_kv_heads; /* Hk key/value heads; H is a multiple, head h reads KV head h / (H/Hk) */
+  int32_t head_dim;   /* D: 64, 96, 128, 192 or 256                                           */
+  int32_t capacity;   /* entries of the cache per sequence and KV head                        */
+  int32_t dtype;      /* moespec_dtype: storage of q, k, v, the cache and out                 */
+  float scale;        /* factor of the scores, positive and finite (commonly 1 / sqrt(D))     */
+} moespec_attn_desc;
+
+/* The drafted tokens of a call.  Host struct holding device pointers. */
+typedef struct {
+  int32_t n_seq;             /* sequences, 1 .. 65535                                                 */
+  int32_t n_tokens;          /* M, token rows of q, k_tree, v_tree and the outputs, 1 .. 65535        */
+  int32_t max_tree;          /* no tree has more rows (longer ones are cut there), 1 .. M             */
+  int64_t q_stride;          /* elements from a token's row of q to the next one's; 0: H * D          */
+  int64_t kv_stride;         /* the same for k_tree and v_tree; 0: Hk * D                             */
+  const int32_t *tree_off;   /* [n_seq + 1] or NULL: one sequence (n_seq = 1) of all M tokens         */
+  const uint32_t *tree_mask; /* [M, (max_tree + 31) / 32] bit j of a token's row: it sees token j of  */
+                             /* its tree.  NULL: a chain, every token sees those up to itself         */
+} moespec_tree;
+
+/* Checks the ranges above; H <= 1024.  MOESPEC_OK, MOESPEC_ERR_INVALID_ARG or MOESPEC_ERR_UNSUPPORTED_SHAPE.  Host only. */
+moespec_status moespec_check_attn_desc(const moespec_attn_desc *desc);
+
+/*
+ * Bytes of workspace that moespec_tree_attention and moespec_cache_weights need with up to M_max tokens, max_tree rows a tree
+ * and max_len cache entries (0 on an invalid descriptor or range).  Contents are scratch, as for the other calls.  Host only.
+ */
+size_t moespec_attn_workspace_bytes(const moespec_attn_desc *desc, int32_t n_seq, int32_t M_max, int32_t max_tree,
+                                    int32_t max_len);
+
+/*
+ * Attention of drafted tokens: with K the cached keys of the token's sequence and the keys of its tree that its mask shows,
+ *   out[t, h] = sum_j softmax_j(scale q[t, h] . K_j) V_j,    lse[t, h] = log sum_j exp(scale q[t, h] . K_j).
+ *   q        [M, H, D] dtype in     rows q_stride apart (views of one projection's output), multiples of 16 bytes
+ *   k_tree, v_tree [M, Hk, D] dtype in   rows kv_stride apart
+ *   k_cache, v_cache   in           may be NULL if max_len is 0
+ *   cache_len [n_seq] int32 in      may be NULL if max_len is 0
+ *   max_len             in          no sequence has more entries, 0 .. capacity; sizes the launch, the entries that are read
+ *                                   go by cache_len
+ *   out      [M, H, D] dtype out    contiguous
+ *   lse      [M, H] float out       natural logarithm; may be NULL
+ * A token that sees no key gets out = 0 and lse = -inf; so does one whose every score is -inf.  Keys and values that a
+ * token does not see have no part in its result, whatever they hold (NaN and infinities included).  Weights are rounded to the layer's
+ * dtype before they multiply the values (bf16), everything else is fp32.
+ */
+moespec_status moespec_tree_attention(const moespec_attn_desc *desc, const moespec_tree *tree, const void *q,
+                                      const void *k_tree, const void *v_tree, const void *k_cache, const void *v_cache,
+                                      const int32_t *cache_len, int32_t max_len, void *out, float *lse,
+                                      void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * The attention weight that every key received, summed over the tokens and over the query heads of its KV head:
+ *   w_j = sum_{t, h} row_weight[t] exp(scale q[t, h] . K_j - lse[t, h])   over the rows that see key j.
+ *   lse        [M, H] float in      as written by moespec_tree_attention; a row with -inf has no part
+ *   row_weight [M] float in         NULL: 1.  0 for rejected tokens, or the probability of acceptance
+ *   cache_w_in [n_seq, Hk, capacity] float in  NULL: 0.  May be cache_w_out
+ *   cache_w_out                     out  decay * cache_w_in + w for the cached keys; entries behind cache_len are left alone
+ *   tree_w     [M, Hk] float out    w of the trees' own keys (moespec_cache_commit takes it into the cache); may be NULL
+ */
+moespec_status moespec_cache_weights(const moespec_attn_desc *desc, const moespec_tree *tree, const void *q,
+                                     const void *k_tree, const void *k_cache, const int32_t *cache_len, int32_t max_len,
+                                     const float *lse, const float *row_weight, float decay, const float *cache_w_in,
+                                     float *cache_w_out, float *tree_w, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Appends the accepted path of every sequence to the caches of n_layers layers, which share lengths and paths: entry
+ * cache_len[s] + i takes token path[s, i] of the tree of s, for i < n_path[s].
+ *   k_tree, v_tree [n_layers, M, Hk, D] dtype in   rows kv_stride apart, layers M * kv_stride apart
+ *   tree_w   [n_layers, M, Hk] float in, cache_w [n_layers, n_seq, Hk, capacity] float in/out   both or neither NULL
+ *   path     [n_seq, max_path] int32 in   tokens by their place in the tree; max_path >= 1.  A place outside of the tree gives
+ *                                         an entry of zeros
+ *   n_path   [n_seq] int32 in             entries past the capacity are dropped
+ *   k_cache, v_cache [n_layers, n_seq, Hk, capacity, D] dtype in/out
+ *   cache_len [n_seq] int32 in
+ *   new_len  [n_seq] int32 out            min(cache_len + n_path, capacity); not cache_len itself; may be NULL
+ */
+moespec_status moespec_cache_commit(const moespec_attn_desc *desc, int32_t n_layers, const moespec_tree *tree,
+                                    const void *k_tree, const void *v_tree, const float *tree_w, const int32_t *path,
+                                    const int32_t *n_path, int32_t max_path, void *k_cache, void *v_cache, float *cache_w,
+                                    const int32_t *cache_len, int32_t *new_len, void *hip_stream);
+
+/* Bytes of workspace of moespec_cache_evict (0 on an invalid descriptor or range).  Host only. */
+size_t moespec_evict_workspace_bytes(const moespec_attn_desc *desc, int32_t n_layers, int32_t n_seq, int32_t budget);
+
+/*
+ * Cuts caches to `budget` entries per layer, sequence and KV head: kept are the `recent` last ones and, of those before them, the
+ * budget - recent with the largest weight (ties to the lowest index; NaN behind every number), in their order.  A cache
+ * that holds no more than budget entries is copied whole.
+ *   budget, recent                   1 <= budget <= out_capacity, 0 <= recent <= budget
+ *   k_cache, v_cache, cache_w        in   as above, with a leading n_layers axis; cache_len [n_seq] int32 in
+ *   k_out, v_out [n_layers, n_seq, Hk, out_capacity, D] dtype out, w_out [n_layers, n_seq, Hk, out_capacity] float out
+ *                                    none of them an input; entries behind the new length are left alone
+ *   kept     [n_layers, n_seq, Hk, budget] int32 out   former index of every entry, -1 behind the new length; may be NULL
+ *   new_len  [n_seq] int32 out       min(cache_len, budget); not cache_len itself; may be NULL
+ */
+moespec_status moespec_cache_evict(const moespec_attn_desc *desc, int32_t n_layers, int32_t n_seq, const void *k_cache,
+                                   const void *v_cache, const float *cache_w, const int32_t *cache_len, int32_t budget,
+                                   int32_t recent, int32_t out_capacity, void *k_out, void *v_out, float *w_out,
+                                   int32_t *kept, int32_t *new_len, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Shape of the gate of moespec_block_norm: none, one value per channel [d], per token [M], or per element [M, d]. */
+typedef enum {
+  MOESPEC_BLOCK_GATE_NONE = 0,
+  MOESPEC_BLOCK_GATE_CHANNEL = 1,
+  MOESPEC_BLOCK_GATE_TOKEN = 2,
+  MOESPEC_BLOCK_GATE_ELEMENT = 3
+} moespec_block_gate;
+
+/* What lies between two blocks.  Host struct holding device pointers. */
+typedef struct {
+  int32_t post_norm;    /* 1: the block's output is scaled to unit root-mean-square first     */
+  int32_t gate_kind;    /* moespec_block_gate                                                 */
+  int32_t gate_sigmoid; /* 1: the gate is sigmoid(gate)                                       */
+  float scale;          /* of the gated block output                                          */
+  float eps;            /* added to the mean square in both norms, >= 0                       */
+  const void *w_post;   /* [d] dtype or NULL (1); only with post_norm                         */
+  const void *gate;     /* dtype, shape by gate_kind; NULL for none                           */
+  const void *w_pre;    /* [d] dtype or NULL (1)                                              */
+} moespec_block;
+
+/*
+ * From a block's output to the next block's input, row by row in fp32 with one rounding at each output:
+ *   z = post_norm ? w_post * y / sqrt(mean y^2 + eps) : y,   r = residual + scale * gate * z,
+ *   x = w_pre * r / sqrt(mean r^2 + eps).
+ * With y = residual stream of a first block, no gate and residual NULL it is the plain norm before a block.  x is taken from the
+ * unrounded r.  moespec_rms_scale is the form without weights, gate, eps and residual.
+ *   y [M, d] dtype in;  residual [M, d] dtype in, may be NULL (0)
+ *   r, x [M, d] dtype out; one of them may be NULL.  Each may be the same buffer as y, residual or an element gate, not as the other
+ */
+moespec_status moespec_block_norm(const moespec_desc *desc, const moespec_block *block, const void *y, const void *residual,
+                                  int32_t M, void *r, void *x, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

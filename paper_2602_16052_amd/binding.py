@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, c_char_p, c_int32, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_char_p, c_float, c_int32, c_int64, c_size_t, c_void_p
 from dataclasses import dataclass
 from typing import Dict, Optional
 
@@ -22,12 +22,15 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED_SHAPE, ERR_WORKSPACE_TOO_SMALL, ERR_HIP = r
 F32, BF16 = 0, 1
 TRUNCATE, SUBSTITUTE = 0, 1
 GATE_SOFTMAX, GATE_SIGMOID = 0, 1
+BLOCK_GATE_NONE, BLOCK_GATE_CHANNEL, BLOCK_GATE_TOKEN, BLOCK_GATE_ELEMENT = range(4)
 
 EXPORTS = ("moespec_abi_version", "moespec_status_string", "moespec_check_desc", "moespec_workspace_bytes",
            "moespec_route", "moespec_budget", "moespec_expert_ffn", "moespec_layer_forward",
            "moespec_layer_forward_traced", "moespec_layer_forward_static", "moespec_stack_forward", "moespec_rms_scale",
            "moespec_calibration_count", "moespec_static_shortlist", "moespec_coverage_curve",
-           "moespec_reconstruction_error", "moespec_oracle_ranking", "moespec_stream_read")
+           "moespec_reconstruction_error", "moespec_oracle_ranking", "moespec_stream_read",
+           "moespec_check_attn_desc", "moespec_attn_workspace_bytes", "moespec_tree_attention", "moespec_cache_weights",
+           "moespec_cache_commit", "moespec_evict_workspace_bytes", "moespec_cache_evict", "moespec_block_norm")
 
 
 class MoeSpecError(RuntimeError):
@@ -50,6 +53,21 @@ class Taps(Structure):
     _fields_ = [("probs", c_void_p), ("scores", c_void_p), ("budget_ids", c_void_p), ("tok_ids", c_void_p),
                 ("tok_w", c_void_p), ("seg_expert", c_void_p), ("seg_off", c_void_p), ("perm", c_void_p),
                 ("n_loaded", c_void_p)]
+
+
+class CAttnDesc(Structure):
+    _fields_ = [("n_heads", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32), ("capacity", c_int32),
+                ("dtype", c_int32), ("scale", c_float)]
+
+
+class Tree(Structure):
+    _fields_ = [("n_seq", c_int32), ("n_tokens", c_int32), ("max_tree", c_int32), ("q_stride", c_int64),
+                ("kv_stride", c_int64), ("tree_off", c_void_p), ("tree_mask", c_void_p)]
+
+
+class Block(Structure):
+    _fields_ = [("post_norm", c_int32), ("gate_kind", c_int32), ("gate_sigmoid", c_int32), ("scale", c_float),
+                ("eps", c_float), ("w_post", c_void_p), ("gate", c_void_p), ("w_pre", c_void_p)]
 
 
 TRACE_POINTS = 5
@@ -117,6 +135,25 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                                            c_void_p, c_void_p, c_size_t, c_void_p]
     lib.moespec_stream_read.restype = c_int32
     lib.moespec_stream_read.argtypes = [c_void_p, c_size_t, c_void_p, c_void_p]
+    P = c_void_p
+    lib.moespec_check_attn_desc.restype = c_int32
+    lib.moespec_check_attn_desc.argtypes = [POINTER(CAttnDesc)]
+    lib.moespec_attn_workspace_bytes.restype = c_size_t
+    lib.moespec_attn_workspace_bytes.argtypes = [POINTER(CAttnDesc), c_int32, c_int32, c_int32, c_int32]
+    lib.moespec_tree_attention.restype = c_int32
+    lib.moespec_tree_attention.argtypes = [POINTER(CAttnDesc), POINTER(Tree), P, P, P, P, P, P, c_int32, P, P, P, c_size_t, P]
+    lib.moespec_cache_weights.restype = c_int32
+    lib.moespec_cache_weights.argtypes = [POINTER(CAttnDesc), POINTER(Tree), P, P, P, P, c_int32, P, P, c_float, P, P, P, P,
+                                          c_size_t, P]
+    lib.moespec_cache_commit.restype = c_int32
+    lib.moespec_cache_commit.argtypes = [POINTER(CAttnDesc), c_int32, POINTER(Tree), P, P, P, P, P, c_int32, P, P, P, P, P, P]
+    lib.moespec_evict_workspace_bytes.restype = c_size_t
+    lib.moespec_evict_workspace_bytes.argtypes = [POINTER(CAttnDesc), c_int32, c_int32, c_int32]
+    lib.moespec_cache_evict.restype = c_int32
+    lib.moespec_cache_evict.argtypes = [POINTER(CAttnDesc), c_int32, c_int32, P, P, P, P, c_int32, c_int32, c_int32, P, P, P,
+                                        P, P, P, c_size_t, P]
+    lib.moespec_block_norm.restype = c_int32
+    lib.moespec_block_norm.argtypes = [POINTER(Desc), POINTER(Block), P, P, c_int32, P, P, P]
     if path is None:
         _lib = lib
     return lib
@@ -505,3 +542,328 @@ def moespec_stream_read(buf: torch.Tensor, checksum: Optional[torch.Tensor] = No
                                             _stream(stream))
     _check(st, "moespec_stream_read")
     return checksum
+
+
+# ---- Tree attention, its cache, the norm between two blocks.  The calls come as objects with their arguments marshalled once (a
+# program keeps one per layer, next to its buffers) and as functions that build one, allocate what is not given and call it.  Tensors
+# are checked for device, type, exact shape and layout; the call runs on `stream` or, without one, on the stream that is current
+# for the tensors' device at the time of the call.
+
+
+@dataclass
+class AttnDesc:
+    """Shape of one attention layer (host side of moespec_attn_desc).  scale None: 1 / sqrt(head_dim)."""
+    n_heads: int
+    n_kv_heads: int
+    head_dim: int
+    capacity: int
+    dtype: int          # F32 or BF16
+    scale: Optional[float] = None
+
+    def c(self) -> CAttnDesc:
+        scale = self.scale if self.scale is not None else max(int(self.head_dim), 1) ** -0.5
+        return CAttnDesc(self.n_heads, self.n_kv_heads, self.head_dim, self.capacity, self.dtype, scale)
+
+    @property
+    def torch_dtype(self) -> torch.dtype:
+        return torch.bfloat16 if self.dtype == BF16 else torch.float32
+
+
+def check_attn_desc(desc: AttnDesc) -> int:
+    c = desc.c()
+    return int(load_library().moespec_check_attn_desc(ctypes.byref(c)))
+
+
+def attn_workspace_bytes(desc: AttnDesc, n_seq: int, M_max: int, max_tree: int, max_len: int) -> int:
+    c = desc.c()
+    return int(load_library().moespec_attn_workspace_bytes(ctypes.byref(c), int(n_seq), int(M_max), int(max_tree),
+                                                           int(max_len)))
+
+
+def alloc_attn_workspace(desc: AttnDesc, n_seq: int, M_max: int, max_tree: int, max_len: int, device="cuda") -> torch.Tensor:
+    n = attn_workspace_bytes(desc, n_seq, M_max, max_tree, max_len)
+    if n == 0:
+        raise MoeSpecError(ERR_INVALID_ARG, "moespec_attn_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def evict_workspace_bytes(desc: AttnDesc, n_layers: int, n_seq: int, budget: int) -> int:
+    c = desc.c()
+    return int(load_library().moespec_evict_workspace_bytes(ctypes.byref(c), int(n_layers), int(n_seq), int(budget)))
+
+
+def alloc_evict_workspace(desc: AttnDesc, n_layers: int, n_seq: int, budget: int, device="cuda") -> torch.Tensor:
+    n = evict_workspace_bytes(desc, n_layers, n_seq, budget)
+    if n == 0:
+        raise MoeSpecError(ERR_INVALID_ARG, "moespec_evict_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+class _Call:
+    """A C call on one device: its arguments but the stream, and what they point to."""
+
+    def __init__(self, name: str, device: torch.device, args, keep, stream):
+        self._fn, self._name, self._args, self._keep = getattr(load_library(), name), name, args, keep
+        self._device, self._stream = device.index if device.index is not None else torch.cuda.current_device(), stream
+
+    def __call__(self):
+        if torch.cuda.current_device() == self._device:
+            st = self._fn(*self._args, _stream(self._stream))
+        else:
+            with torch.cuda.device(self._device):
+                st = self._fn(*self._args, _stream(self._stream))
+        if st != OK:
+            raise MoeSpecError(int(st), self._name)
+
+
+class _Args:
+    """Pointers of tensors that have to lie on one device."""
+
+    def __init__(self):
+        self.device = None
+
+    def on(self, t: torch.Tensor, name: str):
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a GPU tensor")
+        if self.device is None:
+            self.device = t.device
+        elif t.device != self.device:
+            raise ValueError(f"{name} must be on {self.device}, got {t.device}")
+
+    def ptr(self, t: Optional[torch.Tensor], dtype: torch.dtype, shape, name: str) -> Optional[int]:
+        """Pointer of a contiguous tensor of exactly this shape, or None."""
+        if t is None:
+            return None
+        self.on(t, name)
+        if t.dtype != dtype:
+            raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        return t.data_ptr()
+
+    def rows(self, t: torch.Tensor, dtype: torch.dtype, shape, name: str):
+        """Pointer and row stride of a tensor [.., tokens, heads, head_dim] whose rows are contiguous, wherever they lie."""
+        self.on(t, name)
+        if t.dtype != dtype:
+            raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+        heads, dim = t.shape[-2:]
+        st = t.stride()
+        row = st[-3] if t.shape[-3] > 1 else heads * dim
+        if (dim > 1 and st[-1] != 1) or (heads > 1 and st[-2] != dim) or row < heads * dim or \
+                (len(shape) == 4 and t.shape[0] > 1 and st[0] != t.shape[1] * row):
+            raise ValueError(f"{name}: a token's heads must lie in a row, and rows and layers be equally far apart")
+        return t.data_ptr(), row
+
+    def scratch(self, ws: torch.Tensor):
+        self.on(ws, "ws")
+        if not ws.is_contiguous() or ws.dtype != torch.uint8:
+            raise ValueError("ws must be a contiguous uint8 tensor")
+        return ws.data_ptr(), ws.numel()
+
+
+def _sizes(M: int, tree_off: Optional[torch.Tensor], max_tree: Optional[int]):
+    """Sequences of a batch and the rows of its largest tree: as given, or every token row."""
+    return (1 if tree_off is None else tree_off.numel() - 1), (M if max_tree is None else int(max_tree))
+
+
+def _tree(a: _Args, M: int, n_seq: int, max_tree: int, q_stride: int, kv_stride: int, tree_off, tree_mask) -> Tree:
+    return Tree(n_seq, M, max_tree, q_stride, kv_stride, a.ptr(tree_off, torch.int32, (n_seq + 1,), "tree_off"),
+                a.ptr(tree_mask, torch.int32, (M, (max_tree + 31) // 32), "tree_mask"))
+
+
+class TreeAttentionCall(_Call):
+    """moespec_tree_attention.  q [M, H, D], k_tree, v_tree [M, Hk, D] (views with longer rows are taken as they are); k_cache,
+    v_cache [n_seq, Hk, capacity, D]; cache_len [n_seq] int32; out [M, H, D]; lse [M, H] float32 or None; tree_off [n_seq + 1]
+    int32 or None (one tree of all rows); tree_mask [M, ceil(max_tree / 32)] int32, the packed bits of the trees, or None (chains);
+    max_tree, max_len: bounds on a tree's rows and a cache's entries, M and the capacity if None; max_len 0: no cache."""
+
+    def __init__(self, desc: AttnDesc, q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor,
+                 k_cache: Optional[torch.Tensor], v_cache: Optional[torch.Tensor], cache_len: Optional[torch.Tensor],
+                 ws: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None,
+                 tree_off: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None,
+                 max_tree: Optional[int] = None, max_len: Optional[int] = None, stream=None):
+        a, dt, H, Hk, D = _Args(), desc.torch_dtype, desc.n_heads, desc.n_kv_heads, desc.head_dim
+        M = q.shape[0]
+        S, most = _sizes(M, tree_off, max_tree)
+        max_len = (0 if k_cache is None else desc.capacity) if max_len is None else int(max_len)
+        (qp, qs), (kp, ks) = a.rows(q, dt, (M, H, D), "q"), a.rows(k_tree, dt, (M, Hk, D), "k_tree")
+        vp, vs = a.rows(v_tree, dt, (M, Hk, D), "v_tree")
+        if vs != ks:
+            raise ValueError("k_tree and v_tree must have the same row stride")
+        cache = (S, Hk, desc.capacity, D)
+        self._cd, self._tree = desc.c(), _tree(a, M, S, most, qs, ks, tree_off, tree_mask)
+        args = (ctypes.byref(self._cd), ctypes.byref(self._tree), qp, kp, vp, a.ptr(k_cache, dt, cache, "k_cache"),
+                a.ptr(v_cache, dt, cache, "v_cache"), a.ptr(cache_len, torch.int32, (S,), "cache_len"), max_len,
+                a.ptr(out, dt, (M, H, D), "out"), a.ptr(lse, torch.float32, (M, H), "lse"), *a.scratch(ws))
+        super().__init__("moespec_tree_attention", a.device, args,
+                         (q, k_tree, v_tree, k_cache, v_cache, cache_len, ws, out, lse, tree_off, tree_mask), stream)
+
+
+def moespec_tree_attention(desc: AttnDesc, q, k_tree, v_tree, k_cache=None, v_cache=None, cache_len=None, ws=None, out=None,
+                           lse=None, tree_off=None, tree_mask=None, max_tree=None, max_len=None, stream=None):
+    """Attention of drafted tokens over cache and tree (TreeAttentionCall).  Returns (out, lse).  Without tree_off, rows that are
+    not given are one tree; padding rows of a new `out` are not written."""
+    M = q.shape[0]
+    S, most = _sizes(M, tree_off, max_tree)
+    if out is None:
+        out = torch.empty((M, desc.n_heads, desc.head_dim), dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((M, desc.n_heads), dtype=torch.float32, device=q.device)
+    if ws is None:
+        ws = alloc_attn_workspace(desc, S, M, most, (0 if k_cache is None else desc.capacity) if max_len is None else max_len,
+                                  q.device)
+    TreeAttentionCall(desc, q, k_tree, v_tree, k_cache, v_cache, cache_len, ws, out, lse, tree_off, tree_mask, max_tree,
+                      max_len, stream)()
+    return out, lse
+
+
+class CacheWeightsCall(_Call):
+    """moespec_cache_weights: the attention weight that every key received.  Tensors as in TreeAttentionCall; lse [M, H] float32;
+    cache_w, cache_w_in [n_seq, Hk, capacity] float32 (cache_w = decay * cache_w_in + weight; cache_w_in may be cache_w or
+    None); tree_w [M, Hk] float32 or None; row_weight [M] float32 or None."""
+
+    def __init__(self, desc: AttnDesc, q: torch.Tensor, k_tree: torch.Tensor, k_cache: Optional[torch.Tensor],
+                 cache_len: Optional[torch.Tensor], lse: torch.Tensor, ws: torch.Tensor, cache_w: Optional[torch.Tensor],
+                 tree_w: Optional[torch.Tensor] = None, cache_w_in: Optional[torch.Tensor] = None, decay: float = 1.0,
+                 row_weight: Optional[torch.Tensor] = None, tree_off: Optional[torch.Tensor] = None,
+                 tree_mask: Optional[torch.Tensor] = None, max_tree: Optional[int] = None, max_len: Optional[int] = None,
+                 stream=None):
+        a, dt, H, Hk, D = _Args(), desc.torch_dtype, desc.n_heads, desc.n_kv_heads, desc.head_dim
+        M = q.shape[0]
+        S, most = _sizes(M, tree_off, max_tree)
+        max_len = (0 if k_cache is None else desc.capacity) if max_len is None else int(max_len)
+        (qp, qs), (kp, ks) = a.rows(q, dt, (M, H, D), "q"), a.rows(k_tree, dt, (M, Hk, D), "k_tree")
+        self._cd, self._tree = desc.c(), _tree(a, M, S, most, qs, ks, tree_off, tree_mask)
+        w = (S, Hk, desc.capacity)
+        args = (ctypes.byref(self._cd), ctypes.byref(self._tree), qp, kp, a.ptr(k_cache, dt, (*w, D), "k_cache"),
+                a.ptr(cache_len, torch.int32, (S,), "cache_len"), max_len, a.ptr(lse, torch.float32, (M, H), "lse"),
+                a.ptr(row_weight, torch.float32, (M,), "row_weight"), float(decay),
+                a.ptr(cache_w_in, torch.float32, w, "cache_w_in"), a.ptr(cache_w, torch.float32, w, "cache_w"),
+                a.ptr(tree_w, torch.float32, (M, Hk), "tree_w"), *a.scratch(ws))
+        super().__init__("moespec_cache_weights", a.device, args,
+                         (q, k_tree, k_cache, cache_len, lse, ws, cache_w, tree_w, cache_w_in, row_weight, tree_off, tree_mask),
+                         stream)
+
+
+def moespec_cache_weights(desc: AttnDesc, q, k_tree, k_cache, cache_len, lse, ws=None, cache_w=None, tree_w=None, cache_w_in=None,
+                          decay=1.0, row_weight=None, tree_off=None, tree_mask=None, max_tree=None, max_len=None, stream=None):
+    """Weight that every cached key and every key of the trees received (CacheWeightsCall).  Returns (cache_w, tree_w)."""
+    M = q.shape[0]
+    S, most = _sizes(M, tree_off, max_tree)
+    if cache_w is None and k_cache is not None:
+        cache_w = torch.zeros((S, desc.n_kv_heads, desc.capacity), dtype=torch.float32, device=q.device)
+    if tree_w is None:
+        tree_w = torch.zeros((M, desc.n_kv_heads), dtype=torch.float32, device=q.device)
+    if ws is None:
+        ws = alloc_attn_workspace(desc, S, M, most, (0 if k_cache is None else desc.capacity) if max_len is None else max_len,
+                                  q.device)
+    CacheWeightsCall(desc, q, k_tree, k_cache, cache_len, lse, ws, cache_w, tree_w, cache_w_in, decay, row_weight, tree_off,
+                     tree_mask, max_tree, max_len, stream)()
+    return cache_w, tree_w
+
+
+class CacheCommitCall(_Call):
+    """moespec_cache_commit: the accepted path appended to the caches of n_layers layers.  k_tree, v_tree [n_layers, M, Hk, D];
+    path [n_seq, max_path] int32; n_path, cache_len, new_len [n_seq] int32; k_cache, v_cache [n_layers, n_seq, Hk, capacity, D];
+    tree_w [n_layers, M, Hk] and cache_w [n_layers, n_seq, Hk, capacity] float32, both or neither."""
+
+    def __init__(self, desc: AttnDesc, k_tree: torch.Tensor, v_tree: torch.Tensor, path: torch.Tensor, n_path: torch.Tensor,
+                 k_cache: torch.Tensor, v_cache: torch.Tensor, cache_len: torch.Tensor,
+                 new_len: Optional[torch.Tensor] = None, tree_w: Optional[torch.Tensor] = None,
+                 cache_w: Optional[torch.Tensor] = None, tree_off: Optional[torch.Tensor] = None,
+                 max_tree: Optional[int] = None, n_layers: int = 1, stream=None):
+        a, dt, Hk, D, L, i32 = _Args(), desc.torch_dtype, desc.n_kv_heads, desc.head_dim, int(n_layers), torch.int32
+        M = k_tree.shape[-3]
+        S, most = _sizes(M, tree_off, max_tree)
+        (kp, ks), (vp, vs) = a.rows(k_tree, dt, (L, M, Hk, D), "k_tree"), a.rows(v_tree, dt, (L, M, Hk, D), "v_tree")
+        if vs != ks:
+            raise ValueError("k_tree and v_tree must have the same row stride")
+        self._cd, self._tree = desc.c(), _tree(a, M, S, most, 0, ks, tree_off, None)
+        w = (L, S, Hk, desc.capacity)
+        n = path.shape[-1]
+        args = (ctypes.byref(self._cd), L, ctypes.byref(self._tree), kp, vp, a.ptr(tree_w, torch.float32, (L, M, Hk), "tree_w"),
+                a.ptr(path, i32, (S, n), "path"), a.ptr(n_path, i32, (S,), "n_path"), n, a.ptr(k_cache, dt, (*w, D), "k_cache"),
+                a.ptr(v_cache, dt, (*w, D), "v_cache"), a.ptr(cache_w, torch.float32, w, "cache_w"),
+                a.ptr(cache_len, i32, (S,), "cache_len"), a.ptr(new_len, i32, (S,), "new_len"))
+        super().__init__("moespec_cache_commit", a.device, args,
+                         (k_tree, v_tree, path, n_path, k_cache, v_cache, cache_len, new_len, tree_w, cache_w, tree_off), stream)
+
+
+def moespec_cache_commit(desc: AttnDesc, k_tree, v_tree, path, n_path, k_cache, v_cache, cache_len, new_len=None, tree_w=None,
+                         cache_w=None, tree_off=None, max_tree=None, n_layers=1, stream=None) -> torch.Tensor:
+    """Accepted paths appended to the caches, in place (CacheCommitCall).  Returns new_len."""
+    if new_len is None:
+        new_len = torch.empty_like(cache_len)
+    CacheCommitCall(desc, k_tree, v_tree, path, n_path, k_cache, v_cache, cache_len, new_len, tree_w, cache_w, tree_off, max_tree,
+                    n_layers, stream)()
+    return new_len
+
+
+class CacheEvictCall(_Call):
+    """moespec_cache_evict: caches [n_layers, n_seq, Hk, capacity, D] with weights [n_layers, n_seq, Hk, capacity] float32 cut to
+    `budget` entries, the `recent` last ones among them, into k_out, v_out, w_out (the same with a capacity of their own).  kept
+    [n_layers, n_seq, Hk, budget] int32 and new_len [n_seq] int32 may be None."""
+
+    def __init__(self, desc: AttnDesc, k_cache: torch.Tensor, v_cache: torch.Tensor, cache_w: torch.Tensor,
+                 cache_len: torch.Tensor, budget: int, recent: int, k_out: torch.Tensor, v_out: torch.Tensor,
+                 w_out: torch.Tensor, ws: torch.Tensor, kept: Optional[torch.Tensor] = None,
+                 new_len: Optional[torch.Tensor] = None, n_layers: int = 1, stream=None):
+        a, dt, Hk, D, L, i32 = _Args(), desc.torch_dtype, desc.n_kv_heads, desc.head_dim, int(n_layers), torch.int32
+        S, room = cache_len.numel(), k_out.shape[-2]
+        w, o = (L, S, Hk, desc.capacity), (L, S, Hk, room)
+        self._cd = desc.c()
+        args = (ctypes.byref(self._cd), L, S, a.ptr(k_cache, dt, (*w, D), "k_cache"), a.ptr(v_cache, dt, (*w, D), "v_cache"),
+                a.ptr(cache_w, torch.float32, w, "cache_w"), a.ptr(cache_len, i32, (S,), "cache_len"), int(budget), int(recent),
+                room, a.ptr(k_out, dt, (*o, D), "k_out"), a.ptr(v_out, dt, (*o, D), "v_out"),
+                a.ptr(w_out, torch.float32, o, "w_out"), a.ptr(kept, i32, (L, S, Hk, int(budget)), "kept"),
+                a.ptr(new_len, i32, (S,), "new_len"), *a.scratch(ws))
+        super().__init__("moespec_cache_evict", a.device, args,
+                         (k_cache, v_cache, cache_w, cache_len, k_out, v_out, w_out, ws, kept, new_len), stream)
+
+
+def moespec_cache_evict(desc: AttnDesc, k_cache, v_cache, cache_w, cache_len, budget, recent, n_layers=1, stream=None):
+    """Caches cut to a budget (CacheEvictCall).  Returns dict(k, v, w, kept, new_len); entries of k, v, w behind new_len are 0."""
+    L, S, Hk, D, dev = int(n_layers), cache_len.numel(), desc.n_kv_heads, desc.head_dim, k_cache.device
+    n = max(int(budget), 1)
+    k, v = (torch.zeros((L, S, Hk, n, D), dtype=k_cache.dtype, device=dev) for _ in range(2))
+    w = torch.zeros((L, S, Hk, n), dtype=torch.float32, device=dev)
+    kept = torch.empty((L, S, Hk, n), dtype=torch.int32, device=dev)
+    new_len = torch.empty_like(cache_len)
+    ws = torch.empty(max(evict_workspace_bytes(desc, L, S, n), 1), dtype=torch.uint8, device=dev)
+    CacheEvictCall(desc, k_cache, v_cache, cache_w, cache_len, budget, recent, k, v, w, ws, kept if budget == n else None, new_len,
+                   n_layers, stream)()
+    return dict(k=k, v=v, w=w, kept=kept, new_len=new_len)
+
+
+class BlockNormCall(_Call):
+    """moespec_block_norm: r = residual + scale * gate * norm(y), x = norm(r).  y, residual, r, x [M, d] in the layer's dtype
+    (residual None: 0; r or x None: not wanted); w_post, w_pre [d] or None; gate by gate_kind: [d], [M], [M, d] or None."""
+
+    def __init__(self, desc: LayerDesc, y: torch.Tensor, residual: Optional[torch.Tensor], r: Optional[torch.Tensor],
+                 x: Optional[torch.Tensor], post_norm: bool = False, w_post: Optional[torch.Tensor] = None,
+                 gate: Optional[torch.Tensor] = None, gate_kind: int = BLOCK_GATE_NONE, gate_sigmoid: bool = False,
+                 scale: float = 1.0, w_pre: Optional[torch.Tensor] = None, eps: float = 0.0, stream=None):
+        a, dt, d = _Args(), desc.torch_dtype, desc.d
+        M = y.shape[0]
+        shapes = {BLOCK_GATE_CHANNEL: (d,), BLOCK_GATE_TOKEN: (M,), BLOCK_GATE_ELEMENT: (M, d)}
+        yp = a.ptr(y, dt, (M, d), "y")
+        self._cd = desc.c()
+        self._block = Block(int(bool(post_norm)), int(gate_kind), int(bool(gate_sigmoid)), scale, eps,
+                            a.ptr(w_post, dt, (d,), "w_post"), a.ptr(gate, dt, shapes.get(gate_kind, ()), "gate"),
+                            a.ptr(w_pre, dt, (d,), "w_pre"))
+        args = (ctypes.byref(self._cd), ctypes.byref(self._block), yp, a.ptr(residual, dt, (M, d), "residual"), M,
+                a.ptr(r, dt, (M, d), "r"), a.ptr(x, dt, (M, d), "x"))
+        super().__init__("moespec_block_norm", a.device, args, (y, residual, r, x, w_post, gate, w_pre), stream)
+
+
+def moespec_block_norm(desc: LayerDesc, y, residual=None, r=None, x=None, post_norm=False, w_post=None, gate=None,
+                       gate_kind=BLOCK_GATE_NONE, gate_sigmoid=False, scale=1.0, w_pre=None, eps=0.0, stream=None):
+    """From a block's output to the residual stream and the next block's input (BlockNormCall).  Returns (r, x)."""
+    r = torch.empty_like(y) if r is None else r
+    x = torch.empty_like(y) if x is None else x
+    BlockNormCall(desc, y, residual, r, x, post_norm, w_post, gate, gate_kind, gate_sigmoid, scale, w_pre, eps, stream)()
+    return r, x

@@ -10,7 +10,8 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libmoespec.so")
-SOURCES = ("api.hip", "route.hip", "budget.hip", "prologue.hip", "expert_ffn.hip", "expert_wide.hip", "analysis.hip", "stack.hip")
+SOURCES = ("api.hip", "route.hip", "budget.hip", "prologue.hip", "expert_ffn.hip", "expert_wide.hip", "analysis.hip", "stack.hip",
+           "attention.hip", "cache_weights.hip", "cache.hip", "block_norm.hip", "attention_api.hip")
 
 # The first 14 words of a kernel's arguments arrive in scalar registers (kernarg preload) instead of by a load from cold
 # memory: 0.1 to 0.2 us of every launch.  Kernels name the arguments that their first loads need first.

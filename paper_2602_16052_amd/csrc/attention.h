@@ -1,0 +1,114 @@
+// What the kernels over a cache of keys share: where a sequence's rows and entries lie, and how tiles of keys lie in LDS.
+#pragma once
+
+#include "common.h"
+
+namespace moespec {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+
+constexpr int kMaxSplits = 256;  // parts of a sequence's keys that one combine joins
+
+// The arguments that say which rows and entries there are (host pointers resolved, strides in elements, never 0).
+struct KeyArgs {
+  const void *q, *k_tree, *v_tree, *k_cache, *v_cache;
+  const int32_t *cache_len, *tree_off;
+  const uint32_t *tree_mask;
+  int64_t q_stride, kv_stride, capacity;
+  int n_seq, M, max_tree, words, max_len, H, Hk, G;
+  float c;  // scale * log2(e): scores in units of log 2
+};
+
+// One sequence: first token row, rows of its tree, entries of its cache.  Device data, clamped to what the buffers hold.
+struct SeqGeom {
+  int row0, T, len;
+};
+__device__ __forceinline__ SeqGeom seq_geom(const KeyArgs &a, int s) {
+  SeqGeom g{0, a.M, 0};
+  if (a.tree_off) {
+    g.row0 = min(max(a.tree_off[s], 0), a.M);
+    g.T = min(max(a.tree_off[s + 1], g.row0), a.M) - g.row0;
+  }
+  g.T = min(g.T, a.max_tree);
+  if (a.max_len > 0) g.len = min(max(a.cache_len[s], 0), a.max_len);
+  return g;
+}
+
+__host__ __device__ constexpr int pow2_ceil(int x) {
+  int p = 1;
+  while (p < x) p <<= 1;
+  return p;
+}
+
+// A tile of rows of D elements in LDS: a row is kSlots slots of 16 bytes (a power of two; the row's pieces and padding that is
+// never read).  Piece p of row r sits in slot p ^ swz(r).  Reads of the same piece of 16 consecutive rows (keys as a matrix operand) then
+// touch every bank once, and so do reads of the same 64 bytes of 4 rows in a row (values, transposed on the way out of LDS).
+template <typename T, int D>
+struct Rows {
+  static constexpr int kPieceElems = 16 / (int)sizeof(T);
+  static constexpr int kPieces = D / kPieceElems;
+  static constexpr int kSlots = pow2_ceil(kPieces);
+  static constexpr int kBytes = 16 * kSlots;
+  static __device__ __forceinline__ int swz(int row) {
+    return kSlots == 8 ? 4 * ((row >> 1) & 1) + ((row >> 2) & 3) : 4 * (row & 3) + ((row >> 2) & 3);
+  }
+};
+
+// The matrix operands of 32 rows x D: step i multiplies pieces 2 i (lanes 0-31) and 2 i + 1 (lanes 32-63) of every row, so
+// that both operands load 16 bytes per lane and the order of the sum over D is the same in both.
+template <typename T>
+struct Frag;
+template <>
+struct Frag<uint16_t> {
+  typedef bf16x8 type;
+  static __device__ __forceinline__ f32x16 mma(type a, type b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Frag<float> {
+  typedef f32x4 type;
+  static __device__ __forceinline__ f32x16 mma(type a, type b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// Row (of 32) of element i of a lane's 32 x 32 result; half = lane >> 5.  The column is lane & 31.
+__device__ __forceinline__ int acc_row(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
+
+// v of lane ^ 32 combined with the lane's own.
+__device__ __forceinline__ float half_swap(float v, bool max_) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  const float a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
+  return max_ ? fmaxf(a, b) : a + b;
+}
+
+// Which of the 32 keys base .. base + 31 (of n) a row sees: all of a cache, a token's ancestors in its tree.
+__device__ __forceinline__ uint32_t keys_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t tree_word(const KeyArgs &a, const SeqGeom &g, int t, int base) {
+  if (base >= g.T) return 0;
+  const uint32_t w = a.tree_mask ? a.tree_mask[(size_t)(g.row0 + t) * a.words + (base >> 5)] : keys_below(t + 1 - base);
+  return w & keys_below(g.T - base);
+}
+
+hipError_t launch_tree_attention(const moespec_attn_desc &ds, const KeyArgs &a, void *out, float *lse, void *ws,
+                                 hipStream_t st);
+size_t tree_attention_ws(const moespec_attn_desc &ds, int64_t n_seq, int64_t max_tree, int64_t max_len);
+hipError_t launch_cache_weights(const moespec_attn_desc &ds, const KeyArgs &a, const float *lse, const float *row_weight,
+                                float decay, const float *w_in, float *w_out, float *tree_w, void *ws, hipStream_t st);
+size_t cache_weights_ws(const moespec_attn_desc &ds, int64_t n_seq, int64_t max_tree, int64_t max_len);
+hipError_t launch_cache_commit(const moespec_attn_desc &ds, int n_layers, const moespec_tree &tree, const void *k_tree,
+                               const void *v_tree, const float *tree_w, const int32_t *path, const int32_t *n_path,
+                               int max_path, void *k_cache, void *v_cache, float *cache_w, const int32_t *cache_len,
+                               int32_t *new_len, hipStream_t st);
+hipError_t launch_cache_evict(const moespec_attn_desc &ds, int n_layers, int n_seq, const void *k_cache,
+                              const void *v_cache, const float *cache_w, const int32_t *cache_len, int budget, int recent,
+                              int out_capacity, void *k_out, void *v_out, float *w_out, int32_t *kept, int32_t *new_len,
+                              hipStream_t st);
+hipError_t launch_block_norm(const moespec_desc &ds, const moespec_block &b, const void *y, const void *residual, int M,
+                             void *r, void *x, hipStream_t st);
+
+}  // namespace moespec

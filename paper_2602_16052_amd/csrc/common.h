@@ -150,6 +150,27 @@ __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// 64 lanes x 16 bytes from base + voff (per lane) to LDS bytes [lds, lds + 1024), lane after lane.  Completion is
+// counted by vmcnt in issue order; the compiler does not see the load, so the waits are written by hand.  m0 is a register
+// that the compiler reserves for sequences of its own, and warns about in a clobber list; named there, it keeps a value of
+// its own in m0 from being carried across.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma_to_lds(uint32_t lds, const void *base, uint32_t voff) {
+  const uint64_t b = reinterpret_cast<uint64_t>(base);  // uniform, and the compiler is told so
+  const uint64_t ub = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32 |
+                      (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(
+                   __builtin_amdgcn_readfirstlane(lds)),
+               "v"(voff), "s"(ub)
+               : "m0", "memory");
+}
+#pragma clang diagnostic pop
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
+}
+
 // Ranks before nothing: every comparison with it is false, whatever the other value (also an infinity or a log-probability).
 constexpr double kNoRival = __builtin_nan("");
 
