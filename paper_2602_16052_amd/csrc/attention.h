@@ -94,6 +94,34 @@ __device__ __forceinline__ uint32_t tree_word(const KeyArgs &a, const SeqGeom &g
   return w & keys_below(g.T - base);
 }
 
+// What a lane holds of a finished row (elements acc_row(i, half) of every 32; m in units of log 2) written out, or left for the
+// combine where the row's keys are in n_split parts.
+template <typename T, int D>
+__device__ __forceinline__ void finish_row(const KeyArgs &a, const f32x16 (&o)[D / 32], float m, float l, int s, int split,
+                                           int n_split, int t, int h, size_t orow, int half, T *out, float *lse, float *part,
+                                           float2 *part_ml) {
+  if (n_split == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        Elem<T>::store4(out + orow * D + 32 * b + acc_row(i, half),
+                        f32x4{o[b][i] * inv, o[b][i + 1] * inv, o[b][i + 2] * inv, o[b][i + 3] * inv});
+    if (lse && half == 0) lse[orow] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
+  } else {
+    const size_t at = ((size_t)split * a.n_seq + s) * a.max_tree * a.H + (size_t)t * a.H + h;
+    if (half == 0) part_ml[at] = make_float2(m, l);
+    if (m == -INFINITY) return;  // the combine passes it over
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<f32x4 *>(part + at * D + 32 * b + acc_row(i, half)) =
+            f32x4{o[b][i], o[b][i + 1], o[b][i + 2], o[b][i + 3]};
+  }
+}
+
 hipError_t launch_tree_attention(const moespec_attn_desc &ds, const KeyArgs &a, void *out, float *lse, void *ws,
                                  hipStream_t st);
 size_t tree_attention_ws(const moespec_attn_desc &ds, int64_t n_seq, int64_t max_tree, int64_t max_len);

@@ -23,6 +23,160 @@ struct AttnShape {
   static constexpr int kKb4 = kRow <= 256 && sizeof(T) == 2 ? 2 : 1;  // 32-key blocks of a wave with 128 rows a workgroup
 };
 
+// One tile of 32 KB keys, base .. of n, that lies in LDS at kt, vt, taken into a wave's 32 rows (row l31 is token t; no token of
+// the workgroup is in front of first_t): scores, masks, running maximum and sum, values.
+template <typename T, int D, int KB>
+__device__ __forceinline__ void attend_tile(const KeyArgs &a, const SeqGeom &g, bool tree, int base, int n, int t, int first_t,
+                                            const unsigned char *kt, const unsigned char *vt,
+                                            const typename Frag<T>::type (&q)[Rows<T, D>::kPieces / 2], f32x16 (&o)[D / 32],
+                                            float &m, float &l) {
+  typedef Rows<T, D> R;
+  typedef typename Frag<T>::type frag;
+  constexpr int NB = D / 32, NS = R::kPieces / 2;
+  const int lane = threadIdx.x & 63, l31 = lane & 31, half = lane >> 5;
+  f32x16 sc[KB];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const frag kf =
+          *reinterpret_cast<const frag *>(kt + (32 * kb + l31) * R::kBytes + (((2 * i + half) ^ R::swz(l31)) << 4));
+      sc[kb] = Frag<T>::mma(kf, q[i], sc[kb]);
+    }
+  }
+  // A stage inside the cache, or in front of every row's own token in a chain, is seen whole.
+  uint32_t word[KB];
+  const bool whole = base + 32 * KB <= n && (!tree || (a.tree_mask == nullptr && base + 32 * KB - 1 <= first_t));
+  if (!whole) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      word[kb] = tree ? tree_word(a, g, t, base + 32 * kb) : keys_below(n - base - 32 * kb);
+      const uint32_t w = word[kb] >> (4 * half);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!((w >> acc_row(i, 0)) & 1u)) sc[kb][i] = -INFINITY;
+    }
+  }
+  float mx = sc[0][0];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[kb][i]);
+  mx = half_swap(mx, true) * a.c;
+  // The maximum is only raised when it is passed by more than 2^8: until then the weights stay below 2^8, in fp32 and in
+  // bf16 as exact as below 1, and O is not rescaled.
+  const bool raise = mx > m + 8.f;
+  if (__ballot(raise) != 0) {
+    const float alpha = raise ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
+    m = raise ? mx : m;
+    l *= alpha;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
+  }
+  const float mu = m == -INFINITY ? 0.f : m;  // nothing seen so far: all weights are 0
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      sc[kb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][i], a.c, -mu));
+      l += sc[kb][i];
+    }
+
+  // A weight of 0 times a NaN or an infinity would reach a token that does not see that key.  Keys of the tree with such a
+  // value are found first; their values enter the product as 0 and are added to the rows that see them.
+  uint32_t odd[KB];
+  uint32_t any_odd = 0;
+  if (tree && !whole) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      uint32_t bad = 0;
+#pragma unroll
+      for (int p = 0; p < NS; ++p) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(vt + (32 * kb + l31) * R::kBytes + (((2 * p + half) ^ R::swz(l31)) << 4));
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          bad |= (w[e] & 0x7f800000u) == 0x7f800000u;
+          if (sizeof(T) == 2) bad |= (w[e] & 0x7f80u) == 0x7f80u;
+        }
+      }
+      const unsigned long long b = __ballot(bad != 0);
+      odd[kb] = (uint32_t)b | (uint32_t)(b >> 32);
+      any_odd |= odd[kb];
+    }
+  }
+  auto values = [&](auto clean) {
+    constexpr bool kClean = decltype(clean)::value;  // non-finite values replaced by 0
+    if constexpr (sizeof(T) == 2) {
+      typedef __attribute__((address_space(3))) bf16x4 lds4;
+      const int i16 = lane & 15, vrow = 4 * half + (i16 >> 2), low = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          bf16x8 p;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) p[i] = (__bf16)sc[kb][8 * j + i];
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const int ra = 32 * kb + 16 * j + vrow, rb = ra + 8;
+            bf16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+                (lds4 *)(vt + ra * R::kBytes + (((4 * b + low) ^ R::swz(ra)) << 4) + 8 * (i16 & 1)));
+            bf16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+                (lds4 *)(vt + rb * R::kBytes + (((4 * b + low) ^ R::swz(rb)) << 4) + 8 * (i16 & 1)));
+            bf16x8 v = __builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7);
+            if constexpr (kClean) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if ((__float_as_uint((float)v[e]) & 0x7f800000u) == 0x7f800000u) v[e] = (__bf16)0.f;
+            }
+            o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, o[b], 0, 0, 0);
+          }
+        }
+    } else {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int vr = 32 * kb + acc_row(i, half);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            float v = *reinterpret_cast<const float *>(vt + vr * R::kBytes +
+                                                       (((8 * b + (l31 >> 2)) ^ R::swz(vr)) << 4) + 4 * (l31 & 3));
+            if constexpr (kClean)
+              if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) v = 0.f;
+            o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, sc[kb][i], o[b], 0, 0, 0);
+          }
+        }
+    }
+  };
+  if (any_odd == 0) {
+    values(std::false_type{});
+  } else {
+    values(std::true_type{});
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+      for (uint32_t left = odd[kb]; left != 0; left &= left - 1) {
+        const int j = __builtin_ctz(left), vr = 32 * kb + j;
+        const bool seen = (word[kb] >> j) & 1u;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int e = 32 * b + acc_row(i, half);
+            const float v = Elem<T>::load(reinterpret_cast<const T *>(
+                vt + vr * R::kBytes + ((e / R::kPieceElems ^ R::swz(vr)) << 4) + sizeof(T) * (e % R::kPieceElems)));
+            if (seen && (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[b][i] += v;
+          }
+      }
+  }
+}
+
+
 template <typename T, int D, int WR, int WK, int KB>
 __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attention_kernel(
     KeyArgs a, int row_tiles, int n_split, T *__restrict__ out, float *__restrict__ lse, float *__restrict__ part,
@@ -98,146 +252,7 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
     const bool tree = st >= ct;
     const int base = (tree ? st - ct : st) * kStageKeys + wk * KB * 32, n = tree ? g.T : g.len;
 
-    f32x16 sc[KB];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
-#pragma unroll
-      for (int i = 0; i < NS; ++i) {
-        const frag kf =
-            *reinterpret_cast<const frag *>(kt + (32 * kb + l31) * R::kBytes + (((2 * i + half) ^ R::swz(l31)) << 4));
-        sc[kb] = Frag<T>::mma(kf, q[i], sc[kb]);
-      }
-    }
-    // A stage inside the cache, or in front of every row's own token in a chain, is seen whole.
-    uint32_t word[KB];
-    const bool whole = base + 32 * KB <= n && (!tree || (a.tree_mask == nullptr && base + 32 * KB - 1 <= r0 / a.G));
-    if (!whole) {
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        word[kb] = tree ? tree_word(a, g, t, base + 32 * kb) : keys_below(n - base - 32 * kb);
-        const uint32_t w = word[kb] >> (4 * half);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (!((w >> acc_row(i, 0)) & 1u)) sc[kb][i] = -INFINITY;
-      }
-    }
-    float mx = sc[0][0];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[kb][i]);
-    mx = half_swap(mx, true) * a.c;
-    // The maximum is only raised when it is passed by more than 2^8: until then the weights stay below 2^8, in fp32 and in
-    // bf16 as exact as below 1, and O is not rescaled.
-    const bool raise = mx > m + 8.f;
-    if (__ballot(raise) != 0) {
-      const float alpha = raise ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
-      m = raise ? mx : m;
-      l *= alpha;
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
-    }
-    const float mu = m == -INFINITY ? 0.f : m;  // nothing seen so far: all weights are 0
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[kb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][i], a.c, -mu));
-        l += sc[kb][i];
-      }
-
-    // A weight of 0 times a NaN or an infinity would reach a token that does not see that key.  Keys of the tree with such a
-    // value are found first; their values enter the product as 0 and are added to the rows that see them.
-    uint32_t odd[KB];
-    uint32_t any_odd = 0;
-    if (tree && !whole) {
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        uint32_t bad = 0;
-#pragma unroll
-        for (int p = 0; p < NS; ++p) {
-          const uint4 v = *reinterpret_cast<const uint4 *>(vt + (32 * kb + l31) * R::kBytes + (((2 * p + half) ^ R::swz(l31)) << 4));
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            bad |= (w[e] & 0x7f800000u) == 0x7f800000u;
-            if (sizeof(T) == 2) bad |= (w[e] & 0x7f80u) == 0x7f80u;
-          }
-        }
-        const unsigned long long b = __ballot(bad != 0);
-        odd[kb] = (uint32_t)b | (uint32_t)(b >> 32);
-        any_odd |= odd[kb];
-      }
-    }
-    auto values = [&](auto clean) {
-      constexpr bool kClean = decltype(clean)::value;  // non-finite values replaced by 0
-      if constexpr (sizeof(T) == 2) {
-        typedef __attribute__((address_space(3))) bf16x4 lds4;
-        const int i16 = lane & 15, vrow = 4 * half + (i16 >> 2), low = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            bf16x8 p;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = (__bf16)sc[kb][8 * j + i];
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-              const int ra = 32 * kb + 16 * j + vrow, rb = ra + 8;
-              bf16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-                  (lds4 *)(vt + ra * R::kBytes + (((4 * b + low) ^ R::swz(ra)) << 4) + 8 * (i16 & 1)));
-              bf16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-                  (lds4 *)(vt + rb * R::kBytes + (((4 * b + low) ^ R::swz(rb)) << 4) + 8 * (i16 & 1)));
-              bf16x8 v = __builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7);
-              if constexpr (kClean) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                  if ((__float_as_uint((float)v[e]) & 0x7f800000u) == 0x7f800000u) v[e] = (__bf16)0.f;
-              }
-              o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, o[b], 0, 0, 0);
-            }
-          }
-      } else {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int vr = 32 * kb + acc_row(i, half);
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-              float v = *reinterpret_cast<const float *>(vt + vr * R::kBytes +
-                                                         (((8 * b + (l31 >> 2)) ^ R::swz(vr)) << 4) + 4 * (l31 & 3));
-              if constexpr (kClean)
-                if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) v = 0.f;
-              o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, sc[kb][i], o[b], 0, 0, 0);
-            }
-          }
-      }
-    };
-    if (any_odd == 0) {
-      values(std::false_type{});
-    } else {
-      values(std::true_type{});
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-        for (uint32_t left = odd[kb]; left != 0; left &= left - 1) {
-          const int j = __builtin_ctz(left), vr = 32 * kb + j;
-          const bool seen = (word[kb] >> j) & 1u;
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int e = 32 * b + acc_row(i, half);
-              const float v = Elem<T>::load(reinterpret_cast<const T *>(
-                  vt + vr * R::kBytes + ((e / R::kPieceElems ^ R::swz(vr)) << 4) + sizeof(T) * (e % R::kPieceElems)));
-              if (seen && (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[b][i] += v;
-            }
-        }
-    }
+    attend_tile<T, D, KB>(a, g, tree, base, n, t, r0 / a.G, kt, vt, q, o, m, l);
   }
   l = half_swap(l, false);
   if (m == -INFINITY && l != 0.f) m = 0.f;  // scores that are all NaN: so is the row
@@ -286,163 +301,451 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
     m = mt;
     l = lt;
   }
-  if (!row_ok) return;
-  if (n_split == 1) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (row_ok) finish_row<T, D>(a, o, m, l, s, split, n_split, t, h, orow, half, out, lse, part, part_ml);
+}
+
+// ---- Many rows per KV head (bf16, D <= 128): bound by arithmetic.
+//
+// A workgroup of four waves takes 256 rows, a wave 64 of them: every operand that is read from LDS is multiplied twice, which
+// halves the LDS traffic that equals the time of the matrix instructions at 32 rows.  One wave per SIMD has all 512 registers and
+// overlaps its own work: in one straight line of code the matrix instructions of S(i + 1) = K Q^T run beside the exponentials of
+// S(i), those of O += V^T P(i) beside the rest of them and beside the maxima of S(i + 1).  Keys and values of the tiles come
+// through two places each, K one tile ahead of V; one barrier per tile.
+// Tiles that some row sees in part (the cache's last one, those of the tree) follow one by one.
+template <int D>
+struct WideShape {
+  static constexpr int kKeys = 64, kTile = kKeys * Rows<uint16_t, D>::kBytes, kLds = 4 * kTile;
+};
+
+// s (+)= a b with s and a in the registers that other instructions can read, b in the accumulation registers.  Left to the compiler,
+// scores land in accumulation registers and cost a copy each.  The result is there 16 passes later: no instruction may read s before
+// other matrix instructions have been issued and waited for.
+__device__ __forceinline__ void score_mfma(f32x16 &s, bf16x8 a, bf16x8 b, bool first) {
+  if (first)
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b));
+  else
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b));
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, int row_tiles, int n_split,
+                                                                     uint16_t *__restrict__ out, float *__restrict__ lse,
+                                                                     float *__restrict__ part, float2 *__restrict__ part_ml) {
+  typedef Rows<uint16_t, D> R;
+  typedef WideShape<D> W;
+  typedef __attribute__((address_space(3))) bf16x4 lds4;
+  constexpr int NB = D / 32, NS = R::kPieces / 2, kLoads = W::kTile / 1024 / 4, kRowsPerLoad = 64 / R::kSlots;
+  constexpr int kSteps1 = 2 * NS, kSteps2 = 4 * NB;  // pairs of matrix instructions of S and of O
+  extern __shared__ __align__(16) unsigned char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l31 = lane & 31, half = lane >> 5;
+  const int slot = blockIdx.x / 8, group = slot / row_tiles * 8 + (int)(blockIdx.x % 8), tile = slot % row_tiles;
+  if (group >= a.n_seq * a.Hk * n_split) return;
+  const int split = group % n_split, hk = group / n_split % a.Hk, s = group / n_split / a.Hk;
+  const SeqGeom g = seq_geom(a, s);
+  const int n_rows = g.T * a.G, r0 = tile * 256;
+  if (r0 >= n_rows) return;
+  const int first_t = r0 / a.G, last_t = (min(r0 + 256, n_rows) - 1) / a.G;
+
+  // tiles that every row sees whole: of the cache, then of a chain in front of the first row's token; the others behind them
+  const int cache_whole = g.len / 64, whole = cache_whole + (a.tree_mask ? 0 : (first_t + 1) / 64);
+  const int cache_rest = (g.len + 63) / 64 - cache_whole;
+  const int all = whole + cache_rest + (a.tree_mask ? (g.T + 63) / 64 : last_t / 64 + 1 - (first_t + 1) / 64);
+  const int chunk = (all + n_split - 1) / n_split;
+  const int x0 = split * chunk, x1 = min(x0 + chunk, all);
+
+  int t[2], h[2];
+#pragma unroll
+  for (int rb = 0; rb < 2; ++rb) {
+    const int row = min(r0 + 64 * wave + 32 * rb + l31, n_rows - 1);
+    t[rb] = row / a.G;
+    h[rb] = hk * a.G + row % a.G;
+  }
+  auto load_q = [&](bf16x8(&q)[NS], int rb) {
+    const uint16_t *qp = static_cast<const uint16_t *>(a.q) + (g.row0 + t[rb]) * a.q_stride + h[rb] * D + 8 * half;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) q[i] = *reinterpret_cast<const bf16x8 *>(qp + 16 * i);
+  };
+  f32x16 o[2][NB];
+#pragma unroll
+  for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        Elem<T>::store4(out + orow * D + 32 * b + acc_row(i, half),
-                        f32x4{o[b][i] * inv, o[b][i + 1] * inv, o[b][i + 2] * inv, o[b][i + 3] * inv});
-    if (lse && half == 0) lse[orow] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
-  } else {
-    const size_t at = ((size_t)split * a.n_seq + s) * a.max_tree * a.H + (size_t)t * a.H + h;
-    if (half == 0) part_ml[at] = make_float2(m, l);
-    if (m == -INFINITY) return;  // the combine passes it over
+      for (int i = 0; i < 16; ++i) o[rb][b][i] = 0.f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds);
+  const int64_t head = ((int64_t)s * a.Hk + hk) * a.capacity * D;
+  // this wave's share of a tile of which n keys are there
+  auto fetch = [&](const void *src, int64_t stride, int n, uint32_t dst) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+    for (int i = 0; i < kLoads; ++i) {
+      const int ld = i * 4 + wave, rr = ld * kRowsPerLoad + lane / R::kSlots;
+      const int piece = min((lane % R::kSlots) ^ R::swz(rr), R::kPieces - 1);
+      dma_to_lds(dst + ld * 1024, src, (uint32_t)min(rr, n - 1) * (uint32_t)(2 * stride) + 16 * piece);
+    }
+  };
+  auto fetch_whole = [&](const void *cache, const void *tree, int x, uint32_t dst) {
+    const bool in_tree = x >= cache_whole;
+    const int64_t at = in_tree ? (g.row0 + (x - cache_whole) * 64) * a.kv_stride + hk * D : head + (int64_t)x * 64 * D;
+    fetch(static_cast<const uint16_t *>(in_tree ? tree : cache) + at, in_tree ? a.kv_stride : D, 64, dst);
+  };
+  auto barrier = [&]() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+
+  const int n = min(x1, whole) - x0;  // whole tiles of this part
+  if (n > 0) {
+    auto issue = [&](int i) {  // keys of tile i, values of tile i - 1
+      if (i < n) fetch_whole(a.k_cache, a.k_tree, x0 + i, lds0 + (i & 1) * W::kTile);
+      if (i >= 1 && i <= n) fetch_whole(a.v_cache, a.v_tree, x0 + i - 1, lds0 + (2 + ((i - 1) & 1)) * W::kTile);
+    };
+    // the keys of tile i + 1 and the values of tile i are there, and the places of those before them are free
+    auto next_tile = [&](int i) {
+      wait_vm<0>();
+      barrier();
+      issue(i + 2);
+    };
+    issue(0);
+    wait_vm<0>();
+    barrier();
+    issue(1);
+    const bool active = r0 + 64 * wave < n_rows;
+    if (!active) {  // rows past the end: this wave only carries its share of the tiles
+      for (int i = 0; i < n; ++i) next_tile(i);
+    } else {
+      typedef __attribute__((address_space(3))) bf16x8 lds8;
+      bf16x8 q[2][NS];
+      load_q(q[0], 0);
+      load_q(q[1], 1);
+      f32x16 sa[2][2], sb[2][2];  // scores [32-key block][32-row block] of the present and of the next tile
+      // LDS addresses of this lane's pieces; place, key block and the like are constant offsets from them
+      uint32_t k_at[NS], v_at[NB][2];
+      const int i16 = lane & 15, vrow = 4 * half + (i16 >> 2), low = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<f32x4 *>(part + at * D + 32 * b + acc_row(i, half)) =
-            f32x4{o[b][i], o[b][i + 1], o[b][i + 2], o[b][i + 3]};
+      for (int i = 0; i < NS; ++i) k_at[i] = lds0 + l31 * R::kBytes + (((2 * i + half) ^ R::swz(l31)) << 4);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          v_at[b][e] = lds0 + 2 * W::kTile + (vrow + 8 * e) * R::kBytes + (((4 * b + low) ^ R::swz(vrow + 8 * e)) << 4) + 8 * (i16 & 1);
+      auto key = [&](int place, int step) {
+        return *(lds8 *)(uintptr_t)(k_at[step % NS] + place * W::kTile + step / NS * 32 * R::kBytes);
+      };
+      auto value = [&](int place, int step) {
+        const int off = place * W::kTile + step / NB * 16 * R::kBytes;
+        const bf16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(uintptr_t)(v_at[step % NB][0] + off));
+        const bf16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(uintptr_t)(v_at[step % NB][1] + off));
+        return __builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+      float mx[2];
+      auto raise_max = [&]() {
+        const float top[2] = {half_swap(mx[0], true) * a.c, half_swap(mx[1], true) * a.c};
+        const bool raise[2] = {top[0] > m[0] + 8.f, top[1] > m[1] + 8.f};
+        if (__builtin_expect(__ballot(raise[0] || raise[1]) != 0, 0)) {
+#pragma unroll
+          for (int rb = 0; rb < 2; ++rb) {
+            const float alpha = raise[rb] ? __builtin_amdgcn_exp2f(m[rb] - top[rb]) : 1.f;
+            m[rb] = raise[rb] ? top[rb] : m[rb];
+            l[rb] *= alpha;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[rb][b][i] *= alpha;
+          }
+        }
+      };
+      // the scores `sc` of a tile whose values lie in place `at` into O, and the scores `next` of the tile behind it if there is one
+      auto body = [&](f32x16(&sc)[2][2], f32x16(&next)[2][2], auto at_, auto has_next_) {
+        constexpr int kAt = decltype(at_)::value;
+        constexpr bool kNext = decltype(has_next_)::value;
+        const float mu[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+#pragma unroll
+        for (int e = 0; e < 2 * NS; ++e) asm volatile("" : "+a"(q[e / NS][e % NS]));  // that is where they stay
+        uint32_t p[4][2][4];  // weights as operands: [16 keys][32-row block], two per word
+        // weight e of 64: keys 16 (e / 16) .., row block e / 8 % 2
+        auto weight = [&](int e) {
+          const int j = e / 16, rb = e / 8 % 2, k = e % 8;
+          const float v = __builtin_amdgcn_exp2f(fmaf(sc[j / 2][rb][8 * (j % 2) + k], a.c, -mu[rb]));
+          sc[j / 2][rb][8 * (j % 2) + k] = v;
+          l[rb] += v;
+          if (k % 2 == 1) {
+            typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+            typedef __attribute__((ext_vector_type(2))) float f32x2;
+            const bf16x2 w = __builtin_convertvector(f32x2{sc[j / 2][rb][8 * (j % 2) + k - 1], v}, bf16x2);
+            p[j][rb][k / 2] = __builtin_bit_cast(uint32_t, w);
+          }
+        };
+        if constexpr (kNext) {
+          bf16x8 kf[2] = {key(1 - kAt, 0), key(1 - kAt, 1)};
+#pragma unroll
+          for (int st = 0; st < kSteps1; ++st) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb) score_mfma(next[st / NS][rb], kf[st % 2], q[rb][st % NS], st % NS == 0);
+            if (st + 2 < kSteps1) kf[st % 2] = key(1 - kAt, st + 2);
+#pragma unroll
+            for (int e = 48 * st / kSteps1; e < 48 * (st + 1) / kSteps1; ++e) weight(e);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 48; ++e) weight(e);
+        }
+        float top[2] = {-INFINITY, -INFINITY};
+        bf16x8 vf[2] = {value(kAt, 0), value(kAt, 1)};
+#pragma unroll
+        for (int st = 0; st < kSteps2; ++st) {
+          __builtin_amdgcn_sched_barrier(0);
+          constexpr int kHalf = kSteps2 / 2;
+          const int j = st / NB;
+#pragma unroll
+          for (int rb = 0; rb < 2; ++rb)
+            o[rb][st % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                vf[st % 2], __builtin_bit_cast(bf16x8, uint4{p[j][rb][0], p[j][rb][1], p[j][rb][2], p[j][rb][3]}),
+                o[rb][st % NB], 0, 0, 0);
+          if (st + 2 < kSteps2) vf[st % 2] = value(kAt, st + 2);
+          if (st < kHalf) {
+#pragma unroll
+            for (int e = 48 + 16 * st / kHalf; e < 48 + 16 * (st + 1) / kHalf; ++e) weight(e);
+          } else if (kNext) {
+#pragma unroll
+            for (int e = 64 * (st - kHalf) / kHalf; e < 64 * (st - kHalf + 1) / kHalf; ++e)
+              top[e / 32] = fmaxf(top[e / 32], next[e / 16 % 2][e / 32][e % 16]);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        mx[0] = top[0];
+        mx[1] = top[1];
+      };
+      // scores of the first tile
+#pragma unroll
+      for (int st = 0; st < kSteps1; ++st) {
+        const bf16x8 kf = key(0, st);
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) score_mfma(sa[st / NS][rb], kf, q[rb][st % NS], st % NS == 0);
+      }
+      // what was multiplied last is there after 18 wait states
+      asm volatile("s_nop 15\n\ts_nop 7" : "+v"(sa[0][0]), "+v"(sa[0][1]), "+v"(sa[1][0]), "+v"(sa[1][1]));
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) {
+        mx[rb] = sa[0][rb][0];
+#pragma unroll
+        for (int e = 1; e < 32; ++e) mx[rb] = fmaxf(mx[rb], sa[e / 16][rb][e % 16]);
+      }
+      raise_max();
+      constexpr std::integral_constant<int, 0> even{};
+      constexpr std::integral_constant<int, 1> odd{};
+      int i = 0;
+      for (; i + 2 < n; i += 2) {
+        next_tile(i);
+        body(sa, sb, even, std::true_type{});
+        raise_max();
+        next_tile(i + 1);
+        body(sb, sa, odd, std::true_type{});
+        raise_max();
+      }
+      next_tile(i);
+      if (i + 1 < n) {
+        body(sa, sb, even, std::true_type{});
+        raise_max();
+        next_tile(i + 1);
+        body(sb, sa, odd, std::false_type{});
+      } else {
+        body(sa, sb, even, std::false_type{});
+      }
+    }
+    barrier();  // all places are free
+  }
+
+  for (int x = max(x0, whole); x < x1; ++x) {
+    const bool in_tree = x >= whole + cache_rest;
+    const int base = 64 * (in_tree ? x - cache_rest - cache_whole : cache_whole), keys = in_tree ? g.T : g.len;
+    const int64_t stride = in_tree ? a.kv_stride : D;
+    const int64_t at = in_tree ? (g.row0 + base) * a.kv_stride + hk * D : head + (int64_t)base * D;
+    fetch(static_cast<const uint16_t *>(in_tree ? a.k_tree : a.k_cache) + at, stride, keys - base, lds0);
+    fetch(static_cast<const uint16_t *>(in_tree ? a.v_tree : a.v_cache) + at, stride, keys - base, lds0 + 2 * W::kTile);
+    wait_vm<0>();
+    barrier();
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      bf16x8 q[NS];  // loaded again, so that the registers of the walk above are free here
+      load_q(q, rb);
+#pragma unroll 1
+      for (int kb = 0; kb < 2; ++kb)
+        attend_tile<uint16_t, D, 1>(a, g, in_tree, base + 32 * kb, keys, t[rb], first_t, lds + kb * 32 * R::kBytes,
+                                    lds + 2 * W::kTile + kb * 32 * R::kBytes, q, o[rb], m[rb], l[rb]);
+    }
+    barrier();
+  }
+#pragma unroll
+  for (int rb = 0; rb < 2; ++rb) {
+    l[rb] = half_swap(l[rb], false);
+    if (m[rb] == -INFINITY && l[rb] != 0.f) m[rb] = 0.f;  // scores that are all NaN: so is the row
+    if (r0 + 64 * wave + 32 * rb + l31 < n_rows)
+      finish_row<uint16_t, D>(a, o[rb], m[rb], l[rb], s, split, n_split, t[rb], h[rb], (size_t)(g.row0 + t[rb]) * a.H + h[rb], half,
+                              out, lse, part, part_ml);
   }
 }
 
-// The parts of a row's keys joined: out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.  One wave per row, lane i has the weight of
-// parts i, i + 64, ...
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attention_combine_kernel(KeyArgs a, int n_split, const float *__restrict__ part,
-                                                                const float2 *__restrict__ part_ml, T *__restrict__ out,
-                                                                float *__restrict__ lse) {
-  constexpr int NC = (D + 63) / 64, NP = kMaxSplits / 64;
-  const int lane = threadIdx.x & 63;
-  const SeqGeom g = seq_geom(a, blockIdx.y);
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= (int64_t)g.T * a.H) return;
-  const size_t row = (size_t)g.row0 * a.H + r, stride = (size_t)a.n_seq * a.max_tree * a.H;
-  const size_t first = (size_t)blockIdx.y * a.max_tree * a.H + r;
-  float w[NP], m = -INFINITY, l = 0.f;
-  float2 ml[NP];
+// The parts of a row's keys joined: out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.  D / 4 threads hold four elements each
+// of a row; with PG > 1 that many groups of them share a row's parts and meet in LDS.  Nothing that is loaded depends on another
+// load: what bounds a small combine is one trip to memory, and every part's statistics come with its values.
+constexpr int kJoinGroups = 8;
+template <typename T, int D, int PG>
+__global__ __launch_bounds__(kJoinGroups *D / 4) void attention_combine_kernel(KeyArgs a, int n_split,
+                                                                              const float *__restrict__ part,
+                                                                              const float2 *__restrict__ part_ml,
+                                                                              T *__restrict__ out, float *__restrict__ lse) {
+  constexpr int kCols = D / 4, kRows = kJoinGroups / PG;
+  const int col = threadIdx.x % kCols, grp = threadIdx.x / kCols, pg = grp % PG;
+  const int64_t r = (int64_t)blockIdx.x * kRows + grp / PG, n = (int64_t)a.max_tree * a.H;
+  const size_t stride = (size_t)a.n_seq * n, first = (size_t)blockIdx.y * n + min(r, n - 1);
+  float m = -INFINITY, l = 0.f;
+  f32x4 o{0.f, 0.f, 0.f, 0.f};
+  for (int i0 = pg; i0 < n_split; i0 += 4 * PG) {
+    float2 ml[4];
+    f32x4 v[4];
 #pragma unroll
-  for (int u = 0; u < NP; ++u) {
-    const int i = lane + 64 * u;
-    ml[u] = i < n_split ? part_ml[i * stride + first] : make_float2(-INFINITY, 0.f);
-    m = fmaxf(m, ml[u].x);
-  }
+    for (int j = 0; j < 4; ++j) {
+      const size_t at = (size_t)min(i0 + j * PG, n_split - 1) * stride + first;
+      ml[j] = part_ml[at];
+      v[j] = *reinterpret_cast<const f32x4 *>(part + at * D + 4 * col);
+    }
+    float top = m;
 #pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, kWave));
-  const float mu = m == -INFINITY ? 0.f : m;
+    for (int j = 0; j < 4; ++j) top = fmaxf(top, i0 + j * PG < n_split ? ml[j].x : -INFINITY);
+    const float mu = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f(m - mu);
+    l *= f0;
 #pragma unroll
-  for (int u = 0; u < NP; ++u) {
-    w[u] = __builtin_amdgcn_exp2f(ml[u].x - mu);
-    l = fmaf(w[u], ml[u].y, l);
-  }
+    for (int e = 0; e < 4; ++e) o[e] *= f0;
 #pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) l += __shfl_xor(l, x, kWave);
-  float o[NC];
+    for (int j = 0; j < 4; ++j) {
+      if (i0 + j * PG < n_split && ml[j].x != -INFINITY) {  // a part without keys has left no values
+        const float f = __builtin_amdgcn_exp2f(ml[j].x - mu);
+        l = fmaf(f, ml[j].y, l);
 #pragma unroll
-  for (int c = 0; c < NC; ++c) o[c] = 0.f;
-#pragma unroll
-  for (int u = 0; u < NP; ++u) {
-    const uint64_t live = __ballot(ml[u].x != -INFINITY);
-    const int top = min(64, n_split - 64 * u);
-    for (int i0 = 0; i0 < top; i0 += 8) {  // eight parts in flight
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int i = min(i0 + j, top - 1);
-        const float f = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w[u]), i));
-        const bool used = i0 + j < top && ((live >> i) & 1);  // a part without keys has left nothing there
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const int e = min(lane + 64 * c, D - 1);
-          const float v = part[((64 * u + i) * stride + first) * D + e];
-          o[c] = used ? fmaf(f, v, o[c]) : o[c];
-        }
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(f, v[j][e], o[e]);
       }
     }
+    m = top;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if constexpr (PG > 1) {
+    __shared__ float2 ml[kJoinGroups];
+    __shared__ f32x4 part_o[kJoinGroups][kCols];
+    part_o[grp][col] = o;
+    if (col == 0) ml[grp] = make_float2(m, l);
+    __syncthreads();
+    if (pg > 0) return;
+    float top = m;
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int e = lane + 64 * c;
-    if (D % 64 == 0 || e < D) Elem<T>::store(out + row * D + e, o[c] * inv);
+    for (int g = 1; g < PG; ++g) top = fmaxf(top, ml[grp + g].x);
+    const float mu = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f(m - mu);
+    l *= f0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= f0;
+#pragma unroll
+    for (int g = 1; g < PG; ++g) {
+      const float f = __builtin_amdgcn_exp2f(ml[grp + g].x - mu);
+      l = fmaf(f, ml[grp + g].y, l);
+      const f32x4 v = part_o[grp + g][col];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(f, v[e], o[e]);
+    }
+    m = top;
   }
-  if (lse && lane == 0) lse[row] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
+  const SeqGeom g = seq_geom(a, blockIdx.y);
+  if (r >= (int64_t)g.T * a.H) return;
+  const size_t row = (size_t)g.row0 * a.H + r;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  Elem<T>::store4(out + row * D + 4 * col, f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
+  if (lse && col == 0) lse[row] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
 }
 
 namespace {
 
-constexpr int kAttnTarget = 512;  // workgroups wanted
+constexpr int kPartRows = 1 << 16;  // most rows (x parts) of a launch whose keys are in parts: workgroups wanted x their rows
+constexpr int kJoinRows = 4096;     // up to here a workgroup of the combine has one row
 
-// Row tiles and parts of the keys.  stage_keys: keys of a stage.
-struct AttnPlan {
-  int wr, row_tiles, n_split;
-};
-int64_t stages_of(int64_t max_tree, int64_t max_len) { return (max_len + 63) / 64 + (max_tree + 63) / 64; }
-AttnPlan plan_of(const moespec_attn_desc &ds, int64_t n_seq, int64_t max_tree, int64_t max_len) {
-  const int64_t rows = max_tree * (ds.n_heads / ds.n_kv_heads);
-  AttnPlan p;
-  p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-  p.row_tiles = (int)((rows + 32 * p.wr - 1) / (32 * p.wr));
-  const int64_t groups = n_seq * ds.n_kv_heads * p.row_tiles;
-  const int64_t stages = stages_of(max_tree, max_len);
-  int64_t n = kAttnTarget / groups;
+// Parts of the keys: as many as give `target` workgroups, none without a stage.
+int splits_of(const KeyArgs &a, int64_t row_tiles, int64_t target, int64_t stage_keys) {
+  const int64_t stages = (a.max_len + stage_keys - 1) / stage_keys + (a.max_tree + stage_keys - 1) / stage_keys;
+  int64_t n = target / (a.n_seq * a.Hk * row_tiles);
   n = n < stages ? n : stages;
   n = n < kMaxSplits ? n : kMaxSplits;
-  p.n_split = (int)(n > 1 ? n : 1);
-  return p;
+  return (int)(n > 1 ? n : 1);
 }
 
-template <typename T, int D, int WR, int WK, int KB>
-hipError_t run_attention(const KeyArgs &a, const AttnPlan &p, void *out, float *lse, void *ws, hipStream_t st) {
-  constexpr size_t stages = (size_t)2 * 2 * 32 * KB * WK * Rows<T, D>::kBytes;
-  constexpr size_t join = WK > 1 ? sizeof(float2) * 32 * WR * WK + sizeof(float) * (WK - 1) * WR * 32 * D : 0;
-  constexpr size_t smem = stages > join ? stages : join;
-  static_assert(smem <= 160 * 1024, "LDS of a compute unit");
-  auto kern = tree_attention_kernel<T, D, WR, WK, KB>;
+// A launch of `kern` (rows of a workgroup, workgroups wanted, keys of a stage, threads, LDS) and the combine.
+template <typename T, int D, typename Kern>
+hipError_t run_kernel(Kern kern, int tile_rows, int target, int stage_keys, int threads, size_t smem, const KeyArgs &a, void *out,
+                      float *lse, void *ws, hipStream_t st) {
+  const int row_tiles = (int)(((int64_t)a.max_tree * a.G + tile_rows - 1) / tile_rows);
+  const int n_split = splits_of(a, row_tiles, target, stage_keys);
   if (smem > 64 * 1024) {  // beyond the default limit of a launch
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != hipSuccess) return e;
   }
+  const int64_t rows = (int64_t)a.max_tree * a.H;
   float *part = static_cast<float *>(ws);
-  float2 *ml = reinterpret_cast<float2 *>(part + (size_t)p.n_split * a.n_seq * a.max_tree * a.H * D);
-  const int groups = a.n_seq * a.Hk * p.n_split;
-  kern<<<(groups + 7) / 8 * 8 * p.row_tiles, 64 * WR * WK, smem, st>>>(a, p.row_tiles, p.n_split, static_cast<T *>(out), lse,
-                                                                       part, ml);
+  float2 *ml = reinterpret_cast<float2 *>(part + (size_t)n_split * a.n_seq * rows * D);
+  const int64_t groups = (int64_t)a.n_seq * a.Hk * n_split;
+  kern<<<(unsigned)((groups + 7) / 8 * 8 * row_tiles), threads, smem, st>>>(a, row_tiles, n_split, static_cast<T *>(out), lse, part,
+                                                                            ml);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.n_split == 1) return e;
-  attention_combine_kernel<T, D><<<dim3((unsigned)(((int64_t)a.max_tree * a.H + 3) / 4), a.n_seq), 256, 0, st>>>(
-      a, p.n_split, part, ml, static_cast<T *>(out), lse);
+  if (e != hipSuccess || n_split == 1) return e;
+  if (rows * a.n_seq <= kJoinRows)
+    attention_combine_kernel<T, D, kJoinGroups><<<dim3((unsigned)rows, a.n_seq), kJoinGroups * D / 4, 0, st>>>(
+        a, n_split, part, ml, static_cast<T *>(out), lse);
+  else
+    attention_combine_kernel<T, D, 1><<<dim3((unsigned)((rows + kJoinGroups - 1) / kJoinGroups), a.n_seq), kJoinGroups * D / 4,
+                                        0, st>>>(a, n_split, part, ml, static_cast<T *>(out), lse);
   return hipGetLastError();
 }
 
+template <typename T, int D, int WR, int WK, int KB>
+hipError_t run_attention(const KeyArgs &a, void *out, float *lse, void *ws, hipStream_t st) {
+  constexpr size_t stages = (size_t)2 * 2 * 32 * KB * WK * Rows<T, D>::kBytes;
+  constexpr size_t join = WK > 1 ? sizeof(float2) * 32 * WR * WK + sizeof(float) * (WK - 1) * WR * 32 * D : 0;
+  constexpr size_t smem = stages > join ? stages : join;
+  static_assert(smem <= 160 * 1024, "LDS of a compute unit");
+  static_assert(512 * 32 * WR <= kPartRows, "the workspace has room for the parts");
+  return run_kernel<T, D>(tree_attention_kernel<T, D, WR, WK, KB>, 32 * WR, smem <= 80 * 1024 ? 512 : 256, 32 * KB * WK, 64 * WR * WK,
+                          smem, a, out, lse, ws, st);
+}
+
 template <typename T, int D>
-hipError_t run_shape(const KeyArgs &a, const AttnPlan &p, void *out, float *lse, void *ws, hipStream_t st) {
+hipError_t run_shape(const KeyArgs &a, void *out, float *lse, void *ws, hipStream_t st) {
   typedef AttnShape<T, D> S;
-  if (p.wr == 1) return run_attention<T, D, 1, S::kWk1, 1>(a, p, out, lse, ws, st);
-  if (p.wr == 2) return run_attention<T, D, 2, S::kWk2, 1>(a, p, out, lse, ws, st);
-  return run_attention<T, D, 4, 1, S::kKb4>(a, p, out, lse, ws, st);
+  const int64_t rows = (int64_t)a.max_tree * a.G;
+  if (rows <= 32) return run_attention<T, D, 1, S::kWk1, 1>(a, out, lse, ws, st);
+  if (rows <= 64) return run_attention<T, D, 2, S::kWk2, 1>(a, out, lse, ws, st);
+  if constexpr (sizeof(T) == 2 && D <= 128) {
+    if (rows > 128)
+      return run_kernel<T, D>(tree_attention_wide_kernel<D>, 256, 256, 64, 256, WideShape<D>::kLds, a, out, lse, ws, st);
+  }
+  return run_attention<T, D, 4, 1, S::kKb4>(a, out, lse, ws, st);
 }
 
 template <typename T>
-hipError_t run_type(const moespec_attn_desc &ds, const KeyArgs &a, const AttnPlan &p, void *out, float *lse, void *ws,
-                    hipStream_t st) {
+hipError_t run_type(const moespec_attn_desc &ds, const KeyArgs &a, void *out, float *lse, void *ws, hipStream_t st) {
   switch (ds.head_dim) {
-    case 64: return run_shape<T, 64>(a, p, out, lse, ws, st);
-    case 96: return run_shape<T, 96>(a, p, out, lse, ws, st);
-    case 128: return run_shape<T, 128>(a, p, out, lse, ws, st);
-    case 192: return run_shape<T, 192>(a, p, out, lse, ws, st);
-    default: return run_shape<T, 256>(a, p, out, lse, ws, st);
+    case 64: return run_shape<T, 64>(a, out, lse, ws, st);
+    case 96: return run_shape<T, 96>(a, out, lse, ws, st);
+    case 128: return run_shape<T, 128>(a, out, lse, ws, st);
+    case 192: return run_shape<T, 192>(a, out, lse, ws, st);
+    default: return run_shape<T, 256>(a, out, lse, ws, st);
   }
 }
 
 }  // namespace
 
-// The parts of every row there may be: n_split <= min(kMaxSplits, stages), and where n_split > 1 there are at most
-// kAttnTarget workgroups of up to 128 rows.  Neither bound falls where a call gets smaller.
+// The parts of every row there may be: n_split <= min(kMaxSplits, stages of 32 keys or more), and where n_split > 1 there are at
+// most kPartRows rows of workgroups.  Neither bound grows where a call gets smaller.
 size_t tree_attention_ws(const moespec_attn_desc &ds, int64_t n_seq, int64_t max_tree, int64_t max_len) {
-  const int64_t stages = stages_of(max_tree, max_len), most = (int64_t)kAttnTarget * 128;
+  const int64_t stages = (max_len + 31) / 32 + (max_tree + 31) / 32, most = kPartRows;
   int64_t rows = n_seq * max_tree * ds.n_heads;
   rows = rows > most ? most : rows * (stages < kMaxSplits ? stages : kMaxSplits);
   return (size_t)(rows < most ? rows : most) * (sizeof(float) * ds.head_dim + sizeof(float2));
@@ -450,8 +753,7 @@ size_t tree_attention_ws(const moespec_attn_desc &ds, int64_t n_seq, int64_t max
 
 hipError_t launch_tree_attention(const moespec_attn_desc &ds, const KeyArgs &a, void *out, float *lse, void *ws,
                                  hipStream_t st) {
-  const AttnPlan p = plan_of(ds, a.n_seq, a.max_tree, a.max_len);
-  return ds.dtype == MOESPEC_BF16 ? run_type<uint16_t>(ds, a, p, out, lse, ws, st) : run_type<float>(ds, a, p, out, lse, ws, st);
+  return ds.dtype == MOESPEC_BF16 ? run_type<uint16_t>(ds, a, out, lse, ws, st) : run_type<float>(ds, a, out, lse, ws, st);
 }
 
 }  // namespace moespec

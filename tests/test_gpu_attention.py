@@ -48,6 +48,24 @@ def test_ragged_batches_with_empty_sequences_and_padding(dtype, H, Hk, D, kind):
     assert torch.all(out[b.M - 6:] == 7.0) and torch.all(lse[b.M - 6:] == 7.0), "rows behind the last sequence were written"
 
 
+@pytest.mark.parametrize("D", [64, 96, 128])
+@pytest.mark.parametrize("n", [0, 40, 64, 128, 170, 192, 256, 321, 1500])
+def test_many_rows_over_few_and_many_tiles(D, n):
+    """More than 128 rows per KV head; the last workgroup's waves have rows, some, or none."""
+    b = Batch("bf16", 8, 2, D, [33, 70, 49], [n, max(0, n - 64), n // 2], seed=n + D)
+    b.check(*b.attention())
+
+
+@pytest.mark.parametrize("q_scale", [0.1, 12.0])
+def test_many_rows_with_a_rising_maximum(q_scale):
+    """Scores that grow along the cache: every tile raises the maximum."""
+    b = Batch("bf16", 8, 2, 128, [40], [700], seed=1, q_scale=q_scale)
+    ramp = torch.linspace(0.05, 1.0, b.kc.shape[2], device="cuda")
+    b.kc.copy_((b.q[0, ::4, None, :].float() * 0.3 + b.kc.float() * 0.2) * ramp[None, None, :, None])
+    b.kc[0, :, 700:] = float("nan")
+    b.check(*b.attention())
+
+
 def test_large_tree_and_long_cache():
     b = Batch("bf16", 8, 2, 128, [255], [2051], seed=3)
     b.check(*b.attention())
