@@ -43,7 +43,8 @@ __host__ __device__ constexpr int pow2_ceil(int x) {
 
 // A tile of rows of D elements in LDS: a row is kSlots slots of 16 bytes (a power of two; the row's pieces and padding that is
 // never read).  Piece p of row r sits in slot p ^ swz(r).  Reads of the same piece of 16 consecutive rows (keys as a matrix operand) then
-// touch every bank once, and so do reads of the same 64 bytes of 4 rows in a row (values, transposed on the way out of LDS).
+// touch every bank once, and so do reads of the same 64 bytes of 4 rows in a row (bf16 values, transposed on the way out of
+// LDS).  fp32 values are read as 128 bytes of two rows, 4 apart: swz_values puts those into different halves of the banks.
 template <typename T, int D>
 struct Rows {
   static constexpr int kPieceElems = 16 / (int)sizeof(T);
@@ -53,6 +54,7 @@ struct Rows {
   static __device__ __forceinline__ int swz(int row) {
     return kSlots == 8 ? 4 * ((row >> 1) & 1) + ((row >> 2) & 3) : 4 * (row & 3) + ((row >> 2) & 3);
   }
+  static __device__ __forceinline__ int swz_values(int row) { return sizeof(T) == 2 ? swz(row) : 8 * ((row >> 2) & 1); }
 };
 
 // The matrix operands of 32 rows x D: step i multiplies pieces 2 i (lanes 0-31) and 2 i + 1 (lanes 32-63) of every row, so

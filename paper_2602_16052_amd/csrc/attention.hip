@@ -23,32 +23,142 @@ struct AttnShape {
   static constexpr int kKb4 = kRow <= 256 && sizeof(T) == 2 ? 2 : 1;  // 32-key blocks of a wave with 128 rows a workgroup
 };
 
-// One tile of 32 KB keys, base .. of n, that lies in LDS at kt, vt, taken into a wave's 32 rows (row l31 is token t; no token of
-// the workgroup is in front of first_t): scores, masks, running maximum and sum, values.
+// Where a lane's operands lie in a tile of keys and one of values: few addresses, everything else is a constant offset (swz
+// only touches the last 4 bits of a slot).
+template <typename T, int D>
+struct TileAddr {
+  typedef Rows<T, D> R;
+  static constexpr int NB = D / 32, NS = R::kPieces / 2, NK = NS < 8 ? NS : 8, NV = NB < 4 ? NB : 4;
+  uint32_t k[NK], v[sizeof(T) == 2 ? NV : 2][sizeof(T) == 2 ? 2 : 1];
+  __device__ __forceinline__ TileAddr() {
+    const int lane = threadIdx.x & 63, l31 = lane & 31, half = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) k[i] = l31 * R::kBytes + (((2 * i + half) ^ R::swz(l31)) << 4);
+    if constexpr (sizeof(T) == 2) {
+      // lane i of 16 points at 4 elements of row i / 4 and receives element i of 4 rows
+      const int i16 = lane & 15, vrow = 4 * half + (i16 >> 2), low = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
+#pragma unroll
+      for (int b = 0; b < NV; ++b)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          v[b][e] = (vrow + 8 * e) * R::kBytes + (((4 * b + low) ^ R::swz(vrow + 8 * e)) << 4) + 8 * (i16 & 1);
+    } else {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) v[b][0] = 4 * half * R::kBytes + (((8 * b + (l31 >> 2)) ^ (8 * half)) << 4) + 4 * (l31 & 3);
+    }
+  }
+  // The addresses in another place.  Opaque to the compiler, which would join the place and the constant offsets and add their sum
+  // for every read.
+  __device__ __forceinline__ void move(uint32_t keys, uint32_t values) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      k[i] += keys;
+      asm volatile("" : "+v"(k[i]));
+    }
+#pragma unroll
+    for (auto &x : v)
+#pragma unroll
+      for (uint32_t &y : x) {
+        y += values;
+        asm volatile("" : "+v"(y));
+      }
+  }
+  // keys 32 kb .. + 31, step i of the sum over D
+  __device__ __forceinline__ typename Frag<T>::type key(uint32_t tile, int kb, int i) const {
+    typedef __attribute__((address_space(3))) typename Frag<T>::type lds_frag;
+    return *(lds_frag *)(uintptr_t)(k[i % 8] + tile + 32 * kb * R::kBytes + i / 8 * 256);
+  }
+  // bf16: elements 32 b .. + 31 of keys 32 kb + 16 j .. + 15 in the order of a lane's scores
+  __device__ __forceinline__ bf16x8 values(uint32_t tile, int kb, int j, int b) const {
+    typedef __attribute__((address_space(3))) bf16x4 lds4;
+    const uint32_t at = tile + (32 * kb + 16 * j) * R::kBytes + b / 4 * 256;
+    const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(uintptr_t)(v[b % 4][0] + at));
+    const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(uintptr_t)(v[b % 4][1] + at));
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  // fp32: element 32 b + l31 of key 32 kb + acc_row(i, half)
+  __device__ __forceinline__ float value(uint32_t tile, int kb, int i, int b) const {
+    typedef __attribute__((address_space(3))) float lds1;
+    return *(lds1 *)(uintptr_t)(v[b % 2][0] + tile + (32 * kb + acc_row(i, 0)) * R::kBytes + b / 2 * 256);
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ bool not_finite(T bits) {
+  return sizeof(T) == 2 ? (bits & 0x7f80u) == 0x7f80u : ((uint32_t)bits & 0x7f800000u) == 0x7f800000u;
+}
+
+// A weight of 0 times a NaN or an infinity would reach a token that does not see that key.  So values of a tree are looked at by the
+// workgroup before they are multiplied: what is not finite becomes 0 in LDS, its key's bit is set in odd (one word per 32 keys), and
+// add_odd adds it to the rows that see the key.
+template <typename T, int D, int kKeys, int kThreads>
+__device__ __forceinline__ void clean_values(unsigned char *tile, uint32_t *odd) {
+  typedef Rows<T, D> R;
+  static_assert(kKeys * R::kSlots % kThreads == 0, "whole rounds of the workgroup");
+#pragma unroll 4
+  for (int x = 0; x < kKeys * R::kSlots / kThreads; ++x) {
+    const int id = x * kThreads + (int)threadIdx.x, key = id / R::kSlots;
+    if (((id % R::kSlots) ^ R::swz_values(key)) >= R::kPieces) continue;
+    uint4 *p = reinterpret_cast<uint4 *>(tile + 16 * id);
+    uint4 v = *p;
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (sizeof(T) == 2) {
+        const bool lo = not_finite<uint16_t>(w[e] & 0xffffu), hi = not_finite<uint16_t>(w[e] >> 16);
+        w[e] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+        bad |= lo | hi;
+      } else {
+        const bool is = not_finite<uint32_t>(w[e]);
+        w[e] = is ? 0u : w[e];
+        bad |= is;
+      }
+    }
+    if (bad) {
+      *p = make_uint4(w[0], w[1], w[2], w[3]);
+      atomicOr(&odd[key >> 5], 1u << (key & 31));
+    }
+  }
+}
+// bad: the keys (of 32, the first one's values at vg) that have such values; seen: those that this row sees.
+template <typename T, int D>
+__device__ __forceinline__ void add_odd(uint32_t bad, uint32_t seen, const T *vg, int64_t stride, f32x16 (&o)[D / 32]) {
+  const int half = (threadIdx.x & 63) >> 5;
+  for (; bad != 0; bad &= bad - 1) {
+    const int j = __builtin_ctz(bad);
+    const bool mine = (seen >> j) & 1u;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const f32x4 v = Elem<T>::load4(vg + j * stride + 32 * b + acc_row(i, half));
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (mine && not_finite<uint32_t>(__float_as_uint(v[e]))) o[b][i + e] += v[e];
+      }
+  }
+}
+
+// 32 KB keys, base .. of n, that lie in LDS at kt and vt, taken into a wave's 32 rows (row l31 is token t): scores, masks, running
+// maximum and sum, values.  whole: every row sees all of them.  odd: see clean_values (not read for whole tiles and a cache).
 template <typename T, int D, int KB>
-__device__ __forceinline__ void attend_tile(const KeyArgs &a, const SeqGeom &g, bool tree, int base, int n, int t, int first_t,
-                                            const unsigned char *kt, const unsigned char *vt,
+__device__ __forceinline__ void attend_tile(const KeyArgs &a, const SeqGeom &g, TileAddr<T, D> at, bool tree, bool whole,
+                                            int base, int n, int t, uint32_t kt, uint32_t vt, const uint32_t *odd, const T *vg,
                                             const typename Frag<T>::type (&q)[Rows<T, D>::kPieces / 2], f32x16 (&o)[D / 32],
                                             float &m, float &l) {
-  typedef Rows<T, D> R;
-  typedef typename Frag<T>::type frag;
-  constexpr int NB = D / 32, NS = R::kPieces / 2;
-  const int lane = threadIdx.x & 63, l31 = lane & 31, half = lane >> 5;
+  constexpr int NB = D / 32, NS = Rows<T, D>::kPieces / 2;
+  const int half = (threadIdx.x & 63) >> 5;
+  at.move(kt, vt);
   f32x16 sc[KB];
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      const frag kf =
-          *reinterpret_cast<const frag *>(kt + (32 * kb + l31) * R::kBytes + (((2 * i + half) ^ R::swz(l31)) << 4));
-      sc[kb] = Frag<T>::mma(kf, q[i], sc[kb]);
-    }
+    for (int i = 0; i < NS; ++i) sc[kb] = Frag<T>::mma(at.key(0, kb, i), q[i], sc[kb]);
   }
-  // A stage inside the cache, or in front of every row's own token in a chain, is seen whole.
   uint32_t word[KB];
-  const bool whole = base + 32 * KB <= n && (!tree || (a.tree_mask == nullptr && base + 32 * KB - 1 <= first_t));
   if (!whole) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
@@ -65,10 +175,10 @@ __device__ __forceinline__ void attend_tile(const KeyArgs &a, const SeqGeom &g, 
 #pragma unroll
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[kb][i]);
   mx = half_swap(mx, true) * a.c;
-  // The maximum is only raised when it is passed by more than 2^8: until then the weights stay below 2^8, in fp32 and in
-  // bf16 as exact as below 1, and O is not rescaled.
+  // The maximum is only raised when it is passed by more than 2^8: until then the weights stay below 2^8, in fp32 and in bf16
+  // as exact as below 1, and O is not rescaled.
   const bool raise = mx > m + 8.f;
-  if (__ballot(raise) != 0) {
+  if (__builtin_expect(__ballot(raise) != 0, 0)) {
     const float alpha = raise ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
     m = raise ? mx : m;
     l *= alpha;
@@ -85,97 +195,33 @@ __device__ __forceinline__ void attend_tile(const KeyArgs &a, const SeqGeom &g, 
       sc[kb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][i], a.c, -mu));
       l += sc[kb][i];
     }
-
-  // A weight of 0 times a NaN or an infinity would reach a token that does not see that key.  Keys of the tree with such a
-  // value are found first; their values enter the product as 0 and are added to the rows that see them.
-  uint32_t odd[KB];
-  uint32_t any_odd = 0;
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        bf16x8 p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = (__bf16)sc[kb][8 * j + i];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.values(0, kb, j, b), p, o[b], 0, 0, 0);
+      }
+  } else {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(at.value(0, kb, i, b), sc[kb][i], o[b], 0, 0, 0);
+  }
   if (tree && !whole) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      uint32_t bad = 0;
-#pragma unroll
-      for (int p = 0; p < NS; ++p) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(vt + (32 * kb + l31) * R::kBytes + (((2 * p + half) ^ R::swz(l31)) << 4));
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          bad |= (w[e] & 0x7f800000u) == 0x7f800000u;
-          if (sizeof(T) == 2) bad |= (w[e] & 0x7f80u) == 0x7f80u;
-        }
-      }
-      const unsigned long long b = __ballot(bad != 0);
-      odd[kb] = (uint32_t)b | (uint32_t)(b >> 32);
-      any_odd |= odd[kb];
+      const uint32_t bad = __builtin_amdgcn_readfirstlane(odd[kb]);
+      if (__builtin_expect(bad != 0, 0)) add_odd<T, D>(bad, word[kb], vg + 32 * kb * a.kv_stride, a.kv_stride, o);
     }
-  }
-  auto values = [&](auto clean) {
-    constexpr bool kClean = decltype(clean)::value;  // non-finite values replaced by 0
-    if constexpr (sizeof(T) == 2) {
-      typedef __attribute__((address_space(3))) bf16x4 lds4;
-      const int i16 = lane & 15, vrow = 4 * half + (i16 >> 2), low = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          bf16x8 p;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) p[i] = (__bf16)sc[kb][8 * j + i];
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            const int ra = 32 * kb + 16 * j + vrow, rb = ra + 8;
-            bf16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-                (lds4 *)(vt + ra * R::kBytes + (((4 * b + low) ^ R::swz(ra)) << 4) + 8 * (i16 & 1)));
-            bf16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-                (lds4 *)(vt + rb * R::kBytes + (((4 * b + low) ^ R::swz(rb)) << 4) + 8 * (i16 & 1)));
-            bf16x8 v = __builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7);
-            if constexpr (kClean) {
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if ((__float_as_uint((float)v[e]) & 0x7f800000u) == 0x7f800000u) v[e] = (__bf16)0.f;
-            }
-            o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, o[b], 0, 0, 0);
-          }
-        }
-    } else {
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int vr = 32 * kb + acc_row(i, half);
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            float v = *reinterpret_cast<const float *>(vt + vr * R::kBytes +
-                                                       (((8 * b + (l31 >> 2)) ^ R::swz(vr)) << 4) + 4 * (l31 & 3));
-            if constexpr (kClean)
-              if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) v = 0.f;
-            o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, sc[kb][i], o[b], 0, 0, 0);
-          }
-        }
-    }
-  };
-  if (any_odd == 0) {
-    values(std::false_type{});
-  } else {
-    values(std::true_type{});
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-      for (uint32_t left = odd[kb]; left != 0; left &= left - 1) {
-        const int j = __builtin_ctz(left), vr = 32 * kb + j;
-        const bool seen = (word[kb] >> j) & 1u;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int e = 32 * b + acc_row(i, half);
-            const float v = Elem<T>::load(reinterpret_cast<const T *>(
-                vt + vr * R::kBytes + ((e / R::kPieceElems ^ R::swz(vr)) << 4) + sizeof(T) * (e % R::kPieceElems)));
-            if (seen && (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[b][i] += v;
-          }
-      }
   }
 }
-
 
 template <typename T, int D, int WR, int WK, int KB>
 __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attention_kernel(
@@ -184,9 +230,10 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
   typedef Rows<T, D> R;
   typedef typename Frag<T>::type frag;
   constexpr int NW = WR * WK, kStageKeys = 32 * KB * WK, kTile = kStageKeys * R::kBytes, kStage = 2 * kTile;
-  constexpr int kRowsPerLoad = 64 / R::kSlots, kLoads = kStageKeys / kRowsPerLoad, NB = D / 32, NS = R::kPieces / 2;
-  static_assert(kLoads % NW == 0, "every wave issues as many loads");
+  constexpr int kRowsPerLoad = 64 / R::kSlots, kLoads = kStageKeys / kRowsPerLoad / NW, NB = D / 32, NS = R::kPieces / 2;
+  static_assert(kStageKeys % (kRowsPerLoad * NW) == 0, "every wave issues as many loads");
   extern __shared__ __align__(16) unsigned char lds[];
+  uint32_t *const odd = reinterpret_cast<uint32_t *>(lds + 2 * kStage);  // [2][kStageKeys / 32], for a stage and the next one
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
   const int l31 = lane & 31, half = lane >> 5;
   // row tiles that share keys are neighbours on one XCD (workgroup b runs on XCD b mod 8)
@@ -196,10 +243,11 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
   const SeqGeom g = seq_geom(a, s);
   const int n_rows = g.T * a.G, r0 = tile * 32 * WR;
   if (r0 >= n_rows) return;
+  if (threadIdx.x < 2 * kStageKeys / 32) odd[threadIdx.x] = 0;
 
   // stages: those of the cache, then those of the tree (of a chain only up to the last row's token)
   const int ct = (g.len + kStageKeys - 1) / kStageKeys, all = ct + (g.T + kStageKeys - 1) / kStageKeys;
-  const int last_t = (min(r0 + 32 * WR, n_rows) - 1) / a.G;
+  const int first_t = r0 / a.G, last_t = (min(r0 + 32 * WR, n_rows) - 1) / a.G;
   const int tt = a.tree_mask ? all - ct : last_t / kStageKeys + 1;
   const int chunk = (all + n_split - 1) / n_split;
   const int st0 = split * chunk, st1 = min(st0 + chunk, ct + tt);
@@ -208,12 +256,41 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
   const size_t orow = (size_t)(g.row0 + t) * a.H + h;
   const bool row_ok = r0 + 32 * wr + l31 < n_rows;
 
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds);
+  const int64_t head = ((int64_t)s * a.Hk + hk) * a.capacity * D;
+  // this lane's share of a stage: slots ld 64 + lane of both tiles.  Padding slots repeat a piece and are not read.
+  int rr[kLoads];
+  uint32_t kp[kLoads], vp[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    rr[i] = (i * NW + wave) * kRowsPerLoad + lane / R::kSlots;
+    kp[i] = 16 * min((lane % R::kSlots) ^ R::swz(rr[i]), R::kPieces - 1);
+    vp[i] = 16 * min((lane % R::kSlots) ^ R::swz_values(rr[i]), R::kPieces - 1);
+  }
+  auto issue = [&](int st, int buf) {
+    const bool tree = st >= ct;
+    const int base = (tree ? st - ct : st) * kStageKeys, last = (tree ? g.T : g.len) - 1 - base;
+    const uint32_t stride = (uint32_t)((tree ? a.kv_stride : D) * sizeof(T));
+    const int64_t at = tree ? (g.row0 + base) * a.kv_stride + hk * D : head + (int64_t)base * D;
+    const T *kb = static_cast<const T *>(tree ? a.k_tree : a.k_cache) + at;
+    const T *vb = static_cast<const T *>(tree ? a.v_tree : a.v_cache) + at;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      // keys past the end repeat the last one: their scores are masked, and their weights of 0 must meet numbers
+      const uint32_t off = (uint32_t)min(rr[i], last) * stride;
+      dma_to_lds(lds0 + buf * kStage + (i * NW + wave) * 1024, kb, off + kp[i]);
+      dma_to_lds(lds0 + buf * kStage + kTile + (i * NW + wave) * 1024, vb, off + vp[i]);
+    }
+  };
+
   frag q[NS];
   {
     const T *qp = static_cast<const T *>(a.q) + (g.row0 + t) * a.q_stride + h * D + half * R::kPieceElems;
 #pragma unroll
     for (int i = 0; i < NS; ++i) q[i] = *reinterpret_cast<const frag *>(qp + 2 * i * R::kPieceElems);
   }
+  if (st0 < st1) issue(st0, 0);
+  const TileAddr<T, D> at;
   f32x16 o[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b)
@@ -221,38 +298,27 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
     for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
   float m = -INFINITY, l = 0.f;
 
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds);
-  const size_t head = ((size_t)s * a.Hk + hk) * a.capacity * D;
-  auto issue = [&](int st, int buf) {
-    const bool tree = st >= ct;
-    const int base = (tree ? st - ct : st) * kStageKeys, n = tree ? g.T : g.len;
-    const int64_t stride = tree ? a.kv_stride : D;
-    const int64_t at = tree ? (g.row0 + base) * a.kv_stride + hk * D : (int64_t)head + (int64_t)base * D;
-    const T *kp = static_cast<const T *>(tree ? a.k_tree : a.k_cache) + at;
-    const T *vp = static_cast<const T *>(tree ? a.v_tree : a.v_cache) + at;
-#pragma unroll
-    for (int i = 0; i < kLoads / NW; ++i) {
-      const int ld = i * NW + wave, rr = ld * kRowsPerLoad + lane / R::kSlots;
-      const int piece = min((lane % R::kSlots) ^ R::swz(rr), R::kPieces - 1);  // padding slots repeat a piece, and are not read
-      // keys past the end repeat the last one: their scores are masked, and their weights of 0 must meet numbers
-      const uint32_t off = (uint32_t)min(rr, n - 1 - base) * (uint32_t)(stride * sizeof(T)) + 16 * piece;
-      dma_to_lds(lds0 + buf * kStage + ld * 1024, kp, off);
-      dma_to_lds(lds0 + buf * kStage + kTile + ld * 1024, vp, off);
-    }
-  };
-
-  if (st0 < st1) issue(st0, 0);
   for (int st = st0; st < st1; ++st) {
     const int buf = (st - st0) & 1;
     wait_vm<0>();
     asm volatile("" ::: "memory");
     __syncthreads();  // the stage has arrived, everybody's part of it, and nobody reads the other one any more
     if (st + 1 < st1) issue(st + 1, buf ^ 1);
-    const unsigned char *kt = lds + buf * kStage + wk * KB * 32 * R::kBytes, *vt = kt + kTile;
     const bool tree = st >= ct;
-    const int base = (tree ? st - ct : st) * kStageKeys + wk * KB * 32, n = tree ? g.T : g.len;
-
-    attend_tile<T, D, KB>(a, g, tree, base, n, t, r0 / a.G, kt, vt, q, o, m, l);
+    const int base0 = (tree ? st - ct : st) * kStageKeys, n = tree ? g.T : g.len, base = base0 + wk * KB * 32;
+    // keys inside the cache, or in front of every row's own token in a chain, are seen by all rows
+    auto seen_whole = [&](int from, int keys) {
+      return from + keys <= n && (!tree || (a.tree_mask == nullptr && from + keys - 1 <= first_t));
+    };
+    uint32_t *const my_odd = odd + buf * (kStageKeys / 32);
+    if (tree && !seen_whole(base0, kStageKeys)) {
+      if (threadIdx.x < kStageKeys / 32) odd[(buf ^ 1) * (kStageKeys / 32) + threadIdx.x] = 0;
+      clean_values<T, D, kStageKeys, 64 * NW>(lds + buf * kStage + kTile, my_odd);
+      __syncthreads();
+    }
+    const uint32_t kt = lds0 + buf * kStage + wk * KB * 32 * R::kBytes;
+    const T *vg = static_cast<const T *>(a.v_tree) + (g.row0 + base) * a.kv_stride + hk * D;
+    attend_tile<T, D, KB>(a, g, at, tree, seen_whole(base, 32 * KB), base, n, t, kt, kt + kTile, my_odd + wk * KB, vg, q, o, m, l);
   }
   l = half_swap(l, false);
   if (m == -INFINITY && l != 0.f) m = 0.f;  // scores that are all NaN: so is the row
@@ -314,7 +380,7 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
 // Tiles that some row sees in part (the cache's last one, those of the tree) follow one by one.
 template <int D>
 struct WideShape {
-  static constexpr int kKeys = 64, kTile = kKeys * Rows<uint16_t, D>::kBytes, kLds = 4 * kTile;
+  static constexpr int kKeys = 64, kTile = kKeys * Rows<uint16_t, D>::kBytes, kLds = 4 * kTile + 16;
 };
 
 // s (+)= a b with s and a in the registers that other instructions can read, b in the accumulation registers.  Left to the compiler,
@@ -333,7 +399,6 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
                                                                      float *__restrict__ part, float2 *__restrict__ part_ml) {
   typedef Rows<uint16_t, D> R;
   typedef WideShape<D> W;
-  typedef __attribute__((address_space(3))) bf16x4 lds4;
   constexpr int NB = D / 32, NS = R::kPieces / 2, kLoads = W::kTile / 1024 / 4, kRowsPerLoad = 64 / R::kSlots;
   constexpr int kSteps1 = 2 * NS, kSteps2 = 4 * NB;  // pairs of matrix instructions of S and of O
   extern __shared__ __align__(16) unsigned char lds[];
@@ -366,6 +431,8 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
 #pragma unroll
     for (int i = 0; i < NS; ++i) q[i] = *reinterpret_cast<const bf16x8 *>(qp + 16 * i);
   };
+  const TileAddr<uint16_t, D> at;
+  uint32_t *const odd = reinterpret_cast<uint32_t *>(lds + 4 * W::kTile);
   f32x16 o[2][NB];
 #pragma unroll
   for (int rb = 0; rb < 2; ++rb)
@@ -417,29 +484,13 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
     if (!active) {  // rows past the end: this wave only carries its share of the tiles
       for (int i = 0; i < n; ++i) next_tile(i);
     } else {
-      typedef __attribute__((address_space(3))) bf16x8 lds8;
       bf16x8 q[2][NS];
       load_q(q[0], 0);
       load_q(q[1], 1);
       f32x16 sa[2][2], sb[2][2];  // scores [32-key block][32-row block] of the present and of the next tile
-      // LDS addresses of this lane's pieces; place, key block and the like are constant offsets from them
-      uint32_t k_at[NS], v_at[NB][2];
-      const int i16 = lane & 15, vrow = 4 * half + (i16 >> 2), low = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
-#pragma unroll
-      for (int i = 0; i < NS; ++i) k_at[i] = lds0 + l31 * R::kBytes + (((2 * i + half) ^ R::swz(l31)) << 4);
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          v_at[b][e] = lds0 + 2 * W::kTile + (vrow + 8 * e) * R::kBytes + (((4 * b + low) ^ R::swz(vrow + 8 * e)) << 4) + 8 * (i16 & 1);
-      auto key = [&](int place, int step) {
-        return *(lds8 *)(uintptr_t)(k_at[step % NS] + place * W::kTile + step / NS * 32 * R::kBytes);
-      };
+      auto key = [&](int place, int step) { return at.key(lds0 + place * W::kTile, step / NS, step % NS); };
       auto value = [&](int place, int step) {
-        const int off = place * W::kTile + step / NB * 16 * R::kBytes;
-        const bf16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(uintptr_t)(v_at[step % NB][0] + off));
-        const bf16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(uintptr_t)(v_at[step % NB][1] + off));
-        return __builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7);
+        return at.values(lds0 + (2 + place) * W::kTile, step / NB / 2, step / NB % 2, step % NB);
       };
       float mx[2];
       auto raise_max = [&]() {
@@ -564,21 +615,25 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
     const bool in_tree = x >= whole + cache_rest;
     const int base = 64 * (in_tree ? x - cache_rest - cache_whole : cache_whole), keys = in_tree ? g.T : g.len;
     const int64_t stride = in_tree ? a.kv_stride : D;
-    const int64_t at = in_tree ? (g.row0 + base) * a.kv_stride + hk * D : head + (int64_t)base * D;
-    fetch(static_cast<const uint16_t *>(in_tree ? a.k_tree : a.k_cache) + at, stride, keys - base, lds0);
-    fetch(static_cast<const uint16_t *>(in_tree ? a.v_tree : a.v_cache) + at, stride, keys - base, lds0 + 2 * W::kTile);
+    const int64_t first = in_tree ? (g.row0 + base) * a.kv_stride + hk * D : head + (int64_t)base * D;
+    fetch(static_cast<const uint16_t *>(in_tree ? a.k_tree : a.k_cache) + first, stride, keys - base, lds0);
+    fetch(static_cast<const uint16_t *>(in_tree ? a.v_tree : a.v_cache) + first, stride, keys - base, lds0 + 2 * W::kTile);
     wait_vm<0>();
-    barrier();
+    if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+    __syncthreads();
+    if (in_tree) {
+      clean_values<uint16_t, D, 64, 256>(lds + 2 * W::kTile, odd);
+      __syncthreads();
+    }
+    const uint16_t *vg = static_cast<const uint16_t *>(a.v_tree) + (g.row0 + base) * a.kv_stride + hk * D;
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
       bf16x8 q[NS];  // loaded again, so that the registers of the walk above are free here
       load_q(q, rb);
-#pragma unroll 1
-      for (int kb = 0; kb < 2; ++kb)
-        attend_tile<uint16_t, D, 1>(a, g, in_tree, base + 32 * kb, keys, t[rb], first_t, lds + kb * 32 * R::kBytes,
-                                    lds + 2 * W::kTile + kb * 32 * R::kBytes, q, o[rb], m[rb], l[rb]);
+      attend_tile<uint16_t, D, 2>(a, g, at, in_tree, false, base, keys, t[rb], lds0, lds0 + 2 * W::kTile, odd, vg, q, o[rb], m[rb],
+                                  l[rb]);
     }
-    barrier();
+    __syncthreads();
   }
 #pragma unroll
   for (int rb = 0; rb < 2; ++rb) {
@@ -707,7 +762,7 @@ hipError_t run_kernel(Kern kern, int tile_rows, int target, int stage_keys, int 
 
 template <typename T, int D, int WR, int WK, int KB>
 hipError_t run_attention(const KeyArgs &a, void *out, float *lse, void *ws, hipStream_t st) {
-  constexpr size_t stages = (size_t)2 * 2 * 32 * KB * WK * Rows<T, D>::kBytes;
+  constexpr size_t stages = (size_t)2 * 2 * 32 * KB * WK * Rows<T, D>::kBytes + 2 * 4 * KB * WK;
   constexpr size_t join = WK > 1 ? sizeof(float2) * 32 * WR * WK + sizeof(float) * (WK - 1) * WR * 32 * D : 0;
   constexpr size_t smem = stages > join ? stages : join;
   static_assert(smem <= 160 * 1024, "LDS of a compute unit");
