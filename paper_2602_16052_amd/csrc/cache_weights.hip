@@ -16,6 +16,7 @@ template <typename T, int D>
 struct WeightShape {
   static constexpr int kKb = D * (int)sizeof(T) <= 384 ? 2 : 1;  // 32-key blocks held by a wave
   static constexpr int kKeys = 32 * kKb * kWeightWaves;
+  static constexpr int kRing = 4, kLds = kRing * (32 * Rows<T, D>::kBytes + 512 * kWeightWaves);
 };
 
 // 64 lanes x 16 bytes from their own addresses to LDS bytes [lds, lds + 1024) (see dma_to_lds).
@@ -27,25 +28,33 @@ __device__ __forceinline__ void dma_to_lds_from(uint32_t lds, const void *p) {
                "v"(p)
                : "m0", "memory");
 }
+// The same with 4 bytes per lane.
+__device__ __forceinline__ void dma_word_to_lds_from(uint32_t lds, const void *p) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
+               "v"(p)
+               : "m0", "memory");
+}
 #pragma clang diagnostic pop
 
 template <typename T, int D>
 __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
-    KeyArgs a, int cache_tiles, int tiles, int row_splits, const float *__restrict__ lse, const float *__restrict__ row_weight,
+    KeyArgs a, int tree_tiles, int tiles, int row_splits, const float *__restrict__ lse, const float *__restrict__ row_weight,
     float decay, const float *w_in, float *w_out, float *__restrict__ tree_w, float *__restrict__ part) {
   typedef Rows<T, D> R;
   typedef typename Frag<T>::type frag;
   constexpr int KB = WeightShape<T, D>::kKb, kKeys = WeightShape<T, D>::kKeys, NS = R::kPieces / 2;
   constexpr int kTile = 32 * R::kBytes, kRowsPerLoad = 64 / R::kSlots, kLoads = 32 / kRowsPerLoad;
+  constexpr int kRing = WeightShape<T, D>::kRing, kStage = kTile + 512 * kWeightWaves;  // rows, and 128 words for every wave
   static_assert(kLoads % kWeightWaves == 0, "every wave issues as many loads");
-  __shared__ __align__(16) unsigned char lds[2 * kTile];
+  extern __shared__ __align__(16) unsigned char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l31 = lane & 31, half = lane >> 5;
-  const int rs = blockIdx.x % row_splits, tile = blockIdx.x / row_splits % tiles, sh = blockIdx.x / row_splits / tiles;
-  const int hk = sh % a.Hk, s = sh / a.Hk;
+  // tiles of the trees, which take longer, first; the heads and sequences of a tile side by side
+  const int n_sh = a.n_seq * a.Hk, rs = blockIdx.x % row_splits, sh = blockIdx.x / row_splits % n_sh;
+  const int tile = blockIdx.x / row_splits / n_sh, hk = sh % a.Hk, s = sh / a.Hk;
   const SeqGeom g = seq_geom(a, s);
-  const bool tree = tile >= cache_tiles;
-  const int base = (tree ? tile - cache_tiles : tile) * kKeys, n = tree ? g.T : g.len;
+  const bool tree = tile < tree_tiles;
+  const int base = (tree ? tile : tile - tree_tiles) * kKeys, n = tree ? g.T : g.len;
   if (base >= n) return;
   const int n_rows = g.T * a.G, blocks = (n_rows + 31) / 32, chunk = (blocks + row_splits - 1) / row_splits;
   const int b0 = rs * chunk, b1 = min(b0 + chunk, blocks);
@@ -67,38 +76,75 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
     for (int i = 0; i < 16; ++i) w[kb][i] = 0.f;
 
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds);
-  auto issue = [&](int b, int buf) {
-#pragma unroll
-    for (int i = 0; i < kLoads / kWeightWaves; ++i) {
-      const int ld = i * kWeightWaves + wave, rr = ld * kRowsPerLoad + lane / R::kSlots;
-      const int piece = min((lane % R::kSlots) ^ R::swz(rr), R::kPieces - 1);
-      const int row = min(32 * b + rr, n_rows - 1);
-      dma_to_lds_from(lds0 + buf * kTile + ld * 1024,
-                      static_cast<const T *>(a.q) + (g.row0 + row / a.G) * a.q_stride + (hk * a.G + row % a.G) * D +
-                          piece * R::kPieceElems);
-    }
+  // A walk over every 32nd row from `row`, without divisions and products: where something that belongs to the row lies (per_token
+  // bytes a token, per_head a query head of it), the last row's place, and the row's place among the G rows of its token.
+  const int step_t = 32 / a.G, step_r = 32 % a.G;
+  struct Walk {
+    const char *p, *last;
+    int64_t step, wrap;
+    int row, r;
   };
-  if (b0 < b1) issue(b0, 0);
+  auto walk = [&](const void *first, int64_t per_token, int64_t per_head, int row) {
+    const char *f = static_cast<const char *>(first) + g.row0 * per_token + hk * a.G * per_head;
+    return Walk{f + row / a.G * per_token + row % a.G * per_head, f + (g.T - 1) * per_token + (a.G - 1) * per_head,
+                step_t * per_token + step_r * per_head, per_token - a.G * per_head, row, row % a.G};
+  };
+  auto forward = [&](Walk &w) {  // where it was; rows past the end are the last one
+    const char *p = w.row < n_rows ? w.p : w.last;
+    w.row += 32;
+    w.r += step_r;
+    const bool wrap = w.r >= a.G;
+    w.r -= wrap ? a.G : 0;
+    w.p += wrap ? w.step + w.wrap : w.step;
+    return p;
+  };
+  // this lane's share of a tile of 32 rows, and (lanes 0-31) the row's lse or (others) its weight
+  Walk src[kLoads / kWeightWaves];
+#pragma unroll
+  for (int i = 0; i < kLoads / kWeightWaves; ++i) {
+    const int rr = (i * kWeightWaves + wave) * kRowsPerLoad + lane / R::kSlots;
+    src[i] = walk(a.q, a.q_stride * sizeof(T), D * sizeof(T), 32 * b0 + rr);
+    const int piece = 16 * min((lane % R::kSlots) ^ R::swz(rr), R::kPieces - 1);
+    src[i].p += piece;
+    src[i].last += piece;
+  }
+  Walk stat = half == 1 && row_weight ? walk(row_weight, 4, 0, 32 * b0 + l31) : walk(lse, 4 * (int64_t)a.H, 4, 32 * b0 + l31);
+  // in a tile of a tree the words of its mask with this wave's keys (lanes 0-31 the first, the others the second)
+  const bool masks = tree && a.tree_mask != nullptr;
+  Walk seen = masks ? walk(a.tree_mask + min(base / 32 + wave * KB + (KB > 1 ? half : 0), a.words - 1), 4 * (int64_t)a.words, 0,
+                           32 * b0 + l31)
+                    : stat;
+  auto issue = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < kLoads / kWeightWaves; ++i)
+      dma_to_lds_from(lds0 + buf * kStage + (i * kWeightWaves + wave) * 1024, forward(src[i]));
+    dma_word_to_lds_from(lds0 + buf * kStage + kTile + wave * 512, forward(stat));
+    if (masks) dma_word_to_lds_from(lds0 + buf * kStage + kTile + wave * 512 + 256, forward(seen));
+  };
+  uint32_t q_at[NS < 8 ? NS : 8];
+#pragma unroll
+  for (int i = 0; i < (NS < 8 ? NS : 8); ++i) q_at[i] = lds0 + l31 * R::kBytes + (((2 * i + half) ^ R::swz(l31)) << 4);
+  constexpr int kCount = kLoads / kWeightWaves + 1;  // fetches of a wave for a tile
+  for (int i = 0; i < kRing - 1; ++i)
+    if (b0 + i < b1) issue(i);
+  int buf = 0;
   for (int b = b0; b < b1; ++b) {
-    const int buf = (b - b0) & 1;
-    const int row = min(32 * b + l31, n_rows - 1), t = row / a.G;
-    float ls = lse[(size_t)(g.row0 + t) * a.H + hk * a.G + row % a.G];
-    const float rw = row_weight ? row_weight[g.row0 + t] : 1.f;
-    const bool ok = 32 * b + l31 < n_rows && ls != -INFINITY;
-    ls *= 1.4426950408889634f;
-    uint32_t word[KB];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-      word[kb] = !ok ? 0u : tree ? tree_word(a, g, t, base + (wave * KB + kb) * 32) : ~0u;
-    bool all = true;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) all &= word[kb] == ~0u;
-    const bool masked = __ballot(!all) != 0;
-    wait_vm<0>();
+    // tile b is there, and nobody reads the one before it any more
+    const int later = min(b1 - 1 - b, 2);
+    if (later == 0) wait_vm<0>();
+    else if (!masks && later == 2) wait_vm<2 * kCount>();
+    else if (!masks) wait_vm<kCount>();
+    else if (later == 2) wait_vm<2 * kCount + 2>();
+    else wait_vm<kCount + 1>();
     asm volatile("" ::: "memory");
-    __syncthreads();
-    if (b + 1 < b1) issue(b + 1, buf ^ 1);
-    const unsigned char *qt = lds + buf * kTile;
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (b + kRing - 1 < b1) issue((buf + kRing - 1) % kRing);
+    const float *st = reinterpret_cast<const float *>(lds + buf * kStage + kTile + wave * 512);
+    const int row = 32 * b + l31;
+    const float ls = st[l31];
+    const bool ok = row < n_rows && ls != -INFINITY;
+    const float shift = ok ? ls * 1.4426950408889634f : 0.f, weight = !ok ? 0.f : row_weight ? st[32 + l31] : 1.f;
     f32x16 sc[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
@@ -106,26 +152,35 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
       for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-      const frag q = *reinterpret_cast<const frag *>(qt + l31 * R::kBytes + (((2 * i + half) ^ R::swz(l31)) << 4));
+      typedef __attribute__((address_space(3))) frag lds_frag;
+      const frag q = *(lds_frag *)(uintptr_t)(q_at[i % 8] + buf * kStage + i / 8 * 256);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) sc[kb] = Frag<T>::mma(k[kb][i], q, sc[kb]);
     }
-    if (!masked) {
+    if (tree) {  // a branch: as selections in the common path they would double its instructions
+      asm volatile("");
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const int from = base + (wave * KB + kb) * 32;
+        uint32_t v = masks ? reinterpret_cast<const uint32_t *>(st)[64 + 32 * kb + l31] : keys_below(row / a.G + 1 - from);
+        v = (ok ? v & keys_below(g.T - from) : 0u) >> (4 * half);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (!((v >> acc_row(i, 0)) & 1u)) sc[kb][i] = -INFINITY;
+      }
+    }
+    if (__builtin_expect(__ballot(!ok) != 0, 0)) {  // rows without a part: also none of their NaN
+      asm volatile("");
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) w[kb][i] = fmaf(rw, __builtin_amdgcn_exp2f(fmaf(sc[kb][i], a.c, -ls)), w[kb][i]);
-    } else {
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const uint32_t v = word[kb] >> (4 * half);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float p = fmaf(rw, __builtin_amdgcn_exp2f(fmaf(sc[kb][i], a.c, -ls)), w[kb][i]);
-          w[kb][i] = ((v >> acc_row(i, 0)) & 1u) ? p : w[kb][i];
-        }
-      }
+        for (int i = 0; i < 16; ++i) sc[kb][i] = ok ? sc[kb][i] : -INFINITY;
     }
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[kb][i] = fmaf(weight, __builtin_amdgcn_exp2f(fmaf(sc[kb][i], a.c, -shift)), w[kb][i]);
+    buf = buf + 1 == kRing ? 0 : buf + 1;
   }
   // the 32 lanes of a half summed; lane i < 16 keeps the sum of element i
 #pragma unroll
@@ -151,7 +206,7 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
 }
 
 // The parts of the rows added up, in order.
-__global__ __launch_bounds__(256) void cache_weights_join_kernel(KeyArgs a, int cache_tiles, int tiles, int keys,
+__global__ __launch_bounds__(256) void cache_weights_join_kernel(KeyArgs a, int tree_tiles, int tiles, int keys,
                                                                  int row_splits, float decay, const float *w_in, float *w_out,
                                                                  float *__restrict__ tree_w,
                                                                  const float *__restrict__ part) {
@@ -159,8 +214,8 @@ __global__ __launch_bounds__(256) void cache_weights_join_kernel(KeyArgs a, int 
   const SeqGeom g = seq_geom(a, s);
   const int i = blockIdx.x * 256 + threadIdx.x;
   if (i >= tiles * keys) return;
-  const bool tree = i >= cache_tiles * keys;
-  const int key = tree ? i - cache_tiles * keys : i;
+  const bool tree = i < tree_tiles * keys;
+  const int key = tree ? i : i - tree_tiles * keys;
   if (key >= (tree ? g.T : g.len)) return;
   const size_t stride = (size_t)a.n_seq * a.Hk * tiles * keys;
   const float *p = part + (size_t)sh * tiles * keys + i;
@@ -192,15 +247,21 @@ template <typename T, int D>
 hipError_t run_weights(const moespec_attn_desc &ds, const KeyArgs &a, const float *lse, const float *row_weight, float decay,
                        const float *w_in, float *w_out, float *tree_w, void *ws, hipStream_t st) {
   constexpr int K = WeightShape<T, D>::kKeys;
-  const int cache_tiles = (a.max_len + K - 1) / K, tiles = cache_tiles + (tree_w ? (a.max_tree + K - 1) / K : 0);
+  const int tree_tiles = tree_w ? (a.max_tree + K - 1) / K : 0, tiles = tree_tiles + (a.max_len + K - 1) / K;
   if (tiles == 0) return hipSuccess;
   const int rs = row_splits_of(ds, a.n_seq, tiles, a.max_tree);
   float *part = static_cast<float *>(ws);
-  cache_weights_kernel<T, D><<<(unsigned)((int64_t)a.n_seq * a.Hk * tiles * rs), 64 * kWeightWaves, 0, st>>>(
-      a, cache_tiles, tiles, rs, lse, row_weight, decay, w_in, w_out, tree_w, part);
+  auto kern = cache_weights_kernel<T, D>;
+  constexpr size_t smem = WeightShape<T, D>::kLds;
+  if (smem > 64 * 1024) {  // beyond the default limit of a launch
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != hipSuccess) return e;
+  }
+  kern<<<(unsigned)((int64_t)a.n_seq * a.Hk * tiles * rs), 64 * kWeightWaves, smem, st>>>(
+      a, tree_tiles, tiles, rs, lse, row_weight, decay, w_in, w_out, tree_w, part);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || rs == 1) return e;
-  cache_weights_join_kernel<<<dim3((tiles * K + 255) / 256, a.n_seq * a.Hk), 256, 0, st>>>(a, cache_tiles, tiles, K, rs, decay,
+  cache_weights_join_kernel<<<dim3((tiles * K + 255) / 256, a.n_seq * a.Hk), 256, 0, st>>>(a, tree_tiles, tiles, K, rs, decay,
                                                                                           w_in, w_out, tree_w, part);
   return hipGetLastError();
 }
