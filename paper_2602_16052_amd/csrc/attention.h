@@ -78,6 +78,13 @@ struct Frag<float> {
   }
 };
 
+// An operand that has been loaded, for the compiler too: it does not see the fetches to LDS, and would else wait inside of a loop for
+// the youngest of them where it means the operand.
+template <typename F>
+__device__ __forceinline__ void arrived(F &f) {
+  asm volatile("" : "+v"(f));
+}
+
 // Row (of 32) of element i of a lane's 32 x 32 result; half = lane >> 5.  The column is lane & 31.
 __device__ __forceinline__ int acc_row(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
 

@@ -297,6 +297,8 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
   float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < NS; ++i) arrived(q[i]);
 
   for (int st = st0; st < st1; ++st) {
     const int buf = (st - st0) & 1;
@@ -383,14 +385,23 @@ struct WideShape {
   static constexpr int kKeys = 64, kTile = kKeys * Rows<uint16_t, D>::kBytes, kLds = 4 * kTile + 16;
 };
 
-// s (+)= a b with s and a in the registers that other instructions can read, b in the accumulation registers.  Left to the compiler,
-// scores land in accumulation registers and cost a copy each.  The result is there 16 passes later: no instruction may read s before
-// other matrix instructions have been issued and waited for.
-__device__ __forceinline__ void score_mfma(f32x16 &s, bf16x8 a, bf16x8 b, bool first) {
+// s0 (+)= a b0 and s1 (+)= a b1 with s and a in the registers that other instructions can read, b in the accumulation registers.  Left
+// to the compiler, scores land in accumulation registers and cost a copy each.  The compiler keeps no distances to instructions
+// that it does not see: a matrix instruction may read a register two wait states after another instruction has written it
+// (s_nop 1), and the results are there 16 passes after the last of a chain: whoever reads them does so behind eight other matrix
+// instructions or score_wait.
+__device__ __forceinline__ void score_mfma(f32x16 &s0, f32x16 &s1, bf16x8 a, bf16x8 b0, bf16x8 b1, bool first) {
   if (first)
-    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b));
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %2, %3, 0\n\tv_mfma_f32_32x32x16_bf16 %1, %2, %4, 0"
+                 : "=&v"(s0), "=&v"(s1)
+                 : "v"(a), "a"(b0), "a"(b1));
   else
-    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b));
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %2, %3, %0\n\tv_mfma_f32_32x32x16_bf16 %1, %2, %4, %1"
+                 : "+v"(s0), "+v"(s1)
+                 : "v"(a), "a"(b0), "a"(b1));
+}
+__device__ __forceinline__ void score_wait(f32x16 (&s)[2][2]) {
+  asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[1][0]), "+v"(s[1][1]));
 }
 
 template <int D>
@@ -430,6 +441,8 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
     const uint16_t *qp = static_cast<const uint16_t *>(a.q) + (g.row0 + t[rb]) * a.q_stride + h[rb] * D + 8 * half;
 #pragma unroll
     for (int i = 0; i < NS; ++i) q[i] = *reinterpret_cast<const bf16x8 *>(qp + 16 * i);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) arrived(q[i]);
   };
   const TileAddr<uint16_t, D> at;
   uint32_t *const odd = reinterpret_cast<uint32_t *>(lds + 4 * W::kTile);
@@ -487,6 +500,8 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
       bf16x8 q[2][NS];
       load_q(q[0], 0);
       load_q(q[1], 1);
+#pragma unroll
+      for (int e = 0; e < 2 * NS; ++e) asm volatile("" : "+a"(q[e / NS][e % NS]));  // that is where they stay
       f32x16 sa[2][2], sb[2][2];  // scores [32-key block][32-row block] of the present and of the next tile
       auto key = [&](int place, int step) { return at.key(lds0 + place * W::kTile, step / NS, step % NS); };
       auto value = [&](int place, int step) {
@@ -514,8 +529,6 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
         constexpr int kAt = decltype(at_)::value;
         constexpr bool kNext = decltype(has_next_)::value;
         const float mu[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
-#pragma unroll
-        for (int e = 0; e < 2 * NS; ++e) asm volatile("" : "+a"(q[e / NS][e % NS]));  // that is where they stay
         uint32_t p[4][2][4];  // weights as operands: [16 keys][32-row block], two per word
         // weight e of 64: keys 16 (e / 16) .., row block e / 8 % 2
         auto weight = [&](int e) {
@@ -535,8 +548,7 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
 #pragma unroll
           for (int st = 0; st < kSteps1; ++st) {
             __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int rb = 0; rb < 2; ++rb) score_mfma(next[st / NS][rb], kf[st % 2], q[rb][st % NS], st % NS == 0);
+            score_mfma(next[st / NS][0], next[st / NS][1], kf[st % 2], q[0][st % NS], q[1][st % NS], st % NS == 0);
             if (st + 2 < kSteps1) kf[st % 2] = key(1 - kAt, st + 2);
 #pragma unroll
             for (int e = 48 * st / kSteps1; e < 48 * (st + 1) / kSteps1; ++e) weight(e);
@@ -574,12 +586,9 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
       // scores of the first tile
 #pragma unroll
       for (int st = 0; st < kSteps1; ++st) {
-        const bf16x8 kf = key(0, st);
-#pragma unroll
-        for (int rb = 0; rb < 2; ++rb) score_mfma(sa[st / NS][rb], kf, q[rb][st % NS], st % NS == 0);
+        score_mfma(sa[st / NS][0], sa[st / NS][1], key(0, st), q[0][st % NS], q[1][st % NS], st % NS == 0);
       }
-      // what was multiplied last is there after 18 wait states
-      asm volatile("s_nop 15\n\ts_nop 7" : "+v"(sa[0][0]), "+v"(sa[0][1]), "+v"(sa[1][0]), "+v"(sa[1][1]));
+      score_wait(sa);
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb) {
         mx[rb] = sa[0][rb][0];

@@ -127,6 +127,8 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
   constexpr int kCount = kLoads / kWeightWaves + 1;  // fetches of a wave for a tile
   for (int i = 0; i < kRing - 1; ++i)
     if (b0 + i < b1) issue(i);
+#pragma unroll
+  for (int i = 0; i < KB * NS; ++i) arrived(k[i / NS][i % NS]);
   int buf = 0;
   for (int b = b0; b < b1; ++b) {
     // tile b is there, and nobody reads the one before it any more
@@ -145,17 +147,30 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
     const float ls = st[l31];
     const bool ok = row < n_rows && ls != -INFINITY;
     const float shift = ok ? ls * 1.4426950408889634f : 0.f, weight = !ok ? 0.f : row_weight ? st[32 + l31] : 1.f;
+    // the rows' operands in groups: read together, the next group while this one is multiplied
+    typedef __attribute__((address_space(3))) frag lds_frag;
+    constexpr int kGroup = NS > 16 ? 2 : NS % 4 == 0 ? 4 : 3;
+    static_assert(NS % kGroup == 0, "whole groups");
+    frag q[2][kGroup];
+    auto read = [&](int n) {
+#pragma unroll
+      for (int i = 0; i < kGroup; ++i)
+        q[n & 1][i] = *(lds_frag *)(uintptr_t)(q_at[(n * kGroup + i) % 8] + buf * kStage + (n * kGroup + i) / 8 * 256);
+    };
     f32x16 sc[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
+    read(0);
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      typedef __attribute__((address_space(3))) frag lds_frag;
-      const frag q = *(lds_frag *)(uintptr_t)(q_at[i % 8] + buf * kStage + i / 8 * 256);
+    for (int n = 0; n < NS / kGroup; ++n) {
+      if (n + 1 < NS / kGroup) read(n + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) sc[kb] = Frag<T>::mma(k[kb][i], q, sc[kb]);
+      for (int i = 0; i < kGroup; ++i)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) sc[kb] = Frag<T>::mma(k[kb][n * kGroup + i], q[n & 1][i], sc[kb]);
     }
     if (tree) {  // a branch: as selections in the common path they would double its instructions
       asm volatile("");
@@ -232,24 +247,32 @@ __global__ __launch_bounds__(256) void cache_weights_join_kernel(KeyArgs a, int 
 
 namespace {
 
-constexpr int kWeightTarget = 512;  // workgroups wanted
+constexpr int kWeightSlots = 512;   // workgroups that run at a time
+constexpr int kWeightParts = 4096;  // most workgroups of a launch whose rows are in parts
 
-// n_seq * Hk * key tiles workgroups, times the parts of the rows where those are few.
-int row_splits_of(const moespec_attn_desc &ds, int64_t n_seq, int64_t tiles, int64_t max_tree) {
-  const int64_t groups = n_seq * ds.n_kv_heads * tiles;
-  const int64_t blocks = (max_tree * (ds.n_heads / ds.n_kv_heads) + 31) / 32;
-  int64_t n = kWeightTarget / groups;
-  n = n < blocks ? n : blocks;
-  return (int)(n > 1 ? n : 1);
+// Parts of the rows.  n_seq * Hk * key tiles workgroups run in rounds of kWeightSlots, the last of which may be nearly empty; parts make
+// more and shorter rounds, at the price of the keys' loads in each (about four tiles of rows).
+int row_splits_of(const KeyArgs &a, int64_t tiles) {
+  const int64_t groups = (int64_t)a.n_seq * a.Hk * tiles, blocks = ((int64_t)a.max_tree * a.G + 31) / 32;
+  int best = 1;
+  int64_t least = INT64_MAX;
+  for (int64_t n = 1; n <= blocks && n <= 64 && (n == 1 || n * groups <= kWeightParts); ++n) {
+    const int64_t cost = (groups * n + kWeightSlots - 1) / kWeightSlots * ((blocks + n - 1) / n + 4);
+    if (cost < least) {
+      least = cost;
+      best = (int)n;
+    }
+  }
+  return best;
 }
 
 template <typename T, int D>
-hipError_t run_weights(const moespec_attn_desc &ds, const KeyArgs &a, const float *lse, const float *row_weight, float decay,
+hipError_t run_weights(const KeyArgs &a, const float *lse, const float *row_weight, float decay,
                        const float *w_in, float *w_out, float *tree_w, void *ws, hipStream_t st) {
   constexpr int K = WeightShape<T, D>::kKeys;
   const int tree_tiles = tree_w ? (a.max_tree + K - 1) / K : 0, tiles = tree_tiles + (a.max_len + K - 1) / K;
   if (tiles == 0) return hipSuccess;
-  const int rs = row_splits_of(ds, a.n_seq, tiles, a.max_tree);
+  const int rs = row_splits_of(a, tiles);
   float *part = static_cast<float *>(ws);
   auto kern = cache_weights_kernel<T, D>;
   constexpr size_t smem = WeightShape<T, D>::kLds;
@@ -270,19 +293,21 @@ template <typename T>
 hipError_t run_weights_type(const moespec_attn_desc &ds, const KeyArgs &a, const float *lse, const float *row_weight,
                             float decay, const float *w_in, float *w_out, float *tree_w, void *ws, hipStream_t st) {
   switch (ds.head_dim) {
-    case 64: return run_weights<T, 64>(ds, a, lse, row_weight, decay, w_in, w_out, tree_w, ws, st);
-    case 96: return run_weights<T, 96>(ds, a, lse, row_weight, decay, w_in, w_out, tree_w, ws, st);
-    case 128: return run_weights<T, 128>(ds, a, lse, row_weight, decay, w_in, w_out, tree_w, ws, st);
-    case 192: return run_weights<T, 192>(ds, a, lse, row_weight, decay, w_in, w_out, tree_w, ws, st);
-    default: return run_weights<T, 256>(ds, a, lse, row_weight, decay, w_in, w_out, tree_w, ws, st);
+    case 64: return run_weights<T, 64>(a, lse, row_weight, decay, w_in, w_out, tree_w, ws, st);
+    case 96: return run_weights<T, 96>(a, lse, row_weight, decay, w_in, w_out, tree_w, ws, st);
+    case 128: return run_weights<T, 128>(a, lse, row_weight, decay, w_in, w_out, tree_w, ws, st);
+    case 192: return run_weights<T, 192>(a, lse, row_weight, decay, w_in, w_out, tree_w, ws, st);
+    default: return run_weights<T, 256>(a, lse, row_weight, decay, w_in, w_out, tree_w, ws, st);
   }
 }
 
 }  // namespace
 
-// With more than one part of the rows there are at most kWeightTarget workgroups, each with a sum for every one of up to 256 keys.
-size_t cache_weights_ws(const moespec_attn_desc &, int64_t, int64_t, int64_t) {
-  return sizeof(float) * kWeightTarget * 256;
+// With more than one part of the rows there are at most kWeightParts workgroups, each with a sum for every one of up to 256 keys; and
+// at most 64 parts of what there is.  Neither bound grows where a call gets smaller.
+size_t cache_weights_ws(const moespec_attn_desc &ds, int64_t n_seq, int64_t max_tree, int64_t max_len) {
+  const int64_t tiles = (max_tree + 127) / 128 + (max_len + 127) / 128, groups = n_seq * ds.n_kv_heads * tiles;
+  return sizeof(float) * 256 * (size_t)(groups < kWeightParts / 64 ? 64 * groups : kWeightParts);
 }
 
 hipError_t launch_cache_weights(const moespec_attn_desc &ds, const KeyArgs &a, const float *lse, const float *row_weight,
