@@ -14,7 +14,7 @@ constexpr int kWeightWaves = 4;
 
 template <typename T, int D>
 struct WeightShape {
-  static constexpr int kKb = D * (int)sizeof(T) <= 384 ? 2 : 1;  // 32-key blocks held by a wave
+  static constexpr int kKb = D * (int)sizeof(T) <= 256 ? 2 : 1;  // 32-key blocks held by a wave
   static constexpr int kKeys = 32 * kKb * kWeightWaves;
   static constexpr int kRing = 4, kLds = kRing * (32 * Rows<T, D>::kBytes + 512 * kWeightWaves);
 };
@@ -125,15 +125,14 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
 #pragma unroll
   for (int i = 0; i < (NS < 8 ? NS : 8); ++i) q_at[i] = lds0 + l31 * R::kBytes + (((2 * i + half) ^ R::swz(l31)) << 4);
   constexpr int kCount = kLoads / kWeightWaves + 1;  // fetches of a wave for a tile
-  for (int i = 0; i < kRing - 1; ++i)
+  for (int i = 0; i < kRing; ++i)
     if (b0 + i < b1) issue(i);
 #pragma unroll
   for (int i = 0; i < KB * NS; ++i) arrived(k[i / NS][i % NS]);
-  int buf = 0;
-  for (int b = b0; b < b1; ++b) {
-    // tile b is there, and nobody reads the one before it any more
+  // tile b is there, and the place of the one two before it is free
+  auto tile_there = [&](int b) {
     const int later = min(b1 - 1 - b, 2);
-    if (later == 0) wait_vm<0>();
+    if (later <= 0) wait_vm<0>();
     else if (!masks && later == 2) wait_vm<2 * kCount>();
     else if (!masks) wait_vm<kCount>();
     else if (later == 2) wait_vm<2 * kCount + 2>();
@@ -141,37 +140,58 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (b + kRing - 1 < b1) issue((buf + kRing - 1) % kRing);
+  };
+  // A step multiplies one operand of the rows by this wave's keys; operands are read in groups, the next one while this one is
+  // multiplied.
+  typedef __attribute__((address_space(3))) frag lds_frag;
+  constexpr int kGroup = 2;
+  static_assert(NS % kGroup == 0, "whole groups");
+  frag q[2][kGroup];
+  auto read = [&](int buf, int n) {
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i)
+      q[n & 1][i] = *(lds_frag *)(uintptr_t)(q_at[(n * kGroup + i) % 8] + buf * kStage + (n * kGroup + i) / 8 * 256);
+  };
+  // Scores of tile b + 1 (place buf) into next, beside the exponentials of those of the tile before it (sc, with shift and
+  // weight of this lane's row), where there are such.
+  float shift = 0.f, weight = 0.f;
+  auto step = [&](f32x16(&sc)[KB], f32x16(&next)[KB], int buf, auto with_next_, auto with_sc_) {
+    constexpr bool kNext = decltype(with_next_)::value, kSc = decltype(with_sc_)::value;
+    constexpr int kAll = 16 * KB;
+    auto add = [&](int e) {
+      w[e / 16][e % 16] = fmaf(weight, __builtin_amdgcn_exp2f(fmaf(sc[e / 16][e % 16], a.c, -shift)), w[e / 16][e % 16]);
+      asm volatile("" : "+v"(w[e / 16][e % 16]));  // here, and not behind the matrix instructions where the compiler would move it
+    };
+    if constexpr (kNext) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) next[kb][i] = 0.f;
+      read(buf, 0);
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        if (n % kGroup == 0 && n + kGroup < NS) read(buf, n / kGroup + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) next[kb] = Frag<T>::mma(k[kb][n], q[n / kGroup & 1][n % kGroup], next[kb]);
+        if constexpr (kSc)
+#pragma unroll
+          for (int e = kAll * n / NS; e < kAll * (n + 1) / NS; ++e) add(e);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kAll; ++e) add(e);
+    }
+  };
+  // this lane's row of tile b, and the masks of its scores
+  auto row_of = [&](f32x16(&sc)[KB], int b, int buf) {
     const float *st = reinterpret_cast<const float *>(lds + buf * kStage + kTile + wave * 512);
     const int row = 32 * b + l31;
-    const float ls = st[l31];
+    const float ls = st[l31], rw = st[32 + l31];
     const bool ok = row < n_rows && ls != -INFINITY;
-    const float shift = ok ? ls * 1.4426950408889634f : 0.f, weight = !ok ? 0.f : row_weight ? st[32 + l31] : 1.f;
-    // the rows' operands in groups: read together, the next group while this one is multiplied
-    typedef __attribute__((address_space(3))) frag lds_frag;
-    constexpr int kGroup = NS > 16 ? 2 : NS % 4 == 0 ? 4 : 3;
-    static_assert(NS % kGroup == 0, "whole groups");
-    frag q[2][kGroup];
-    auto read = [&](int n) {
-#pragma unroll
-      for (int i = 0; i < kGroup; ++i)
-        q[n & 1][i] = *(lds_frag *)(uintptr_t)(q_at[(n * kGroup + i) % 8] + buf * kStage + (n * kGroup + i) / 8 * 256);
-    };
-    f32x16 sc[KB];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
-    read(0);
-#pragma unroll
-    for (int n = 0; n < NS / kGroup; ++n) {
-      if (n + 1 < NS / kGroup) read(n + 1);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < kGroup; ++i)
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) sc[kb] = Frag<T>::mma(k[kb][n * kGroup + i], q[n & 1][i], sc[kb]);
-    }
+    shift = ok ? ls * 1.4426950408889634f : 0.f;
+    weight = !ok ? 0.f : row_weight ? rw : 1.f;
     if (tree) {  // a branch: as selections in the common path they would double its instructions
       asm volatile("");
 #pragma unroll
@@ -191,11 +211,33 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[kb][i] = ok ? sc[kb][i] : -INFINITY;
     }
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w[kb][i] = fmaf(weight, __builtin_amdgcn_exp2f(fmaf(sc[kb][i], a.c, -shift)), w[kb][i]);
-    buf = buf + 1 == kRing ? 0 : buf + 1;
+  };
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  if (b0 < b1) {
+    f32x16 sa[KB], sb[KB];
+    tile_there(b0);
+    step(sb, sa, 0, yes, no);
+    row_of(sa, b0, 0);
+    int b = b0, buf = 0;
+    auto forward_one = [&](f32x16(&sc)[KB], f32x16(&next)[KB]) {
+      tile_there(b + 1);
+      if (b + kRing < b1) issue(buf);
+      buf = (buf + 1) % kRing;
+      step(sc, next, buf, yes, yes);
+      row_of(next, b + 1, buf);
+      ++b;
+    };
+    while (b + 2 < b1) {
+      forward_one(sa, sb);
+      forward_one(sb, sa);
+    }
+    if (b + 1 < b1) {
+      forward_one(sa, sb);
+      step(sb, sa, 0, no, yes);
+    } else {
+      step(sa, sb, 0, no, yes);
+    }
   }
   // the 32 lanes of a half summed; lane i < 16 keeps the sum of element i
 #pragma unroll
