@@ -82,18 +82,141 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 }
 
 // Which entries stay, one workgroup per (layer, sequence, head).  The weights are looked at as integers of the same order:
-// three histograms (11, 11 and 10 bits from the top) give the value of the last one kept and how many of its equals are kept,
-// in one pass each over the weights (L2 after the first); then every wave counts and places the kept ones of its share, in order.
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave, kBins = 2048;
+// three histograms (11, 11 and 10 bits from the top) give the value of the last one kept and how many of its equals are kept; then
+// every wave places the kept ones of its share, in order.  R > 0: a thread holds the R weights of its places (wave v has 64 R entries in a
+// row, lane after lane), which are read once, all loads in flight together; R = 0: longer caches, read in every pass.
+// Weights of a cache lie within some ten powers of two, 40 bins of the first histogram: each of kCopies lanes counts into a
+// histogram of its own, or most of the 64 lanes would wait for each other.
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave, kBins = 2048, kCopies = 4, kMaxHeld = 32;
+// Sum of v over this lane and those in front of it.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_0(uint32_t v) {
+  return __builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  v += dpp_or_0<0x111, 0xf>(v);  // one lane on inside of a row of 16, then two, four and eight
+  v += dpp_or_0<0x112, 0xf>(v);
+  v += dpp_or_0<0x114, 0xf>(v);
+  v += dpp_or_0<0x118, 0xf>(v);
+  v += dpp_or_0<0x142, 0xa>(v);  // the first row's last lane to the second row, the third's to the fourth
+  return v + dpp_or_0<0x143, 0xc>(v);  // the second row's to both rows behind it
+}
+// Sum of the first `wave` of a workgroup's sums, in every lane.
+__device__ __forceinline__ uint32_t sum_before(const uint32_t *sums, int wave) {
+  const int l = threadIdx.x & 15;
+  static_assert(kSelectWaves == 16, "a row of 16 lanes has them all");
+  return (uint32_t)row16_sum(l < wave ? (int)sums[l] : 0);
+}
+
+template <int R>
+__device__ __forceinline__ void select_entries(const float *__restrict__ w, int n, int want, uint32_t *hist, uint32_t *wave_sum,
+                                               uint32_t *wave_eq, uint32_t *found, float *__restrict__ w_out,
+                                               int32_t *__restrict__ kept) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int share = R > 0 ? 64 * R : ((n + kSelectWaves - 1) / kSelectWaves + 63) / 64 * 64, i0 = wave * share;
+  const int rounds = R > 0 ? R : share / 64;
+  float held[R > 0 ? R : 1];
+  if constexpr (R > 0) {
+#pragma unroll
+    for (int x = 0; x < R; ++x) held[x] = i0 + 64 * x + lane < n ? w[i0 + 64 * x + lane] : 0.f;
+  }
+  // f(entry, weight) for every place of this lane; entries from n on are none
+  auto each = [&](auto f) {
+    if constexpr (R > 0) {
+#pragma unroll
+      for (int x = 0; x < R; ++x) f(i0 + 64 * x + lane, held[x]);
+    } else {
+#pragma unroll 1
+      for (int x = 0; x < rounds; x += 4) {
+        float v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int i = i0 + 64 * (x + u) + lane;
+          v[u] = x + u < rounds && i < n ? w[i] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (x + u < rounds) f(i0 + 64 * (x + u) + lane, v[u]);
+      }
+    }
+  };
+  uint32_t prefix = 0, left = want;  // the last one kept starts with `prefix`; it is number `left` of those that do
+  for (int b = tid; b < kCopies * kBins; b += kSelectThreads) hist[b] = 0;
+  __syncthreads();
+#pragma unroll 1
+  for (int round = 0; round < 3; ++round) {
+    const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, mask = round == 2 ? 1023 : 2047, known = round == 1 ? 21 : 10;
+    each([&](int i, float v) {
+      const uint32_t k = weight_key(v);
+      if (i < n && (round == 0 || k >> known == prefix)) atomicAdd(&hist[lane % kCopies * kBins + (k >> shift & mask)], 1u);
+    });
+    __syncthreads();
+    // thread i has bins 2 i' and 2 i' + 1 counted from the top, and clears them for the next round; a scan over the workgroup
+    // finds the bin of number `left`
+    const int top = kBins - 1 - 2 * tid;
+    uint32_t h0 = 0, h1 = 0;
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+      uint2 *h = reinterpret_cast<uint2 *>(hist + c * kBins + top - 1);
+      h0 += h->y;
+      h1 += h->x;
+      *h = make_uint2(0, 0);
+    }
+    const uint32_t scan = wave_scan(h0 + h1);
+    if (lane == 63) wave_sum[wave] = scan;
+    __syncthreads();
+    const uint32_t before = sum_before(wave_sum, wave) + scan - h0 - h1;
+    if (before < left && before + h0 >= left) {
+      found[0] = top;
+      found[1] = left - before;
+    } else if (before + h0 < left && before + h0 + h1 >= left) {
+      found[0] = top - 1;
+      found[1] = left - before - h0;
+    }
+    __syncthreads();
+    const uint32_t bin = found[0];
+    prefix = round == 2 ? prefix << 10 | bin : round == 1 ? prefix << 11 | bin : bin;
+    left = found[1];
+  }
+
+  uint32_t gt = 0, eq = 0;  // of this wave's share: above the last one kept, its equals
+  each([&](int i, float v) {
+    const uint32_t k = weight_key(v);
+    gt += __popcll(__ballot(i < n && k > prefix));
+    eq += __popcll(__ballot(i < n && k == prefix));
+  });
+  if (lane == 0) {
+    wave_sum[wave] = gt;
+    wave_eq[wave] = eq;
+  }
+  __syncthreads();
+  uint32_t eqs = sum_before(wave_eq, wave), at = sum_before(wave_sum, wave);
+  at += min(eqs, left);  // of the equals in front of this share the first `left` are kept
+  const uint64_t below = (1ull << lane) - 1;
+  each([&](int i, float v) {
+    const uint32_t k = weight_key(v);
+    const uint64_t eq_mask = __ballot(i < n && k == prefix);
+    const bool keep = i < n && (k > prefix || (k == prefix && eqs + __popcll(eq_mask & below) < left));
+    const uint64_t mask = __ballot(keep);
+    if (keep) {
+      const uint32_t dst = at + __popcll(mask & below);
+      kept[dst] = i;
+      w_out[dst] = v;
+    }
+    at += __popcll(mask);
+    eqs += __popcll(eq_mask);
+  });
+}
+
+template <int R>
 __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(const float *__restrict__ w_all,
                                                                       const int32_t *__restrict__ cache_len, int n_seq,
                                                                       int Hk, int capacity, int budget, int recent,
                                                                       int64_t out_capacity, float *__restrict__ w_out_all,
                                                                       int32_t *__restrict__ kept_all, int32_t *new_len) {
-  __shared__ uint32_t hist[kBins];
-  __shared__ uint32_t wave_sum[kSelectWaves], wave_eq[kSelectWaves];
-  __shared__ uint32_t found_bin, found_left;
-  const int hd = blockIdx.x, s = hd / Hk % n_seq, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ __align__(8) uint32_t hist[kCopies * kBins];
+  __shared__ uint32_t wave_sum[kSelectWaves], wave_eq[kSelectWaves], found[2];
+  const int hd = blockIdx.x, s = hd / Hk % n_seq, tid = threadIdx.x;
   const int len = clamp_len(cache_len, s, capacity);
   const float *w = w_all + (int64_t)hd * capacity;
   float *w_out = w_out_all + (int64_t)hd * out_capacity;
@@ -114,86 +237,10 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(const floa
   }
   if (want == 0) return;
 
-  uint32_t prefix = 0, left = want;  // the last one kept starts with `prefix`; it is number `left` of those that do
-#pragma unroll 1
-  for (int round = 0; round < 3; ++round) {
-    const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bins = round == 2 ? 1024 : 2048;
-    for (int b = tid; b < kBins; b += kSelectThreads) hist[b] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += kSelectThreads) {
-      const uint32_t k = weight_key(w[i]);
-      const bool in = round == 0 || (k >> (round == 1 ? 21 : 10)) == prefix;
-      if (in) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
-    }
-    __syncthreads();
-    // thread i has bins 2 i' and 2 i' + 1 counted from the top; a scan over the workgroup finds the bin of number `left`
-    const int top = kBins - 1 - 2 * tid;
-    const uint32_t h0 = hist[top], h1 = hist[top - 1];
-    uint32_t scan = h0 + h1;
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-      const uint32_t up = __shfl_up(scan, x, kWave);
-      if (lane >= x) scan += up;
-    }
-    if (lane == 63) wave_sum[wave] = scan;
-    __syncthreads();
-    uint32_t before = scan - h0 - h1;
-    for (int v = 0; v < wave; ++v) before += wave_sum[v];
-    if (before < left && before + h0 >= left) {
-      found_bin = top;
-      found_left = left - before;
-    } else if (before + h0 < left && before + h0 + h1 >= left) {
-      found_bin = top - 1;
-      found_left = left - before - h0;
-    }
-    __syncthreads();
-    prefix = round == 2 ? prefix << 10 | found_bin : round == 1 ? prefix << 11 | found_bin : found_bin;
-    left = found_left;
-    __syncthreads();
-  }
-
-  // wave v places what it keeps of [v share, (v + 1) share)
-  const int share = ((n + kSelectWaves - 1) / kSelectWaves + 63) / 64 * 64, i0 = wave * share, i1 = min(i0 + share, n);
-  uint32_t gt = 0, eq = 0;
-#pragma unroll 4
-  for (int i = i0 + lane; i < i1; i += 64) {
-    const uint32_t k = weight_key(w[i]);
-    gt += k > prefix;
-    eq += k == prefix;
-  }
-#pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) {
-    gt += __shfl_xor(gt, x, kWave);
-    eq += __shfl_xor(eq, x, kWave);
-  }
-  if (lane == 0) {
-    wave_sum[wave] = gt;
-    wave_eq[wave] = eq;
-  }
-  __syncthreads();
-  uint32_t at = 0, eqs = 0;
-  for (int v = 0; v < wave; ++v) {
-    at += wave_sum[v];
-    eqs += wave_eq[v];
-  }
-  at += min(eqs, left);  // of the equals in front of this share the first `left` are kept
-  const uint64_t below = (1ull << lane) - 1;
-#pragma unroll 2
-  for (int i = i0; i < i1; i += 64) {
-    const int j = i + lane;
-    const float v = j < i1 ? w[j] : 0.f;
-    const uint32_t k = weight_key(v);
-    const uint64_t eq_mask = __ballot(j < i1 && k == prefix);
-    const bool keep = j < i1 && (k > prefix || (k == prefix && eqs + __popcll(eq_mask & below) < left));
-    const uint64_t mask = __ballot(keep);
-    if (keep) {
-      const uint32_t dst = at + __popcll(mask & below);
-      kept[dst] = j;
-      w_out[dst] = v;
-    }
-    at += __popcll(mask);
-    eqs += __popcll(eq_mask);
-  }
+  if (R > 0 && n <= kSelectThreads * R)
+    select_entries<R>(w, n, want, hist, wave_sum, wave_eq, found, w_out, kept);
+  else
+    select_entries<0>(w, n, want, hist, wave_sum, wave_eq, found, w_out, kept);
 }
 
 // The rows of the kept entries copied: kRowsPerGroup of them per workgroup, every thread with four loads of each cache in flight.
@@ -209,21 +256,22 @@ __global__ __launch_bounds__(kGatherThreads) void cache_gather_kernel(const uint
   const int64_t in = (int64_t)hd * capacity * pieces, out = (int64_t)hd * out_capacity * pieces;
   const int64_t total = (int64_t)budget * pieces, i0 = (int64_t)grp * kGatherThreads * 4 + threadIdx.x;
   uint4 k[4], v[4];
-  bool ok[4];
+  int src[4];
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int64_t i = i0 + u * kGatherThreads;
-    const int src = i < total ? list[i / pieces] : -1;
-    ok[u] = src >= 0;
-    if (ok[u]) {
-      const int64_t at = in + (int64_t)src * pieces + i % pieces;
-      k[u] = k_in[at];
-      v[u] = v_in[at];
-    }
+    src[u] = list[min(i, total - 1) / pieces];
+    src[u] = i < total ? src[u] : -1;
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {  // places that stay empty load the first entry
+    const int64_t at = in + (int64_t)max(src[u], 0) * pieces + (i0 + u * kGatherThreads) % pieces;
+    k[u] = k_in[at];
+    v[u] = v_in[at];
   }
 #pragma unroll
   for (int u = 0; u < 4; ++u)
-    if (ok[u]) {
+    if (src[u] >= 0) {
       k_out[out + i0 + u * kGatherThreads] = k[u];
       v_out[out + i0 + u * kGatherThreads] = v[u];
     }
@@ -235,9 +283,14 @@ hipError_t launch_cache_evict(const moespec_attn_desc &ds, int n_layers, int n_s
                               hipStream_t st) {
   const int es = ds.dtype == MOESPEC_BF16 ? 2 : 4, pieces = ds.head_dim * es / 16;
   const int64_t heads = (int64_t)n_layers * n_seq * ds.n_kv_heads;
-  cache_select_kernel<<<(unsigned)heads, kSelectThreads, 0, st>>>(cache_w, cache_len, n_seq, ds.n_kv_heads, ds.capacity, budget,
-                                                                  recent, out_capacity, w_out, kept, new_len);
-  hipError_t e = hipGetLastError();
+  auto select = [&](auto kern) {
+    kern<<<(unsigned)heads, kSelectThreads, 0, st>>>(cache_w, cache_len, n_seq, ds.n_kv_heads, ds.capacity, budget, recent,
+                                                     out_capacity, w_out, kept, new_len);
+    return hipGetLastError();
+  };
+  const int each = (ds.capacity + kSelectThreads - 1) / kSelectThreads;  // weights of a thread, at most
+  hipError_t e = each <= 6 ? select(cache_select_kernel<6>) : each <= 16 ? select(cache_select_kernel<16>)
+                                                                        : select(cache_select_kernel<kMaxHeld>);
   if (e != hipSuccess) return e;
   const int64_t groups = ((int64_t)budget * pieces + 4 * kGatherThreads - 1) / (4 * kGatherThreads);
   cache_gather_kernel<<<(unsigned)(heads * groups), kGatherThreads, 0, st>>>(
