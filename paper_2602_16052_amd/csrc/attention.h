@@ -8,7 +8,8 @@ namespace moespec {
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 
-constexpr int kMaxSplits = 256;  // parts of a sequence's keys that one combine joins
+constexpr int kMaxParts = 256;     // parts of a single sequence's keys
+constexpr int kMaxShared = 256;    // sequences that share the parts of a launch
 
 // The arguments that say which rows and entries there are (host pointers resolved, strides in elements, never 0).
 struct KeyArgs {
@@ -33,6 +34,75 @@ __device__ __forceinline__ SeqGeom seq_geom(const KeyArgs &a, int s) {
   g.T = min(g.T, a.max_tree);
   if (a.max_len > 0) g.len = min(max(a.cache_len[s], 0), a.max_len);
   return g;
+}
+
+// Sum of v over the wave, in every lane.
+__device__ __forceinline__ int wave_sum(int v) {
+  v = row16_sum(v);
+  const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+  v = (int)(a[0] + a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+  return (int)(b[0] + b[1]);
+}
+
+// The keys of a launch in parts.  slots == 0: a sequence's keys are one part, `index` is the sequence.  Otherwise the sequences share
+// `slots` parts: with the smallest chunk of units (tiles of keys, by units(geometry); 0 where there is nothing to do) of which
+// every sequence takes as many as it needs and all together fit, `index` is the part.  One sequence has all parts.
+// first_of (may be NULL): [n_seq + 1], receives the first part of every sequence (of more than one).
+struct Share {
+  int s, part, parts;  // sequence (-1: none), which of how many parts
+  // units part * chunk .. of a workgroup that has `all` of them
+  __device__ __forceinline__ int first(int all) const { return (int)min((int64_t)all, (int64_t)part * ((all + parts - 1) / parts)); }
+  __device__ __forceinline__ int last(int all) const { return (int)min((int64_t)all, (part + 1ll) * ((all + parts - 1) / parts)); }
+};
+template <typename Units>
+__device__ __forceinline__ Share share_of(const KeyArgs &a, int slots, int index, Units units, int32_t *first_of) {
+  if (slots == 0) return Share{index, 0, 1};
+  if (a.n_seq == 1) return Share{0, index, slots};
+  constexpr int NU = kMaxShared / kWave;
+  const int lane = threadIdx.x & 63;
+  int n[NU], total = 0;
+#pragma unroll
+  for (int u = 0; u < NU; ++u) {
+    const int s = lane + kWave * u;
+    n[u] = s < a.n_seq ? units(seq_geom(a, s)) : 0;
+    total += n[u];
+  }
+  total = wave_sum(total);
+  int lo = max((total + slots - 1) / slots, 1), hi = max((total + slots - a.n_seq - 1) / (slots - a.n_seq), lo);
+  auto parts = [&](int units_of, int chunk) { return (units_of + chunk - 1) / chunk; };
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    int all = 0;
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+      if (kWave * u < a.n_seq) all += parts(n[u], mid);
+    if (__builtin_amdgcn_readfirstlane(wave_sum(all)) <= slots) hi = mid;
+    else lo = mid + 1;
+  }
+  Share r{-1, 0, 1};
+  int before = 0;
+#pragma unroll
+  for (int u = 0; u < NU; ++u) {
+    if (kWave * u >= a.n_seq) break;
+    const int mine = parts(n[u], lo);
+    int scan = mine;  // parts of this sequence and of those in front of it
+#pragma unroll
+    for (int x = 1; x < kWave; x <<= 1) {
+      const int up = __shfl_up(scan, x, kWave);
+      if (lane >= x) scan += up;
+    }
+    scan += before;
+    if (first_of && lane + kWave * u < a.n_seq) first_of[lane + kWave * u + 1] = scan;
+    const uint64_t hit = __ballot(index >= scan - mine && index < scan);
+    if (hit != 0) {
+      const int l = __builtin_ctzll(hit), part = index - (__shfl(scan, l, kWave) - __shfl(mine, l, kWave));
+      r = Share{kWave * u + l, __builtin_amdgcn_readfirstlane(part), __builtin_amdgcn_readfirstlane(__shfl(mine, l, kWave))};
+    }
+    before = __shfl(scan, 63, kWave);
+  }
+  if (first_of && lane == 0) first_of[0] = 0;
+  return r;
 }
 
 __host__ __device__ constexpr int pow2_ceil(int x) {
@@ -104,12 +174,12 @@ __device__ __forceinline__ uint32_t tree_word(const KeyArgs &a, const SeqGeom &g
 }
 
 // What a lane holds of a finished row (elements acc_row(i, half) of every 32; m in units of log 2) written out, or left for the
-// combine where the row's keys are in n_split parts.
+// combine where the keys are in parts, of which this is number `index`.
 template <typename T, int D>
-__device__ __forceinline__ void finish_row(const KeyArgs &a, const f32x16 (&o)[D / 32], float m, float l, int s, int split,
-                                           int n_split, int t, int h, size_t orow, int half, T *out, float *lse, float *part,
+__device__ __forceinline__ void finish_row(const KeyArgs &a, const f32x16 (&o)[D / 32], float m, float l, int slots,
+                                           int index, int t, int h, size_t orow, int half, T *out, float *lse, float *part,
                                            float2 *part_ml) {
-  if (n_split == 1) {
+  if (slots == 0) {
     const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
@@ -119,7 +189,7 @@ __device__ __forceinline__ void finish_row(const KeyArgs &a, const f32x16 (&o)[D
                         f32x4{o[b][i] * inv, o[b][i + 1] * inv, o[b][i + 2] * inv, o[b][i + 3] * inv});
     if (lse && half == 0) lse[orow] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
   } else {
-    const size_t at = ((size_t)split * a.n_seq + s) * a.max_tree * a.H + (size_t)t * a.H + h;
+    const size_t at = (size_t)index * a.max_tree * a.H + (size_t)t * a.H + h;
     if (half == 0) part_ml[at] = make_float2(m, l);
     if (m == -INFINITY) return;  // the combine passes it over
 #pragma unroll

@@ -225,8 +225,8 @@ __device__ __forceinline__ void attend_tile(const KeyArgs &a, const SeqGeom &g, 
 
 template <typename T, int D, int WR, int WK, int KB>
 __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attention_kernel(
-    KeyArgs a, int row_tiles, int n_split, T *__restrict__ out, float *__restrict__ lse, float *__restrict__ part,
-    float2 *__restrict__ part_ml) {
+    KeyArgs a, int row_tiles, int slots, T *__restrict__ out, float *__restrict__ lse, float *__restrict__ part,
+    float2 *__restrict__ part_ml, int32_t *__restrict__ first_of) {
   typedef Rows<T, D> R;
   typedef typename Frag<T>::type frag;
   constexpr int NW = WR * WK, kStageKeys = 32 * KB * WK, kTile = kStageKeys * R::kBytes, kStage = 2 * kTile;
@@ -238,8 +238,14 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
   const int l31 = lane & 31, half = lane >> 5;
   // row tiles that share keys are neighbours on one XCD (workgroup b runs on XCD b mod 8)
   const int slot = blockIdx.x / 8, group = slot / row_tiles * 8 + (int)(blockIdx.x % 8), tile = slot % row_tiles;
-  if (group >= a.n_seq * a.Hk * n_split) return;
-  const int split = group % n_split, hk = group / n_split % a.Hk, s = group / n_split / a.Hk;
+  const int n_parts = slots == 0 ? a.n_seq : slots, index = group % n_parts, hk = group / n_parts;
+  if (hk >= a.Hk) return;
+  auto stages = [&](const SeqGeom &g) {
+    return g.T == 0 ? 0 : (g.len + kStageKeys - 1) / kStageKeys + (g.T + kStageKeys - 1) / kStageKeys;
+  };
+  const Share part_of = share_of(a, slots, index, stages, blockIdx.x == 0 ? first_of : nullptr);
+  const int s = part_of.s;
+  if (s < 0) return;
   const SeqGeom g = seq_geom(a, s);
   const int n_rows = g.T * a.G, r0 = tile * 32 * WR;
   if (r0 >= n_rows) return;
@@ -249,8 +255,7 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
   const int ct = (g.len + kStageKeys - 1) / kStageKeys, all = ct + (g.T + kStageKeys - 1) / kStageKeys;
   const int first_t = r0 / a.G, last_t = (min(r0 + 32 * WR, n_rows) - 1) / a.G;
   const int tt = a.tree_mask ? all - ct : last_t / kStageKeys + 1;
-  const int chunk = (all + n_split - 1) / n_split;
-  const int st0 = split * chunk, st1 = min(st0 + chunk, ct + tt);
+  const int st0 = part_of.first(ct + tt), st1 = part_of.last(ct + tt);
 
   const int row = min(r0 + 32 * wr + l31, n_rows - 1), t = row / a.G, h = hk * a.G + row % a.G;
   const size_t orow = (size_t)(g.row0 + t) * a.H + h;
@@ -369,7 +374,7 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
     m = mt;
     l = lt;
   }
-  if (row_ok) finish_row<T, D>(a, o, m, l, s, split, n_split, t, h, orow, half, out, lse, part, part_ml);
+  if (row_ok) finish_row<T, D>(a, o, m, l, slots, index, t, h, orow, half, out, lse, part, part_ml);
 }
 
 // ---- Many rows per KV head (bf16, D <= 128): bound by arithmetic.
@@ -405,9 +410,10 @@ __device__ __forceinline__ void score_wait(f32x16 (&s)[2][2]) {
 }
 
 template <int D>
-__global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, int row_tiles, int n_split,
+__global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, int row_tiles, int slots,
                                                                      uint16_t *__restrict__ out, float *__restrict__ lse,
-                                                                     float *__restrict__ part, float2 *__restrict__ part_ml) {
+                                                                     float *__restrict__ part, float2 *__restrict__ part_ml,
+                                                                     int32_t *__restrict__ first_of) {
   typedef Rows<uint16_t, D> R;
   typedef WideShape<D> W;
   constexpr int NB = D / 32, NS = R::kPieces / 2, kLoads = W::kTile / 1024 / 4, kRowsPerLoad = 64 / R::kSlots;
@@ -416,8 +422,16 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l31 = lane & 31, half = lane >> 5;
   const int slot = blockIdx.x / 8, group = slot / row_tiles * 8 + (int)(blockIdx.x % 8), tile = slot % row_tiles;
-  if (group >= a.n_seq * a.Hk * n_split) return;
-  const int split = group % n_split, hk = group / n_split % a.Hk, s = group / n_split / a.Hk;
+  const int n_parts = slots == 0 ? a.n_seq : slots, index = group % n_parts, hk = group / n_parts;
+  if (hk >= a.Hk) return;
+  // a tile that some row sees in part takes as long as kRest others
+  constexpr int kRest = 3;
+  auto units = [&](const SeqGeom &g) {
+    return g.T == 0 ? 0 : g.len / 64 + kRest * ((g.len + 63) / 64 - g.len / 64 + (g.T + 63) / 64);
+  };
+  const Share part_of = share_of(a, slots, index, units, blockIdx.x == 0 ? first_of : nullptr);
+  const int s = part_of.s;
+  if (s < 0) return;
   const SeqGeom g = seq_geom(a, s);
   const int n_rows = g.T * a.G, r0 = tile * 256;
   if (r0 >= n_rows) return;
@@ -427,8 +441,9 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
   const int cache_whole = g.len / 64, whole = cache_whole + (a.tree_mask ? 0 : (first_t + 1) / 64);
   const int cache_rest = (g.len + 63) / 64 - cache_whole;
   const int all = whole + cache_rest + (a.tree_mask ? (g.T + 63) / 64 : last_t / 64 + 1 - (first_t + 1) / 64);
-  const int chunk = (all + n_split - 1) / n_split;
-  const int x0 = split * chunk, x1 = min(x0 + chunk, all);
+  const int my_units = whole + kRest * (all - whole);
+  auto tile_at = [&](int unit) { return unit <= whole ? unit : whole + (unit - whole + kRest - 1) / kRest; };
+  const int x0 = tile_at(part_of.first(my_units)), x1 = tile_at(part_of.last(my_units));
 
   int t[2], h[2];
 #pragma unroll
@@ -620,18 +635,28 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
     barrier();  // all places are free
   }
 
-  for (int x = max(x0, whole); x < x1; ++x) {
+  auto rest_base = [&](int x) { return 64 * (x >= whole + cache_rest ? x - cache_rest - cache_whole : cache_whole); };
+  auto fetch_rest = [&](int x) {
     const bool in_tree = x >= whole + cache_rest;
-    const int base = 64 * (in_tree ? x - cache_rest - cache_whole : cache_whole), keys = in_tree ? g.T : g.len;
+    const int base = rest_base(x), keys = in_tree ? g.T : g.len;
     const int64_t stride = in_tree ? a.kv_stride : D;
     const int64_t first = in_tree ? (g.row0 + base) * a.kv_stride + hk * D : head + (int64_t)base * D;
-    fetch(static_cast<const uint16_t *>(in_tree ? a.k_tree : a.k_cache) + first, stride, keys - base, lds0);
-    fetch(static_cast<const uint16_t *>(in_tree ? a.v_tree : a.v_cache) + first, stride, keys - base, lds0 + 2 * W::kTile);
+    const uint32_t to = lds0 + (x & 1) * W::kTile;
+    fetch(static_cast<const uint16_t *>(in_tree ? a.k_tree : a.k_cache) + first, stride, keys - base, to);
+    fetch(static_cast<const uint16_t *>(in_tree ? a.v_tree : a.v_cache) + first, stride, keys - base, to + 2 * W::kTile);
+  };
+  const int y0 = max(x0, whole);
+  if (y0 < x1) fetch_rest(y0);
+  for (int x = y0; x < x1; ++x) {
+    const bool in_tree = x >= whole + cache_rest;
+    const int base = rest_base(x), keys = in_tree ? g.T : g.len, at_tile = (x & 1) * W::kTile;
+    uint32_t *const my_odd = odd + 2 * (x & 1);
     wait_vm<0>();
-    if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-    __syncthreads();
+    if (threadIdx.x < 2) my_odd[threadIdx.x] = 0;
+    __syncthreads();  // the tile is there, and nobody reads the one before it any more
+    if (x + 1 < x1) fetch_rest(x + 1);
     if (in_tree) {
-      clean_values<uint16_t, D, 64, 256>(lds + 2 * W::kTile, odd);
+      clean_values<uint16_t, D, 64, 256>(lds + 2 * W::kTile + at_tile, my_odd);
       __syncthreads();
     }
     const uint16_t *vg = static_cast<const uint16_t *>(a.v_tree) + (g.row0 + base) * a.kv_stride + hk * D;
@@ -639,18 +664,17 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
     for (int rb = 0; rb < 2; ++rb) {
       bf16x8 q[NS];  // loaded again, so that the registers of the walk above are free here
       load_q(q, rb);
-      attend_tile<uint16_t, D, 2>(a, g, at, in_tree, false, base, keys, t[rb], lds0, lds0 + 2 * W::kTile, odd, vg, q, o[rb], m[rb],
-                                  l[rb]);
+      attend_tile<uint16_t, D, 2>(a, g, at, in_tree, false, base, keys, t[rb], lds0 + at_tile, lds0 + 2 * W::kTile + at_tile, my_odd,
+                                  vg, q, o[rb], m[rb], l[rb]);
     }
-    __syncthreads();
   }
 #pragma unroll
   for (int rb = 0; rb < 2; ++rb) {
     l[rb] = half_swap(l[rb], false);
     if (m[rb] == -INFINITY && l[rb] != 0.f) m[rb] = 0.f;  // scores that are all NaN: so is the row
     if (r0 + 64 * wave + 32 * rb + l31 < n_rows)
-      finish_row<uint16_t, D>(a, o[rb], m[rb], l[rb], s, split, n_split, t[rb], h[rb], (size_t)(g.row0 + t[rb]) * a.H + h[rb], half,
-                              out, lse, part, part_ml);
+      finish_row<uint16_t, D>(a, o[rb], m[rb], l[rb], slots, index, t[rb], h[rb], (size_t)(g.row0 + t[rb]) * a.H + h[rb], half, out,
+                              lse, part, part_ml);
   }
 }
 
@@ -659,14 +683,16 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
 // load: what bounds a small combine is one trip to memory, and every part's statistics come with its values.
 constexpr int kJoinGroups = 8;
 template <typename T, int D, int PG>
-__global__ __launch_bounds__(kJoinGroups *D / 4) void attention_combine_kernel(KeyArgs a, int n_split,
+__global__ __launch_bounds__(kJoinGroups *D / 4) void attention_combine_kernel(KeyArgs a, int slots,
                                                                               const float *__restrict__ part,
                                                                               const float2 *__restrict__ part_ml,
+                                                                              const int32_t *__restrict__ first_of,
                                                                               T *__restrict__ out, float *__restrict__ lse) {
   constexpr int kCols = D / 4, kRows = kJoinGroups / PG;
   const int col = threadIdx.x % kCols, grp = threadIdx.x / kCols, pg = grp % PG;
   const int64_t r = (int64_t)blockIdx.x * kRows + grp / PG, n = (int64_t)a.max_tree * a.H;
-  const size_t stride = (size_t)a.n_seq * n, first = (size_t)blockIdx.y * n + min(r, n - 1);
+  const int p0 = a.n_seq == 1 ? 0 : first_of[blockIdx.y], n_split = a.n_seq == 1 ? slots : first_of[blockIdx.y + 1] - p0;
+  const size_t stride = n, first = (size_t)p0 * n + min(r, n - 1);
   float m = -INFINITY, l = 0.f;
   f32x4 o{0.f, 0.f, 0.f, 0.f};
   for (int i0 = pg; i0 < n_split; i0 += 4 * PG) {
@@ -730,16 +756,18 @@ __global__ __launch_bounds__(kJoinGroups *D / 4) void attention_combine_kernel(K
 
 namespace {
 
-constexpr int kPartRows = 1 << 16;  // most rows (x parts) of a launch whose keys are in parts: workgroups wanted x their rows
-constexpr int kJoinRows = 4096;     // up to here a workgroup of the combine has one row
+constexpr int kPartRows = 1 << 16;    // most rows (x parts) of a launch whose keys are in parts: workgroups wanted x their rows
+constexpr size_t kFirstBytes = 2048;  // first parts of up to kMaxShared sequences
+constexpr int kFewStages = 512;        // (see run_shape)
+constexpr int kJoinRows = 4096;       // up to here a workgroup of the combine has one row
 
-// Parts of the keys: as many as give `target` workgroups, none without a stage.
-int splits_of(const KeyArgs &a, int64_t row_tiles, int64_t target, int64_t stage_keys) {
+// Parts of the keys (share_of): as many as give `target` workgroups, none without a stage; 0 where every sequence is one part.
+int slots_of(const KeyArgs &a, int64_t row_tiles, int64_t target, int64_t stage_keys) {
   const int64_t stages = (a.max_len + stage_keys - 1) / stage_keys + (a.max_tree + stage_keys - 1) / stage_keys;
-  int64_t n = target / (a.n_seq * a.Hk * row_tiles);
-  n = n < stages ? n : stages;
-  n = n < kMaxSplits ? n : kMaxSplits;
-  return (int)(n > 1 ? n : 1);
+  int64_t n = target / (a.Hk * row_tiles);
+  if (n > a.n_seq * stages) n = a.n_seq * stages;
+  if (a.n_seq == 1 && n > kMaxParts) n = kMaxParts;
+  return n <= a.n_seq || a.n_seq > kMaxShared ? 0 : (int)n;
 }
 
 // A launch of `kern` (rows of a workgroup, workgroups wanted, keys of a stage, threads, LDS) and the combine.
@@ -747,25 +775,26 @@ template <typename T, int D, typename Kern>
 hipError_t run_kernel(Kern kern, int tile_rows, int target, int stage_keys, int threads, size_t smem, const KeyArgs &a, void *out,
                       float *lse, void *ws, hipStream_t st) {
   const int row_tiles = (int)(((int64_t)a.max_tree * a.G + tile_rows - 1) / tile_rows);
-  const int n_split = splits_of(a, row_tiles, target, stage_keys);
+  const int slots = slots_of(a, row_tiles, target, stage_keys);
   if (smem > 64 * 1024) {  // beyond the default limit of a launch
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != hipSuccess) return e;
   }
   const int64_t rows = (int64_t)a.max_tree * a.H;
-  float *part = static_cast<float *>(ws);
-  float2 *ml = reinterpret_cast<float2 *>(part + (size_t)n_split * a.n_seq * rows * D);
-  const int64_t groups = (int64_t)a.n_seq * a.Hk * n_split;
-  kern<<<(unsigned)((groups + 7) / 8 * 8 * row_tiles), threads, smem, st>>>(a, row_tiles, n_split, static_cast<T *>(out), lse, part,
-                                                                            ml);
+  int32_t *first_of = static_cast<int32_t *>(ws);
+  float *part = reinterpret_cast<float *>(static_cast<char *>(ws) + kFirstBytes);
+  float2 *ml = reinterpret_cast<float2 *>(part + (size_t)slots * rows * D);
+  const int64_t groups = (int64_t)a.Hk * (slots == 0 ? a.n_seq : slots);
+  kern<<<(unsigned)((groups + 7) / 8 * 8 * row_tiles), threads, smem, st>>>(a, row_tiles, slots, static_cast<T *>(out), lse, part, ml,
+                                                                            first_of);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || n_split == 1) return e;
+  if (e != hipSuccess || slots == 0) return e;
   if (rows * a.n_seq <= kJoinRows)
     attention_combine_kernel<T, D, kJoinGroups><<<dim3((unsigned)rows, a.n_seq), kJoinGroups * D / 4, 0, st>>>(
-        a, n_split, part, ml, static_cast<T *>(out), lse);
+        a, slots, part, ml, first_of, static_cast<T *>(out), lse);
   else
     attention_combine_kernel<T, D, 1><<<dim3((unsigned)((rows + kJoinGroups - 1) / kJoinGroups), a.n_seq), kJoinGroups * D / 4,
-                                        0, st>>>(a, n_split, part, ml, static_cast<T *>(out), lse);
+                                        0, st>>>(a, slots, part, ml, first_of, static_cast<T *>(out), lse);
   return hipGetLastError();
 }
 
@@ -784,8 +813,12 @@ template <typename T, int D>
 hipError_t run_shape(const KeyArgs &a, void *out, float *lse, void *ws, hipStream_t st) {
   typedef AttnShape<T, D> S;
   const int64_t rows = (int64_t)a.max_tree * a.G;
-  if (rows <= 32) return run_attention<T, D, 1, S::kWk1, 1>(a, out, lse, ws, st);
-  if (rows <= 64) return run_attention<T, D, 2, S::kWk2, 1>(a, out, lse, ws, st);
+  // few keys: a stage of 32 keys for every workgroup, whose waves then have nothing to join
+  const bool few = (int64_t)a.n_seq * a.Hk * ((a.max_len + 31) / 32 + (a.max_tree + 31) / 32) <= kFewStages;
+  if (rows <= 32)
+    return few ? run_attention<T, D, 1, 1, 1>(a, out, lse, ws, st) : run_attention<T, D, 1, S::kWk1, 1>(a, out, lse, ws, st);
+  if (rows <= 64)
+    return few ? run_attention<T, D, 2, 1, 1>(a, out, lse, ws, st) : run_attention<T, D, 2, S::kWk2, 1>(a, out, lse, ws, st);
   if constexpr (sizeof(T) == 2 && D <= 128) {
     if (rows > 128)
       return run_kernel<T, D>(tree_attention_wide_kernel<D>, 256, 256, 64, 256, WideShape<D>::kLds, a, out, lse, ws, st);
@@ -806,13 +839,13 @@ hipError_t run_type(const moespec_attn_desc &ds, const KeyArgs &a, void *out, fl
 
 }  // namespace
 
-// The parts of every row there may be: n_split <= min(kMaxSplits, stages of 32 keys or more), and where n_split > 1 there are at
-// most kPartRows rows of workgroups.  Neither bound grows where a call gets smaller.
+// The parts of every row there may be: no more than stages of 32 keys or more in all sequences, and where there are parts at all at most
+// kPartRows rows of workgroups.  Neither bound grows where a call gets smaller.
 size_t tree_attention_ws(const moespec_attn_desc &ds, int64_t n_seq, int64_t max_tree, int64_t max_len) {
-  const int64_t stages = (max_len + 31) / 32 + (max_tree + 31) / 32, most = kPartRows;
-  int64_t rows = n_seq * max_tree * ds.n_heads;
-  rows = rows > most ? most : rows * (stages < kMaxSplits ? stages : kMaxSplits);
-  return (size_t)(rows < most ? rows : most) * (sizeof(float) * ds.head_dim + sizeof(float2));
+  const int64_t stages = (max_len + 31) / 32 + (max_tree + 31) / 32, most = kPartRows, seq = n_seq < kMaxShared ? n_seq : kMaxShared;
+  int64_t rows = max_tree * ds.n_heads;
+  rows = rows > most ? most : rows * (stages * seq < most ? stages * seq : most);
+  return kFirstBytes + (size_t)(rows < most ? rows : most) * (sizeof(float) * ds.head_dim + sizeof(float2));
 }
 
 hipError_t launch_tree_attention(const moespec_attn_desc &ds, const KeyArgs &a, void *out, float *lse, void *ws,

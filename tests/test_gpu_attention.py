@@ -66,6 +66,17 @@ def test_many_rows_with_a_rising_maximum(q_scale):
     b.check(*b.attention())
 
 
+@pytest.mark.parametrize("S,T,H,Hk", [(2, 1, 4, 1), (5, 3, 2, 1), (40, 2, 2, 1), (70, 1, 1, 1), (300, 1, 1, 1), (3, 50, 8, 2)])
+def test_sequences_that_share_the_parts(S, T, H, Hk):
+    """Lengths from nothing to long ones and empty trees: every sequence takes parts by its length."""
+    rng = np.random.default_rng(S)
+    lens = [int(v) for v in (rng.random(S) ** 6 * 3000)]
+    trees = [0 if rng.random() < 0.1 else int(rng.integers(1, T + 1)) for _ in range(S)]
+    trees[-1] = T
+    b = Batch("bf16", H, Hk, 64, trees, lens, seed=S, pad=2)
+    b.check(*b.attention())
+
+
 def test_large_tree_and_long_cache():
     b = Batch("bf16", 8, 2, 128, [255], [2051], seed=3)
     b.check(*b.attention())
