@@ -87,7 +87,7 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 // row, lane after lane), which are read once, all loads in flight together; R = 0: longer caches, read in every pass.
 // Weights of a cache lie within some ten powers of two, 40 bins of the first histogram: each of kCopies lanes counts into a
 // histogram of its own, or most of the 64 lanes would wait for each other.
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave, kBins = 2048, kCopies = 4, kMaxHeld = 32;
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave, kBins = 2048, kCopies = 4, kMaxHeld = 32, kBatch = 16;
 // Sum of v over this lane and those in front of it.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ uint32_t dpp_or_0(uint32_t v) {
@@ -118,7 +118,7 @@ __device__ __forceinline__ void select_entries(const float *__restrict__ w, int 
   float held[R > 0 ? R : 1];
   if constexpr (R > 0) {
 #pragma unroll
-    for (int x = 0; x < R; ++x) held[x] = i0 + 64 * x + lane < n ? w[i0 + 64 * x + lane] : 0.f;
+    for (int x = 0; x < R; ++x) held[x] = w[min(i0 + 64 * x + lane, n - 1)];
   }
   // f(entry, weight) for every place of this lane; entries from n on are none
   auto each = [&](auto f) {
@@ -127,15 +127,15 @@ __device__ __forceinline__ void select_entries(const float *__restrict__ w, int 
       for (int x = 0; x < R; ++x) f(i0 + 64 * x + lane, held[x]);
     } else {
 #pragma unroll 1
-      for (int x = 0; x < rounds; x += 4) {
-        float v[4];
+      for (int x = 0; x < rounds; x += kBatch) {  // a batch of loads in flight
+        float v[kBatch];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < kBatch; ++u) {
           const int i = i0 + 64 * (x + u) + lane;
-          v[u] = x + u < rounds && i < n ? w[i] : 0.f;
+          v[u] = w[min(i, n - 1)];
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < kBatch; ++u)
           if (x + u < rounds) f(i0 + 64 * (x + u) + lane, v[u]);
       }
     }

@@ -245,9 +245,9 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
     float mine = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      float v = row16_sum(w[kb][i]);
-      v += __shfl_xor(v, 16, kWave);
-      if (l31 == i) mine = v;
+      const float v = row16_sum(w[kb][i]);
+      const auto pair = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+      if (l31 == i) mine = __uint_as_float(pair[0]) + __uint_as_float(pair[1]);
     }
     const int key = base + (wave * KB + kb) * 32 + acc_row(l31 & 15, half);
     if (l31 >= 16 || key >= n) continue;
