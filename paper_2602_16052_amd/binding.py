@@ -652,7 +652,8 @@ class _Args:
             raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
         heads, dim = t.shape[-2:]
         st = t.stride()
-        row = st[-3] if t.shape[-3] > 1 else heads * dim
+        one = t.shape[-3] == 1  # a single row: the layers are as far apart as rows would be
+        row = st[-3] if not one else st[0] if len(shape) == 4 and t.shape[0] > 1 else heads * dim
         if (dim > 1 and st[-1] != 1) or (heads > 1 and st[-2] != dim) or row < heads * dim or \
                 (len(shape) == 4 and t.shape[0] > 1 and st[0] != t.shape[1] * row):
             raise ValueError(f"{name}: a token's heads must lie in a row, and rows and layers be equally far apart")

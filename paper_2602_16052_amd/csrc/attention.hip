@@ -88,9 +88,10 @@ __device__ __forceinline__ bool not_finite(T bits) {
   return sizeof(T) == 2 ? (bits & 0x7f80u) == 0x7f80u : ((uint32_t)bits & 0x7f800000u) == 0x7f800000u;
 }
 
-// A weight of 0 times a NaN or an infinity would reach a token that does not see that key.  So values of a tree are looked at by the
-// workgroup before they are multiplied: what is not finite becomes 0 in LDS, its key's bit is set in odd (one word per 32 keys), and
-// add_odd adds it to the rows that see the key.
+// A weight of 0 times a NaN or an infinity would reach a token that does not see that key.  So values that not every row sees are
+// looked at by the workgroup before they are multiplied: what is not finite becomes 0 in LDS, its key's bit is set in odd (one word per 32
+// keys), and add_odd adds it to the rows that see the key.  Those are the values of a tree, and the repetitions of a cache's last entry
+// that fill its last tile (only where that entry has such a value: row_not_finite).
 template <typename T, int D, int kKeys, int kThreads>
 __device__ __forceinline__ void clean_values(unsigned char *tile, uint32_t *odd) {
   typedef Rows<T, D> R;
@@ -121,6 +122,17 @@ __device__ __forceinline__ void clean_values(unsigned char *tile, uint32_t *odd)
     }
   }
 }
+// Whether row r of a tile has a value that is not finite, the same in every lane.
+template <typename T, int D>
+__device__ __forceinline__ bool row_not_finite(const unsigned char *tile, int r) {
+  const uint4 v = *reinterpret_cast<const uint4 *>(tile + r * Rows<T, D>::kBytes + 16 * ((threadIdx.x & 63) % Rows<T, D>::kSlots));
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    bad |= sizeof(T) == 2 ? not_finite<uint16_t>(w[e] & 0xffffu) || not_finite<uint16_t>(w[e] >> 16) : not_finite<uint32_t>(w[e]);
+  return __ballot(bad) != 0;
+}
 // bad: the keys (of 32, the first one's values at vg) that have such values; seen: those that this row sees.
 template <typename T, int D>
 __device__ __forceinline__ void add_odd(uint32_t bad, uint32_t seen, const T *vg, int64_t stride, f32x16 (&o)[D / 32]) {
@@ -141,10 +153,11 @@ __device__ __forceinline__ void add_odd(uint32_t bad, uint32_t seen, const T *vg
 }
 
 // 32 KB keys, base .. of n, that lie in LDS at kt and vt, taken into a wave's 32 rows (row l31 is token t): scores, masks, running
-// maximum and sum, values.  whole: every row sees all of them.  odd: see clean_values (not read for whole tiles and a cache).
+// maximum and sum, values.  whole: every row sees all of them.  odd: see clean_values (NULL: nothing was cleaned); the first key's
+// values lie at vg in memory, vstride elements apart.
 template <typename T, int D, int KB>
 __device__ __forceinline__ void attend_tile(const KeyArgs &a, const SeqGeom &g, TileAddr<T, D> at, bool tree, bool whole,
-                                            int base, int n, int t, uint32_t kt, uint32_t vt, const uint32_t *odd, const T *vg,
+                                            int base, int n, int t, uint32_t kt, uint32_t vt, const uint32_t *odd, const T *vg, int64_t vstride,
                                             const typename Frag<T>::type (&q)[Rows<T, D>::kPieces / 2], f32x16 (&o)[D / 32],
                                             float &m, float &l) {
   constexpr int NB = D / 32, NS = Rows<T, D>::kPieces / 2;
@@ -214,11 +227,11 @@ __device__ __forceinline__ void attend_tile(const KeyArgs &a, const SeqGeom &g, 
 #pragma unroll
         for (int b = 0; b < NB; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(at.value(0, kb, i, b), sc[kb][i], o[b], 0, 0, 0);
   }
-  if (tree && !whole) {
+  if (odd != nullptr && !whole) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       const uint32_t bad = __builtin_amdgcn_readfirstlane(odd[kb]);
-      if (__builtin_expect(bad != 0, 0)) add_odd<T, D>(bad, word[kb], vg + 32 * kb * a.kv_stride, a.kv_stride, o);
+      if (__builtin_expect(bad != 0, 0)) add_odd<T, D>(bad, word[kb], vg + 32 * kb * vstride, vstride, o);
     }
   }
 }
@@ -318,14 +331,21 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
       return from + keys <= n && (!tree || (a.tree_mask == nullptr && from + keys - 1 <= first_t));
     };
     uint32_t *const my_odd = odd + buf * (kStageKeys / 32);
-    if (tree && !seen_whole(base0, kStageKeys)) {
+    const bool clean = !seen_whole(base0, kStageKeys) &&
+                       (tree || row_not_finite<T, D>(lds + buf * kStage + kTile, n - 1 - base0));
+    if (clean) {
+      __syncthreads();  // everybody has looked
       if (threadIdx.x < kStageKeys / 32) odd[(buf ^ 1) * (kStageKeys / 32) + threadIdx.x] = 0;
       clean_values<T, D, kStageKeys, 64 * NW>(lds + buf * kStage + kTile, my_odd);
       __syncthreads();
     }
     const uint32_t kt = lds0 + buf * kStage + wk * KB * 32 * R::kBytes;
-    const T *vg = static_cast<const T *>(a.v_tree) + (g.row0 + base) * a.kv_stride + hk * D;
-    attend_tile<T, D, KB>(a, g, at, tree, seen_whole(base, 32 * KB), base, n, t, kt, kt + kTile, my_odd + wk * KB, vg, q, o, m, l);
+    const int64_t vstride = tree ? a.kv_stride : D;
+    const T *vg = static_cast<const T *>(tree ? a.v_tree : a.v_cache) +
+                  (tree ? (g.row0 + base) * a.kv_stride + hk * D : head + (int64_t)base * D);
+    // (with cleaned values every wave of the stage goes by the masks: a key wave that sees all of its keys may have had some cleaned)
+    attend_tile<T, D, KB>(a, g, at, tree, !clean && seen_whole(base, 32 * KB), base, n, t, kt, kt + kTile,
+                          clean ? my_odd + wk * KB : nullptr, vg, vstride, q, o, m, l);
   }
   l = half_swap(l, false);
   if (m == -INFINITY && l != 0.f) m = 0.f;  // scores that are all NaN: so is the row
@@ -579,6 +599,8 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
           __builtin_amdgcn_sched_barrier(0);
           constexpr int kHalf = kSteps2 / 2;
           const int j = st / NB;
+          if (kNext && st == kHalf)  // from here on the next scores may be read
+            asm volatile("" : "+v"(next[0][0]), "+v"(next[0][1]), "+v"(next[1][0]), "+v"(next[1][1]));
 #pragma unroll
           for (int rb = 0; rb < 2; ++rb)
             o[rb][st % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
@@ -655,17 +677,21 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
     if (threadIdx.x < 2) my_odd[threadIdx.x] = 0;
     __syncthreads();  // the tile is there, and nobody reads the one before it any more
     if (x + 1 < x1) fetch_rest(x + 1);
-    if (in_tree) {
+    const bool clean = in_tree || row_not_finite<uint16_t, D>(lds + 2 * W::kTile + at_tile, keys - 1 - base);
+    if (clean) {
+      __syncthreads();  // everybody has looked
       clean_values<uint16_t, D, 64, 256>(lds + 2 * W::kTile + at_tile, my_odd);
       __syncthreads();
     }
-    const uint16_t *vg = static_cast<const uint16_t *>(a.v_tree) + (g.row0 + base) * a.kv_stride + hk * D;
+    const int64_t vstride = in_tree ? a.kv_stride : D;
+    const uint16_t *vg = static_cast<const uint16_t *>(in_tree ? a.v_tree : a.v_cache) +
+                         (in_tree ? (g.row0 + base) * a.kv_stride + hk * D : head + (int64_t)base * D);
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
       bf16x8 q[NS];  // loaded again, so that the registers of the walk above are free here
       load_q(q, rb);
-      attend_tile<uint16_t, D, 2>(a, g, at, in_tree, false, base, keys, t[rb], lds0 + at_tile, lds0 + 2 * W::kTile + at_tile, my_odd,
-                                  vg, q, o[rb], m[rb], l[rb]);
+      attend_tile<uint16_t, D, 2>(a, g, at, in_tree, false, base, keys, t[rb], lds0 + at_tile, lds0 + 2 * W::kTile + at_tile,
+                                  clean ? my_odd : nullptr, vg, vstride, q, o[rb], m[rb], l[rb]);
     }
   }
 #pragma unroll

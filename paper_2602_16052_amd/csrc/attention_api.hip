@@ -9,7 +9,7 @@ namespace {
 
 constexpr int kMost = 65535;                 // tokens, sequences
 constexpr int64_t kMaxStride = 1 << 20;      // elements; the kernels reach the rows of a stage with 32-bit byte offsets
-constexpr int64_t kMaxGrid = 1ll << 31;      // workgroups of a launch
+constexpr int64_t kMaxThreads = (1ll << 32) - 1024;  // threads of a launch
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -20,7 +20,7 @@ moespec_status check_desc(const moespec_attn_desc *ds) {
   if (ds->dtype != MOESPEC_F32 && ds->dtype != MOESPEC_BF16) return MOESPEC_ERR_INVALID_ARG;
   if (ds->n_heads < 1 || ds->n_kv_heads < 1 || ds->head_dim < 1 || ds->capacity < 1) return MOESPEC_ERR_INVALID_ARG;
   if (ds->n_heads % ds->n_kv_heads != 0) return MOESPEC_ERR_INVALID_ARG;
-  if (!(ds->scale > 0.f) || !isfinite(ds->scale)) return MOESPEC_ERR_INVALID_ARG;
+  if (!(ds->scale > 0.f) || !isfinite((float)((double)ds->scale * 1.4426950408889634))) return MOESPEC_ERR_INVALID_ARG;
   if (ds->n_heads > 1024) return MOESPEC_ERR_UNSUPPORTED_SHAPE;
   switch (ds->head_dim) {
     case 64: case 96: case 128: case 192: case 256: return MOESPEC_OK;
@@ -109,9 +109,9 @@ moespec_status moespec_tree_attention(const moespec_attn_desc *desc, const moesp
   if (max_len > 0 && (!k_cache || !v_cache || !cache_len || !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(cache_len)))
     return MOESPEC_ERR_INVALID_ARG;
   if ((s = check_ws(ws, ws_bytes, attn_ws(*desc, tree->n_seq, tree->max_tree, max_len))) != MOESPEC_OK) return s;
-  // workgroups (row tiles have 32 rows or more; parts are made only where there are few), and those of the combine
-  const int64_t rows = (int64_t)tree->max_tree * (desc->n_heads / desc->n_kv_heads);
-  if ((int64_t)tree->n_seq * desc->n_kv_heads * ((rows + 31) / 32) + 8 * rows >= kMaxGrid) return MOESPEC_ERR_UNSUPPORTED_SHAPE;
+  // workgroups of 256 threads: row tiles of 128 rows or more above 64 rows, parts only where there are few, up to seven more groups
+  const int64_t rows = (int64_t)tree->max_tree * (desc->n_heads / desc->n_kv_heads), tiles = rows <= 64 ? 1 : (rows + 127) / 128;
+  if ((((int64_t)tree->n_seq * desc->n_kv_heads + 7) * tiles + 1024) * 256 > kMaxThreads) return MOESPEC_ERR_UNSUPPORTED_SHAPE;
   return from_hip(launch_tree_attention(*desc, key_args(*desc, *tree, q, k_tree, v_tree, k_cache, v_cache, cache_len, max_len),
                                         out, lse, ws, static_cast<hipStream_t>(hip_stream)));
 }
@@ -130,7 +130,7 @@ moespec_status moespec_cache_weights(const moespec_attn_desc *desc, const moespe
     return MOESPEC_ERR_INVALID_ARG;
   if ((s = check_ws(ws, ws_bytes, attn_ws(*desc, tree->n_seq, tree->max_tree, max_len))) != MOESPEC_OK) return s;
   const int64_t tiles = ((int64_t)max_len + 127) / 128 + (tree->max_tree + 127) / 128;
-  if ((int64_t)tree->n_seq * desc->n_kv_heads * tiles >= kMaxGrid || tiles * 256 >= kMaxGrid) return MOESPEC_ERR_UNSUPPORTED_SHAPE;
+  if ((int64_t)tree->n_seq * desc->n_kv_heads * tiles * 256 > kMaxThreads) return MOESPEC_ERR_UNSUPPORTED_SHAPE;
   return from_hip(launch_cache_weights(*desc, key_args(*desc, *tree, q, k_tree, nullptr, k_cache, nullptr, cache_len, max_len),
                                        lse, row_weight, decay, cache_w_in, cache_w_out, tree_w, ws,
                                        static_cast<hipStream_t>(hip_stream)));
@@ -150,7 +150,7 @@ moespec_status moespec_cache_commit(const moespec_attn_desc *desc, int32_t n_lay
   if ((tree_w == nullptr) != (cache_w == nullptr) || new_len == cache_len) return MOESPEC_ERR_INVALID_ARG;
   // threads: 16 bytes of a row each
   const int64_t pieces = (int64_t)desc->head_dim * (desc->dtype == MOESPEC_BF16 ? 2 : 4) / 16;
-  if ((double)n_layers * tree->n_seq * max_path * desc->n_kv_heads * pieces / 256 >= (double)kMaxGrid - 1)
+  if ((double)n_layers * tree->n_seq * max_path * desc->n_kv_heads * pieces > (double)kMaxThreads)
     return MOESPEC_ERR_UNSUPPORTED_SHAPE;
   return from_hip(launch_cache_commit(*desc, n_layers, *tree, k_tree, v_tree, tree_w, path, n_path, max_path, k_cache, v_cache,
                                       cache_w, cache_len, new_len, static_cast<hipStream_t>(hip_stream)));
@@ -180,7 +180,8 @@ moespec_status moespec_cache_evict(const moespec_attn_desc *desc, int32_t n_laye
   if ((s = check_ws(ws, ws_bytes, moespec_evict_workspace_bytes(desc, n_layers, n_seq, budget))) != MOESPEC_OK) return s;
   const int64_t pieces = (int64_t)desc->head_dim * (desc->dtype == MOESPEC_BF16 ? 2 : 4) / 16;
   const int64_t heads = (int64_t)n_layers * n_seq * desc->n_kv_heads;
-  if ((double)heads * (((double)budget * pieces) / 1024 + 1) >= (double)kMaxGrid) return MOESPEC_ERR_UNSUPPORTED_SHAPE;
+  if (heads * 1024 > kMaxThreads || (double)heads * (((double)budget * pieces) / 1024 + 1) * 256 > (double)kMaxThreads)
+    return MOESPEC_ERR_UNSUPPORTED_SHAPE;
   return from_hip(launch_cache_evict(*desc, n_layers, n_seq, k_cache, v_cache, cache_w, cache_len, budget, recent, out_capacity,
                                      k_out, v_out, w_out, kept ? kept : static_cast<int32_t *>(ws), new_len,
                                      static_cast<hipStream_t>(hip_stream)));

@@ -131,6 +131,13 @@ def test_what_is_seen_comes_through(dtype):
     b.kc[1, 0, 30] = float("-inf")  # scores +-inf: rows of this sequence have no softmax, the other sequence has one
     out = f64(b.attention()[0])
     assert np.all(np.isnan(out[:4, :, 3])) and np.all(np.isfinite(np.delete(out[:4], 3, axis=-1)))
+    # an infinity in the last entry of a cache stays one, beside the places behind it that fill the tile
+    for H in (2, 6, 40):
+        b = Batch(dtype, H, 1, 64, [4], [90], seed=8)
+        b.vc[0, 0, 89, 3], b.vc[0, 0, 89, 7], b.vc[0, 0, 50, 9] = float("inf"), float("-inf"), float("inf")
+        out = f64(b.attention()[0])
+        assert np.all(out[:, :, [3, 9]] == np.inf) and np.all(out[:, :, 7] == -np.inf)
+        assert np.all(np.isfinite(np.delete(out, [3, 7, 9], axis=-1)))
     b = Batch(dtype, 2, 1, 64, [3], [0], seed=9, kind="empty")
     b.mask.zero_()
     out, lse = b.attention()

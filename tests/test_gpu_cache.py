@@ -166,6 +166,15 @@ def test_commit_without_weights_and_with_lengths_out_of_range():
     assert torch.equal(c.k[0, 0, 0, 2:], k0[0, 0, 0, 2:]) and torch.equal(c.k[0, 1], k0[0, 1])
 
 
+def test_commit_of_single_tokens_out_of_one_projection():
+    """One token for a whole model: layers are the only distance there is between rows."""
+    c = Caches("bf16", 3, 1, 2, 64, 9, [4], seed=2)
+    qkv = torch.randn((3, 1, 8, 64), device="cuda").bfloat16()
+    new_len = mb.moespec_cache_commit(c.desc, qkv[:, :, 4:6], qkv[:, :, 6:], i32([[0]]), i32([1]), c.k, c.v, c.len, n_layers=3)
+    assert new_len.tolist() == [5]
+    assert torch.equal(c.k[:, 0, :, 4], qkv[:, 0, 4:6]) and torch.equal(c.v[:, 0, :, 4], qkv[:, 0, 6:])
+
+
 def test_commit_behind_32_bits():
     cap = 9_000_000
     desc = mb.AttnDesc(2, 2, 128, cap, mb.BF16)
