@@ -407,7 +407,8 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
 // Tiles that some row sees in part (the cache's last one, those of the tree) follow one by one.
 template <int D>
 struct WideShape {
-  static constexpr int kKeys = 64, kTile = kKeys * Rows<uint16_t, D>::kBytes, kLds = 4 * kTile + 16;
+  static constexpr int RB = D <= 128 ? 2 : 1;  // blocks of 32 rows of a wave
+  static constexpr int kRows = 128 * RB, kKeys = 64, kTile = kKeys * Rows<uint16_t, D>::kBytes, kLds = 4 * kTile + 16;
 };
 
 // s0 (+)= a b0 and s1 (+)= a b1 with s and a in the registers that other instructions can read, b in the accumulation registers.  Left
@@ -425,9 +426,13 @@ __device__ __forceinline__ void score_mfma(f32x16 &s0, f32x16 &s1, bf16x8 a, bf1
                  : "+v"(s0), "+v"(s1)
                  : "v"(a), "a"(b0), "a"(b1));
 }
-__device__ __forceinline__ void score_wait(f32x16 (&s)[2][2]) {
-  asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[1][0]), "+v"(s[1][1]));
+__device__ __forceinline__ void score_mfma(f32x16 &s, bf16x8 a, bf16x8 b, bool first) {
+  if (first)
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b));
+  else
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b));
 }
+__device__ __forceinline__ void score_wait(f32x16 &s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s)); }
 
 template <int D>
 __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, int row_tiles, int slots,
@@ -437,7 +442,8 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
   typedef Rows<uint16_t, D> R;
   typedef WideShape<D> W;
   constexpr int NB = D / 32, NS = R::kPieces / 2, kLoads = W::kTile / 1024 / 4, kRowsPerLoad = 64 / R::kSlots;
-  constexpr int kSteps1 = 2 * NS, kSteps2 = 4 * NB;  // pairs of matrix instructions of S and of O
+  constexpr int RB = W::RB, kScores = 32 * RB;  // scores of a lane in a tile
+  constexpr int kSteps1 = 2 * NS, kSteps2 = 4 * NB;  // operands of S and of O, each multiplied RB times
   extern __shared__ __align__(16) unsigned char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l31 = lane & 31, half = lane >> 5;
@@ -453,9 +459,9 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
   const int s = part_of.s;
   if (s < 0) return;
   const SeqGeom g = seq_geom(a, s);
-  const int n_rows = g.T * a.G, r0 = tile * 256;
+  const int n_rows = g.T * a.G, r0 = tile * W::kRows;
   if (r0 >= n_rows) return;
-  const int first_t = r0 / a.G, last_t = (min(r0 + 256, n_rows) - 1) / a.G;
+  const int first_t = r0 / a.G, last_t = (min(r0 + W::kRows, n_rows) - 1) / a.G;
 
   // tiles that every row sees whole: of the cache, then of a chain in front of the first row's token; the others behind them
   const int cache_whole = g.len / 64, whole = cache_whole + (a.tree_mask ? 0 : (first_t + 1) / 64);
@@ -465,10 +471,10 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
   auto tile_at = [&](int unit) { return unit <= whole ? unit : whole + (unit - whole + kRest - 1) / kRest; };
   const int x0 = tile_at(part_of.first(my_units)), x1 = tile_at(part_of.last(my_units));
 
-  int t[2], h[2];
+  int t[RB], h[RB];
 #pragma unroll
-  for (int rb = 0; rb < 2; ++rb) {
-    const int row = min(r0 + 64 * wave + 32 * rb + l31, n_rows - 1);
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = min(r0 + 32 * RB * wave + 32 * rb + l31, n_rows - 1);
     t[rb] = row / a.G;
     h[rb] = hk * a.G + row % a.G;
   }
@@ -481,14 +487,19 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
   };
   const TileAddr<uint16_t, D> at;
   uint32_t *const odd = reinterpret_cast<uint32_t *>(lds + 4 * W::kTile);
-  f32x16 o[2][NB];
+  f32x16 o[RB][NB];
 #pragma unroll
-  for (int rb = 0; rb < 2; ++rb)
+  for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[rb][b][i] = 0.f;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float m[RB], l[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    m[rb] = -INFINITY;
+    l[rb] = 0.f;
+  }
 
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds);
   const int64_t head = ((int64_t)s * a.Hk + hk) * a.capacity * D;
@@ -528,27 +539,33 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
     wait_vm<0>();
     barrier();
     issue(1);
-    const bool active = r0 + 64 * wave < n_rows;
+    const bool active = r0 + 32 * RB * wave < n_rows;
     if (!active) {  // rows past the end: this wave only carries its share of the tiles
       for (int i = 0; i < n; ++i) next_tile(i);
     } else {
-      bf16x8 q[2][NS];
-      load_q(q[0], 0);
-      load_q(q[1], 1);
+      bf16x8 q[RB][NS];
 #pragma unroll
-      for (int e = 0; e < 2 * NS; ++e) asm volatile("" : "+a"(q[e / NS][e % NS]));  // that is where they stay
-      f32x16 sa[2][2], sb[2][2];  // scores [32-key block][32-row block] of the present and of the next tile
-      auto key = [&](int place, int step) { return at.key(lds0 + place * W::kTile, step / NS, step % NS); };
-      auto value = [&](int place, int step) {
-        return at.values(lds0 + (2 + place) * W::kTile, step / NB / 2, step / NB % 2, step % NB);
-      };
-      float mx[2];
+      for (int rb = 0; rb < RB; ++rb) load_q(q[rb], rb);
+#pragma unroll
+      for (int e = 0; e < RB * NS; ++e) asm volatile("" : "+a"(q[e / NS][e % NS]));  // that is where they stay
+      f32x16 sa[2][RB], sb[2][RB];  // scores [32-key block][32-row block] of the present and of the next tile
+      TileAddr<uint16_t, D> in = at;
+      in.move(lds0, lds0 + 2 * W::kTile);
+      auto key = [&](int place, int step) { return in.key(place * W::kTile, step / NS, step % NS); };
+      auto value = [&](int place, int step) { return in.values(place * W::kTile, step / NB / 2, step / NB % 2, step % NB); };
+      float mx[RB];
       auto raise_max = [&]() {
-        const float top[2] = {half_swap(mx[0], true) * a.c, half_swap(mx[1], true) * a.c};
-        const bool raise[2] = {top[0] > m[0] + 8.f, top[1] > m[1] + 8.f};
-        if (__builtin_expect(__ballot(raise[0] || raise[1]) != 0, 0)) {
+        float top[RB];
+        bool raise[RB], any = false;
 #pragma unroll
-          for (int rb = 0; rb < 2; ++rb) {
+        for (int rb = 0; rb < RB; ++rb) {
+          top[rb] = half_swap(mx[rb], true) * a.c;
+          raise[rb] = top[rb] > m[rb] + 8.f;
+          any |= raise[rb];
+        }
+        if (__builtin_expect(__ballot(any) != 0, 0)) {
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) {
             const float alpha = raise[rb] ? __builtin_amdgcn_exp2f(m[rb] - top[rb]) : 1.f;
             m[rb] = raise[rb] ? top[rb] : m[rb];
             l[rb] *= alpha;
@@ -560,14 +577,16 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
         }
       };
       // the scores `sc` of a tile whose values lie in place `at` into O, and the scores `next` of the tile behind it if there is one
-      auto body = [&](f32x16(&sc)[2][2], f32x16(&next)[2][2], auto at_, auto has_next_) {
+      auto body = [&](f32x16(&sc)[2][RB], f32x16(&next)[2][RB], auto at_, auto has_next_) {
         constexpr int kAt = decltype(at_)::value;
         constexpr bool kNext = decltype(has_next_)::value;
-        const float mu[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
-        uint32_t p[4][2][4];  // weights as operands: [16 keys][32-row block], two per word
-        // weight e of 64: keys 16 (e / 16) .., row block e / 8 % 2
+        float mu[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) mu[rb] = m[rb] == -INFINITY ? 0.f : m[rb];
+        uint32_t p[4][RB][4];  // weights as operands: [16 keys][32-row block], two per word
+        // weight e of kScores: keys 16 j .., row block rb
         auto weight = [&](int e) {
-          const int j = e / 16, rb = e / 8 % 2, k = e % 8;
+          const int j = e / (8 * RB), rb = e / 8 % RB, k = e % 8;
           const float v = __builtin_amdgcn_exp2f(fmaf(sc[j / 2][rb][8 * (j % 2) + k], a.c, -mu[rb]));
           sc[j / 2][rb][8 * (j % 2) + k] = v;
           l[rb] += v;
@@ -578,56 +597,66 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
             p[j][rb][k / 2] = __builtin_bit_cast(uint32_t, w);
           }
         };
+        constexpr int kEarly = 3 * kScores / 4, kLate = kScores - kEarly;  // weights beside S, and beside the first half of O
         if constexpr (kNext) {
           bf16x8 kf[2] = {key(1 - kAt, 0), key(1 - kAt, 1)};
 #pragma unroll
           for (int st = 0; st < kSteps1; ++st) {
             __builtin_amdgcn_sched_barrier(0);
-            score_mfma(next[st / NS][0], next[st / NS][1], kf[st % 2], q[0][st % NS], q[1][st % NS], st % NS == 0);
+            if constexpr (RB == 2)
+              score_mfma(next[st / NS][0], next[st / NS][1], kf[st % 2], q[0][st % NS], q[1][st % NS], st % NS == 0);
+            else
+              score_mfma(next[st / NS][0], kf[st % 2], q[0][st % NS], st % NS == 0);
             if (st + 2 < kSteps1) kf[st % 2] = key(1 - kAt, st + 2);
 #pragma unroll
-            for (int e = 48 * st / kSteps1; e < 48 * (st + 1) / kSteps1; ++e) weight(e);
+            for (int e = kEarly * st / kSteps1; e < kEarly * (st + 1) / kSteps1; ++e) weight(e);
           }
         } else {
 #pragma unroll
-          for (int e = 0; e < 48; ++e) weight(e);
+          for (int e = 0; e < kEarly; ++e) weight(e);
         }
-        float top[2] = {-INFINITY, -INFINITY};
+        float top[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) top[rb] = -INFINITY;
         bf16x8 vf[2] = {value(kAt, 0), value(kAt, 1)};
 #pragma unroll
         for (int st = 0; st < kSteps2; ++st) {
           __builtin_amdgcn_sched_barrier(0);
           constexpr int kHalf = kSteps2 / 2;
           const int j = st / NB;
-          if (kNext && st == kHalf)  // from here on the next scores may be read
-            asm volatile("" : "+v"(next[0][0]), "+v"(next[0][1]), "+v"(next[1][0]), "+v"(next[1][1]));
+          if (kNext && st == kHalf) {  // from here on the next scores may be read
 #pragma unroll
-          for (int rb = 0; rb < 2; ++rb)
+            for (int e = 0; e < 2 * RB; ++e) asm volatile("" : "+v"(next[e / RB][e % RB]));
+          }
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
             o[rb][st % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                 vf[st % 2], __builtin_bit_cast(bf16x8, uint4{p[j][rb][0], p[j][rb][1], p[j][rb][2], p[j][rb][3]}),
                 o[rb][st % NB], 0, 0, 0);
           if (st + 2 < kSteps2) vf[st % 2] = value(kAt, st + 2);
           if (st < kHalf) {
 #pragma unroll
-            for (int e = 48 + 16 * st / kHalf; e < 48 + 16 * (st + 1) / kHalf; ++e) weight(e);
+            for (int e = kEarly + kLate * st / kHalf; e < kEarly + kLate * (st + 1) / kHalf; ++e) weight(e);
           } else if (kNext) {
 #pragma unroll
-            for (int e = 64 * (st - kHalf) / kHalf; e < 64 * (st - kHalf + 1) / kHalf; ++e)
+            for (int e = kScores * (st - kHalf) / kHalf; e < kScores * (st - kHalf + 1) / kHalf; ++e)
               top[e / 32] = fmaxf(top[e / 32], next[e / 16 % 2][e / 32][e % 16]);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
-        mx[0] = top[0];
-        mx[1] = top[1];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) mx[rb] = top[rb];
       };
       // scores of the first tile
 #pragma unroll
       for (int st = 0; st < kSteps1; ++st) {
-        score_mfma(sa[st / NS][0], sa[st / NS][1], key(0, st), q[0][st % NS], q[1][st % NS], st % NS == 0);
+        if constexpr (RB == 2) score_mfma(sa[st / NS][0], sa[st / NS][1], key(0, st), q[0][st % NS], q[1][st % NS], st % NS == 0);
+        else score_mfma(sa[st / NS][0], key(0, st), q[0][st % NS], st % NS == 0);
       }
-      score_wait(sa);
 #pragma unroll
-      for (int rb = 0; rb < 2; ++rb) {
+      for (int e = 0; e < 2 * RB; ++e) score_wait(sa[e / RB][e % RB]);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
         mx[rb] = sa[0][rb][0];
 #pragma unroll
         for (int e = 1; e < 32; ++e) mx[rb] = fmaxf(mx[rb], sa[e / 16][rb][e % 16]);
@@ -687,7 +716,7 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
     const uint16_t *vg = static_cast<const uint16_t *>(in_tree ? a.v_tree : a.v_cache) +
                          (in_tree ? (g.row0 + base) * a.kv_stride + hk * D : head + (int64_t)base * D);
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
+    for (int rb = 0; rb < RB; ++rb) {
       bf16x8 q[NS];  // loaded again, so that the registers of the walk above are free here
       load_q(q, rb);
       attend_tile<uint16_t, D, 2>(a, g, at, in_tree, false, base, keys, t[rb], lds0 + at_tile, lds0 + 2 * W::kTile + at_tile,
@@ -695,10 +724,10 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
     }
   }
 #pragma unroll
-  for (int rb = 0; rb < 2; ++rb) {
+  for (int rb = 0; rb < RB; ++rb) {
     l[rb] = half_swap(l[rb], false);
     if (m[rb] == -INFINITY && l[rb] != 0.f) m[rb] = 0.f;  // scores that are all NaN: so is the row
-    if (r0 + 64 * wave + 32 * rb + l31 < n_rows)
+    if (r0 + 32 * RB * wave + 32 * rb + l31 < n_rows)
       finish_row<uint16_t, D>(a, o[rb], m[rb], l[rb], slots, index, t[rb], h[rb], (size_t)(g.row0 + t[rb]) * a.H + h[rb], half, out,
                               lse, part, part_ml);
   }
@@ -845,9 +874,10 @@ hipError_t run_shape(const KeyArgs &a, void *out, float *lse, void *ws, hipStrea
     return few ? run_attention<T, D, 1, 1, 1>(a, out, lse, ws, st) : run_attention<T, D, 1, S::kWk1, 1>(a, out, lse, ws, st);
   if (rows <= 64)
     return few ? run_attention<T, D, 2, 1, 1>(a, out, lse, ws, st) : run_attention<T, D, 2, S::kWk2, 1>(a, out, lse, ws, st);
-  if constexpr (sizeof(T) == 2 && D <= 128) {
-    if (rows > 128)
-      return run_kernel<T, D>(tree_attention_wide_kernel<D>, 256, 256, 64, 256, WideShape<D>::kLds, a, out, lse, ws, st);
+  if constexpr (sizeof(T) == 2) {
+    if (rows > (D <= 128 ? 128 : 64))
+      return run_kernel<T, D>(tree_attention_wide_kernel<D>, WideShape<D>::kRows, 256, 64, 256, WideShape<D>::kLds, a, out, lse, ws,
+                              st);
   }
   return run_attention<T, D, 4, 1, S::kKb4>(a, out, lse, ws, st);
 }
