@@ -16,7 +16,9 @@
  * and, around that path, the static ranking of Eq. (4) (moespec_calibration_count,
  * moespec_static_shortlist: a shortlist fixed from calibration data, passed in as ext_shortlist)
  * the Oracle ranking of Eq. (6) (moespec_oracle_ranking, an upper bound for analysis) and two analysis
- * quantities of Section 4 (moespec_coverage_curve, moespec_reconstruction_error).
+ * quantities of Section 4 (moespec_coverage_curve, moespec_reconstruction_error).  The other half of a verification
+ * step - attention of the tree over a cache of keys and values, the cache's upkeep, the norm between two blocks - is at
+ * the end: moespec_tree_attention, moespec_cache_weights, moespec_cache_commit, moespec_cache_evict, moespec_block_norm.
  *
  * Conventions (all calls)
  *   Pointers  Every buffer pointer is a DEVICE pointer unless it is a descriptor struct
@@ -350,7 +352,8 @@ moespec_status moespec_stream_read(const void *buf, size_t bytes, uint32_t *chec
  *   Device data  Lengths, offsets and paths are device data and not checked on the host.  The kernels clamp them to what the
  *             buffers hold (offsets to [0, n_tokens], a tree to max_tree rows, a length to max_len, or to capacity), so
  *             that no value leads to an access outside of a buffer.
- *   Sums      are in fp32, in an order that depends on the arguments alone.
+ *   Sums      are in fp32, in an order that depends on the arguments and the device data above alone.
+ *   Sizes     A launch that would need 2^32 threads or more is MOESPEC_ERR_UNSUPPORTED_SHAPE, as are strides above 2^20.
  */
 
 /* Shape of one attention layer.  Host struct. */

@@ -4,6 +4,11 @@
 // as matrix operands in registers and walks over the rows, whose tiles of 32 lie in LDS, one ahead.  S^T = K Q^T has a row of
 // queries per lane, and the weights of a key add up in one register per lane; the 32 lanes are summed once at the end.  A
 // workgroup is the only writer of its keys, or of its part of the rows, which a second launch adds up in order.
+//
+// What bounds it: for many rows the exponentials and the two multiply-adds per score (VALU busy for 57% of the cycles, the matrix
+// cores for 32%), which run beside the next tile's matrix instructions: 4 trees of 127 tokens x 8 heads, caches of up to 32749 entries,
+// 164 us (570 TFLOP/s; 193 us with the one behind the other).  For few rows the launch and one trip to memory: 63 tokens x 16
+// heads over 4093 entries 10 us for 17 MB of keys.
 #include <math.h>
 
 #include "attention.h"
