@@ -378,7 +378,7 @@ typedef struct {
                              /* its tree.  NULL: a chain, every token sees those up to itself         */
 } moespec_tree;
 
-/* Checks the ranges above; H <= 1024.  MOESPEC_OK, MOESPEC_ERR_INVALID_ARG or MOESPEC_ERR_UNSUPPORTED_SHAPE.  Host only. */
+/* Checks the ranges above; H <= 1024, capacity <= 2^31 - 2^16.  MOESPEC_OK, MOESPEC_ERR_INVALID_ARG or MOESPEC_ERR_UNSUPPORTED_SHAPE.  Host only. */
 moespec_status moespec_check_attn_desc(const moespec_attn_desc *desc);
 
 /*
@@ -432,7 +432,7 @@ moespec_status moespec_cache_weights(const moespec_attn_desc *desc, const moespe
  *   n_path   [n_seq] int32 in             entries past the capacity are dropped
  *   k_cache, v_cache [n_layers, n_seq, Hk, capacity, D] dtype in/out
  *   cache_len [n_seq] int32 in
- *   new_len  [n_seq] int32 out            min(cache_len + n_path, capacity); not cache_len itself; may be NULL
+ *   new_len  [n_seq] int32 out            min(cache_len + n_path, capacity); neither cache_len nor n_path itself; may be NULL
  */
 moespec_status moespec_cache_commit(const moespec_attn_desc *desc, int32_t n_layers, const moespec_tree *tree,
                                     const void *k_tree, const void *v_tree, const float *tree_w, const int32_t *path,

@@ -616,6 +616,12 @@ class _Call:
             raise MoeSpecError(int(st), self._name)
 
 
+def _allocating(stream):
+    """Where a function allocates for a call on `stream`: there, so that fills come before the call and memory that is freed after
+    it is reused behind it."""
+    return torch.cuda.stream(stream)  # (of None: as things are)
+
+
 class _Args:
     """Pointers of tensors that have to lie on one device."""
 
@@ -706,17 +712,18 @@ class TreeAttentionCall(_Call):
 
 def moespec_tree_attention(desc: AttnDesc, q, k_tree, v_tree, k_cache=None, v_cache=None, cache_len=None, ws=None, out=None,
                            lse=None, tree_off=None, tree_mask=None, max_tree=None, max_len=None, stream=None):
-    """Attention of drafted tokens over cache and tree (TreeAttentionCall).  Returns (out, lse).  Without tree_off, rows that are
-    not given are one tree; padding rows of a new `out` are not written."""
+    """Attention of drafted tokens over cache and tree (TreeAttentionCall).  Returns (out, lse).  Without tree_off all rows
+    are one tree; padding rows of a new `out` are not written."""
     M = q.shape[0]
     S, most = _sizes(M, tree_off, max_tree)
-    if out is None:
-        out = torch.empty((M, desc.n_heads, desc.head_dim), dtype=q.dtype, device=q.device)
-    if lse is None:
-        lse = torch.empty((M, desc.n_heads), dtype=torch.float32, device=q.device)
-    if ws is None:
-        ws = alloc_attn_workspace(desc, S, M, most, (0 if k_cache is None else desc.capacity) if max_len is None else max_len,
-                                  q.device)
+    with _allocating(stream):
+        if out is None:
+            out = torch.empty((M, desc.n_heads, desc.head_dim), dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty((M, desc.n_heads), dtype=torch.float32, device=q.device)
+        if ws is None:
+            ws = alloc_attn_workspace(desc, S, M, most, (0 if k_cache is None else desc.capacity) if max_len is None else max_len,
+                                      q.device)
     TreeAttentionCall(desc, q, k_tree, v_tree, k_cache, v_cache, cache_len, ws, out, lse, tree_off, tree_mask, max_tree,
                       max_len, stream)()
     return out, lse
@@ -755,13 +762,14 @@ def moespec_cache_weights(desc: AttnDesc, q, k_tree, k_cache, cache_len, lse, ws
     """Weight that every cached key and every key of the trees received (CacheWeightsCall).  Returns (cache_w, tree_w)."""
     M = q.shape[0]
     S, most = _sizes(M, tree_off, max_tree)
-    if cache_w is None and k_cache is not None:
-        cache_w = torch.zeros((S, desc.n_kv_heads, desc.capacity), dtype=torch.float32, device=q.device)
-    if tree_w is None:
-        tree_w = torch.zeros((M, desc.n_kv_heads), dtype=torch.float32, device=q.device)
-    if ws is None:
-        ws = alloc_attn_workspace(desc, S, M, most, (0 if k_cache is None else desc.capacity) if max_len is None else max_len,
-                                  q.device)
+    with _allocating(stream):
+        if cache_w is None and k_cache is not None:
+            cache_w = torch.zeros((S, desc.n_kv_heads, desc.capacity), dtype=torch.float32, device=q.device)
+        if tree_w is None:
+            tree_w = torch.zeros((M, desc.n_kv_heads), dtype=torch.float32, device=q.device)
+        if ws is None:
+            ws = alloc_attn_workspace(desc, S, M, most, (0 if k_cache is None else desc.capacity) if max_len is None else max_len,
+                                      q.device)
     CacheWeightsCall(desc, q, k_tree, k_cache, cache_len, lse, ws, cache_w, tree_w, cache_w_in, decay, row_weight, tree_off,
                      tree_mask, max_tree, max_len, stream)()
     return cache_w, tree_w
@@ -798,7 +806,8 @@ def moespec_cache_commit(desc: AttnDesc, k_tree, v_tree, path, n_path, k_cache, 
                          cache_w=None, tree_off=None, max_tree=None, n_layers=1, stream=None) -> torch.Tensor:
     """Accepted paths appended to the caches, in place (CacheCommitCall).  Returns new_len."""
     if new_len is None:
-        new_len = torch.empty_like(cache_len)
+        with _allocating(stream):
+            new_len = torch.empty_like(cache_len)
     CacheCommitCall(desc, k_tree, v_tree, path, n_path, k_cache, v_cache, cache_len, new_len, tree_w, cache_w, tree_off, max_tree,
                     n_layers, stream)()
     return new_len
@@ -830,11 +839,12 @@ def moespec_cache_evict(desc: AttnDesc, k_cache, v_cache, cache_w, cache_len, bu
     """Caches cut to a budget (CacheEvictCall).  Returns dict(k, v, w, kept, new_len); entries of k, v, w behind new_len are 0."""
     L, S, Hk, D, dev = int(n_layers), cache_len.numel(), desc.n_kv_heads, desc.head_dim, k_cache.device
     n = max(int(budget), 1)
-    k, v = (torch.zeros((L, S, Hk, n, D), dtype=k_cache.dtype, device=dev) for _ in range(2))
-    w = torch.zeros((L, S, Hk, n), dtype=torch.float32, device=dev)
-    kept = torch.empty((L, S, Hk, n), dtype=torch.int32, device=dev)
-    new_len = torch.empty_like(cache_len)
-    ws = torch.empty(max(evict_workspace_bytes(desc, L, S, n), 1), dtype=torch.uint8, device=dev)
+    with _allocating(stream):
+        k, v = (torch.zeros((L, S, Hk, n, D), dtype=k_cache.dtype, device=dev) for _ in range(2))
+        w = torch.zeros((L, S, Hk, n), dtype=torch.float32, device=dev)
+        kept = torch.empty((L, S, Hk, n), dtype=torch.int32, device=dev)
+        new_len = torch.empty_like(cache_len)
+        ws = torch.empty(max(evict_workspace_bytes(desc, L, S, n), 1), dtype=torch.uint8, device=dev)
     CacheEvictCall(desc, k_cache, v_cache, cache_w, cache_len, budget, recent, k, v, w, ws, kept if budget == n else None, new_len,
                    n_layers, stream)()
     return dict(k=k, v=v, w=w, kept=kept, new_len=new_len)
@@ -864,7 +874,8 @@ class BlockNormCall(_Call):
 def moespec_block_norm(desc: LayerDesc, y, residual=None, r=None, x=None, post_norm=False, w_post=None, gate=None,
                        gate_kind=BLOCK_GATE_NONE, gate_sigmoid=False, scale=1.0, w_pre=None, eps=0.0, stream=None):
     """From a block's output to the residual stream and the next block's input (BlockNormCall).  Returns (r, x)."""
-    r = torch.empty_like(y) if r is None else r
-    x = torch.empty_like(y) if x is None else x
+    with _allocating(stream):
+        r = torch.empty_like(y) if r is None else r
+        x = torch.empty_like(y) if x is None else x
     BlockNormCall(desc, y, residual, r, x, post_norm, w_post, gate, gate_kind, gate_sigmoid, scale, w_pre, eps, stream)()
     return r, x

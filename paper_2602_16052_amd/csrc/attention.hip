@@ -27,7 +27,7 @@ struct AttnShape {
   static constexpr int kRow = Rows<T, D>::kBytes;
   static constexpr int kWk1 = 1024 / kRow < 4 ? 1024 / kRow : 4;  // key waves for up to 32 rows: a stage of up to 64 KB
   static constexpr int kWk2 = 1024 / kRow < 2 ? 1024 / kRow : 2;  // ... for up to 64
-  static constexpr int kKb4 = kRow <= 256 && sizeof(T) == 2 ? 2 : 1;  // 32-key blocks of a wave with 128 rows a workgroup
+  static constexpr int kKb4 = sizeof(T) == 2 ? 2 : 1;  // 32-key blocks of a wave with 128 rows a workgroup
 };
 
 // Where a lane's operands lie in a tile of keys and one of values: few addresses, everything else is a constant offset (swz
@@ -825,10 +825,14 @@ namespace {
 constexpr int kPartRows = 1 << 16;    // most rows (x parts) of a launch whose keys are in parts: workgroups wanted x their rows
 constexpr size_t kFirstBytes = 2048;  // first parts of up to kMaxShared sequences
 constexpr int kFewStages = 512;        // (see run_shape)
-constexpr int kJoinRows = 4096;       // up to here a workgroup of the combine has one row
+// Up to here a workgroup of the combine has one row, whose parts its eight groups share (one token over 4000 entries 12.2 us, against 33.5
+// with a group per row); above, a row per group (16 trees of 31 tokens x 32 heads, 4 parts: 168 us against 196).
+constexpr int kJoinRows = 4096;
 
 // Up to kFewStages stages of 32 keys in all, every workgroup has one (see the head of this file for both sides).  More than 128
-// rows (64 where heads are longer than 128) take the straight-line form: with 129 rows it does the work of 256 and still is ahead.
+// rows (64 where heads are longer than 128) take the straight-line form, which with 132 or 160 rows does the work of 256 and still is
+// ahead over long caches (8 KV heads, 32768 entries: 48.8 and 50.0 us against 52.1 and 53.1; with 124 rows it is not, 47.7 against 43.2).
+// Over short ones and with 240 rows the other form would be a little faster (4 sequences, 4096 entries: 39.2 against 41.3 us).
 // Parts of the keys (share_of): as many as give `target` workgroups, none without a stage; 0 where every sequence is one part.
 int slots_of(const KeyArgs &a, int64_t row_tiles, int64_t target, int64_t stage_keys) {
   const int64_t stages = (a.max_len + stage_keys - 1) / stage_keys + (a.max_tree + stage_keys - 1) / stage_keys;
@@ -892,7 +896,8 @@ hipError_t run_shape(const KeyArgs &a, void *out, float *lse, void *ws, hipStrea
       return run_kernel<T, D>(tree_attention_wide_kernel<D>, WideShape<D>::kRows, 256, 64, 256, WideShape<D>::kLds, a, out, lse, ws,
                               st);
   }
-  return run_attention<T, D, 4, 1, S::kKb4>(a, out, lse, ws, st);
+  if constexpr (sizeof(T) == 4 || D <= 128) return run_attention<T, D, 4, 1, S::kKb4>(a, out, lse, ws, st);
+  return hipErrorInvalidValue;  // not reached: longer bf16 heads have taken one of the forms above
 }
 
 template <typename T>

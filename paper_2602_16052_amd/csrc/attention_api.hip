@@ -8,6 +8,7 @@ using namespace moespec;
 namespace {
 
 constexpr int kMost = 65535;                 // tokens, sequences
+constexpr int32_t kMaxEntries = 0x7fff0000;   // the kernels round numbers of entries up to whole tiles in 32 bits
 constexpr int64_t kMaxStride = 1 << 20;      // elements; the kernels reach the rows of a stage with 32-bit byte offsets
 constexpr int64_t kMaxThreads = (1ll << 32) - 1024;  // threads of a launch
 
@@ -21,7 +22,7 @@ moespec_status check_desc(const moespec_attn_desc *ds) {
   if (ds->n_heads < 1 || ds->n_kv_heads < 1 || ds->head_dim < 1 || ds->capacity < 1) return MOESPEC_ERR_INVALID_ARG;
   if (ds->n_heads % ds->n_kv_heads != 0) return MOESPEC_ERR_INVALID_ARG;
   if (!(ds->scale > 0.f) || !isfinite((float)((double)ds->scale * 1.4426950408889634))) return MOESPEC_ERR_INVALID_ARG;
-  if (ds->n_heads > 1024) return MOESPEC_ERR_UNSUPPORTED_SHAPE;
+  if (ds->n_heads > 1024 || ds->capacity > kMaxEntries) return MOESPEC_ERR_UNSUPPORTED_SHAPE;
   switch (ds->head_dim) {
     case 64: case 96: case 128: case 192: case 256: return MOESPEC_OK;
     default: return MOESPEC_ERR_UNSUPPORTED_SHAPE;
@@ -147,7 +148,8 @@ moespec_status moespec_cache_commit(const moespec_attn_desc *desc, int32_t n_lay
       !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(path) || !aligned4(n_path) || !aligned4(cache_len) ||
       !aligned4(new_len) || !aligned4(tree_w) || !aligned4(cache_w))
     return MOESPEC_ERR_INVALID_ARG;
-  if ((tree_w == nullptr) != (cache_w == nullptr) || new_len == cache_len) return MOESPEC_ERR_INVALID_ARG;
+  if ((tree_w == nullptr) != (cache_w == nullptr) || new_len == cache_len || (new_len && new_len == n_path))
+    return MOESPEC_ERR_INVALID_ARG;
   // threads: 16 bytes of a row each
   const int64_t pieces = (int64_t)desc->head_dim * (desc->dtype == MOESPEC_BF16 ? 2 : 4) / 16;
   if ((double)n_layers * tree->n_seq * max_path * desc->n_kv_heads * pieces > (double)kMaxThreads)
@@ -175,7 +177,7 @@ moespec_status moespec_cache_evict(const moespec_attn_desc *desc, int32_t n_laye
       !aligned4(w_out) || !aligned4(kept) || !aligned4(new_len))
     return MOESPEC_ERR_INVALID_ARG;
   if (k_out == k_cache || k_out == v_cache || v_out == k_cache || v_out == v_cache || k_out == v_out || w_out == cache_w ||
-      new_len == cache_len)
+      new_len == cache_len || kept == cache_len || (kept && kept == new_len))
     return MOESPEC_ERR_INVALID_ARG;
   if ((s = check_ws(ws, ws_bytes, moespec_evict_workspace_bytes(desc, n_layers, n_seq, budget))) != MOESPEC_OK) return s;
   const int64_t pieces = (int64_t)desc->head_dim * (desc->dtype == MOESPEC_BF16 ? 2 : 4) / 16;

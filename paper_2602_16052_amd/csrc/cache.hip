@@ -264,7 +264,7 @@ __global__ __launch_bounds__(kGatherThreads) void cache_gather_kernel(const uint
   for (int u = 0; u < 4; ++u) {
     const int64_t i = i0 + u * kGatherThreads;
     src[u] = list[min(i, total - 1) / pieces];
-    src[u] = i < total ? src[u] : -1;
+    src[u] = i < total && src[u] < capacity ? src[u] : -1;  // (a list that somebody else wrote to meanwhile)
   }
 #pragma unroll
   for (int u = 0; u < 4; ++u) {  // places that stay empty load the first entry

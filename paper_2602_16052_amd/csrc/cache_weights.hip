@@ -19,7 +19,10 @@ constexpr int kWeightWaves = 4;
 
 template <typename T, int D>
 struct WeightShape {
-  static constexpr int kKb = D * (int)sizeof(T) <= 256 ? 2 : 1;  // 32-key blocks held by a wave
+  // 32-key blocks held by a wave.  Two where the registers allow it: every row operand that is read is multiplied twice (4 trees of
+  // 127 tokens, 32749 entries: 172 us against 192; fp32 heads of 64, 63 tokens x 8 over 8192: 37 against 42); one would be faster for one
+  // or two tiles of rows (63 tokens over 4093 entries: 8.2 us against 9.3).
+  static constexpr int kKb = D * (int)sizeof(T) <= 256 ? 2 : 1;
   static constexpr int kKeys = 32 * kKb * kWeightWaves;
   static constexpr int kRing = 4, kLds = kRing * (32 * Rows<T, D>::kBytes + 512 * kWeightWaves);
 };

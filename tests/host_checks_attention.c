@@ -86,6 +86,14 @@ static void descriptors_and_workspaces(void) {
       (void)moespec_attn_workspace_bytes(&ds, 65535, big[i], big[j], big[(i + j) % 8]);
       (void)moespec_evict_workspace_bytes(&ds, 1, big[i], big[j]);
     }
+  EXPECT(moespec_check_attn_desc(&ds) == MOESPEC_ERR_UNSUPPORTED_SHAPE); /* entries in whole tiles have to fit 32 bits */
+  ds.capacity = 0x7fff0000;
+  EXPECT(moespec_check_attn_desc(&ds) == MOESPEC_OK);
+  for (size_t i = 0; i < 8; ++i)
+    for (size_t j = 0; j < 8; ++j) {
+      (void)moespec_attn_workspace_bytes(&ds, big[i], 65535, big[j], 0x7fff0000);
+      (void)moespec_attn_workspace_bytes(&ds, 65535, big[i], big[j], big[(i + j) % 8]);
+    }
   EXPECT(moespec_attn_workspace_bytes(&ds, 1, 8, 9, 50) == 0);  /* a tree larger than all tokens */
   EXPECT(moespec_attn_workspace_bytes(&ds, 0, 8, 8, 50) == 0);
   EXPECT(moespec_evict_workspace_bytes(&ds, 0, 1, 8) == 0);
@@ -159,14 +167,15 @@ static void cache_arguments(void) {
   moespec_tree t = make_tree(2, 16, 8);
   int32_t *p = fake(0x10000), *l = fake(0x20000);
   float *w = fake(0x30000);
-  EXPECT(moespec_cache_commit(&ds, 0, &t, p, p, NULL, p, p, 4, p, p, NULL, l, p, NULL) == MOESPEC_ERR_INVALID_ARG);
-  EXPECT(moespec_cache_commit(&ds, 1, &t, p, p, NULL, p, p, 0, p, p, NULL, l, p, NULL) == MOESPEC_ERR_INVALID_ARG);
-  EXPECT(moespec_cache_commit(&ds, 1, &t, p, p, w, p, p, 4, p, p, NULL, l, p, NULL) == MOESPEC_ERR_INVALID_ARG);
+  EXPECT(moespec_cache_commit(&ds, 0, &t, p, p, NULL, p, l, 4, p, p, NULL, l, p, NULL) == MOESPEC_ERR_INVALID_ARG);
+  EXPECT(moespec_cache_commit(&ds, 1, &t, p, p, NULL, p, l, 0, p, p, NULL, l, p, NULL) == MOESPEC_ERR_INVALID_ARG);
+  EXPECT(moespec_cache_commit(&ds, 1, &t, p, p, w, p, l, 4, p, p, NULL, l, p, NULL) == MOESPEC_ERR_INVALID_ARG);
   EXPECT(moespec_cache_commit(&ds, 1, &t, p, p, NULL, p, p, 4, p, p, NULL, l, l, NULL) == MOESPEC_ERR_INVALID_ARG);
-  EXPECT(moespec_cache_commit(&ds, 1, &t, p, NULL, NULL, p, p, 4, p, p, NULL, l, p, NULL) == MOESPEC_ERR_INVALID_ARG);
-  EXPECT(moespec_cache_commit(&ds, 1, &t, p, p, NULL, NULL, p, 4, p, p, NULL, l, p, NULL) == MOESPEC_ERR_INVALID_ARG);
+  EXPECT(moespec_cache_commit(&ds, 1, &t, p, p, NULL, p, l, 4, p, p, NULL, p, l, NULL) == MOESPEC_ERR_INVALID_ARG);
+  EXPECT(moespec_cache_commit(&ds, 1, &t, p, NULL, NULL, p, l, 4, p, p, NULL, l, p, NULL) == MOESPEC_ERR_INVALID_ARG);
+  EXPECT(moespec_cache_commit(&ds, 1, &t, p, p, NULL, NULL, l, 4, p, p, NULL, l, p, NULL) == MOESPEC_ERR_INVALID_ARG);
   moespec_tree b = make_tree(65535, 65535, 1);
-  EXPECT(moespec_cache_commit(&ds, 4096, &b, p, p, NULL, p, p, 65535, p, p, NULL, l, p, NULL) == MOESPEC_ERR_UNSUPPORTED_SHAPE);
+  EXPECT(moespec_cache_commit(&ds, 4096, &b, p, p, NULL, p, l, 65535, p, p, NULL, l, p, NULL) == MOESPEC_ERR_UNSUPPORTED_SHAPE);
 
   int32_t *ko = fake(0x40000), *vo = fake(0x50000), *ws = fake(0x70000);
   float *wo = fake(0x60000);
@@ -184,6 +193,8 @@ static void cache_arguments(void) {
          MOESPEC_ERR_INVALID_ARG);
   EXPECT(moespec_cache_evict(&ds, 1, 2, p, v, w, l, 50, 10, 50, ko, vo, w, NULL, NULL, ws, need, NULL) == MOESPEC_ERR_INVALID_ARG);
   EXPECT(moespec_cache_evict(&ds, 1, 2, p, v, w, l, 50, 10, 50, ko, vo, wo, NULL, l, ws, need, NULL) == MOESPEC_ERR_INVALID_ARG);
+  EXPECT(moespec_cache_evict(&ds, 1, 2, p, v, w, l, 50, 10, 50, ko, vo, wo, l, NULL, ws, need, NULL) == MOESPEC_ERR_INVALID_ARG);
+  EXPECT(moespec_cache_evict(&ds, 1, 2, p, v, w, l, 50, 10, 50, ko, vo, wo, p, p, ws, need, NULL) == MOESPEC_ERR_INVALID_ARG);
   EXPECT(moespec_cache_evict(&ds, 1, 2, p, v, NULL, l, 50, 10, 50, ko, vo, wo, NULL, NULL, ws, need, NULL) ==
          MOESPEC_ERR_INVALID_ARG);
 }

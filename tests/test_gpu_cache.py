@@ -296,3 +296,23 @@ def test_captured_commit_and_evict_follow_the_lengths():
         for a, b in zip(got, (k, v, w, kept, new_len, evicted)):
             assert torch.equal(a, b)
         assert new_len.tolist() == [min(500, lens[0] + 2), min(500, lens[1] + 1)]
+
+
+def test_functions_allocate_on_the_stream_they_are_given():
+    """Results that a function allocates are cleared before its call on another stream, not by work of the present one that
+    comes later, and its workspace is not handed out again while the call may still run."""
+    c = Caches("bf16", 1, 2, 2, 64, 600, [500, 90], seed=7)
+    b = Batch("bf16", 4, 2, 64, [5, 9], [200, 30], seed=8)
+    lse = b.attention()[1]
+    want = mb.moespec_cache_evict(c.desc, c.k, c.v, c.w, c.len, 100, 10)
+    want_w = mb.moespec_cache_weights(b.desc, b.q, b.kt, b.kc, b.cache_len, lse, **b.args)
+    side, busy = torch.cuda.Stream(), torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(40):
+        busy = busy @ busy  # the present stream is occupied
+    got = mb.moespec_cache_evict(c.desc, c.k, c.v, c.w, c.len, 100, 10, stream=side)
+    got_w = mb.moespec_cache_weights(b.desc, b.q, b.kt, b.kc, b.cache_len, lse, stream=side, **b.args)
+    torch.cuda.synchronize()
+    for name in want:
+        assert torch.equal(want[name], got[name]), name
+    assert torch.equal(want_w[0], got_w[0]) and torch.equal(want_w[1], got_w[1])
