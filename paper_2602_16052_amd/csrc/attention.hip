@@ -256,8 +256,9 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
   uint32_t *const odd = reinterpret_cast<uint32_t *>(lds + 2 * kStage);  // [2][kStageKeys / 32], for a stage and the next one
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
   const int l31 = lane & 31, half = lane >> 5;
-  // row tiles that share keys are neighbours on one XCD (workgroup b runs on XCD b mod 8)
-  const int slot = blockIdx.x / 8, group = slot / row_tiles * 8 + (int)(blockIdx.x % 8), tile = slot % row_tiles;
+  // row tiles that share keys are neighbours on one XCD (workgroup b runs on XCD b mod 8).  The last ones first: in a chain they see the
+  // most keys, and what is left for the end of the launch is short (4096 tokens without a cache 154 us, 193 the other way round).
+  const int slot = blockIdx.x / 8, group = slot / row_tiles * 8 + (int)(blockIdx.x % 8), tile = row_tiles - 1 - slot % row_tiles;
   const int n_parts = slots == 0 ? a.n_seq : slots, index = group % n_parts, hk = group / n_parts;
   if (hk >= a.Hk) return;
   auto stages = [&](const SeqGeom &g) {
@@ -458,7 +459,7 @@ __global__ __launch_bounds__(256, 1) void tree_attention_wide_kernel(KeyArgs a, 
   extern __shared__ __align__(16) unsigned char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l31 = lane & 31, half = lane >> 5;
-  const int slot = blockIdx.x / 8, group = slot / row_tiles * 8 + (int)(blockIdx.x % 8), tile = slot % row_tiles;
+  const int slot = blockIdx.x / 8, group = slot / row_tiles * 8 + (int)(blockIdx.x % 8), tile = row_tiles - 1 - slot % row_tiles;
   const int n_parts = slots == 0 ? a.n_seq : slots, index = group % n_parts, hk = group / n_parts;
   if (hk >= a.Hk) return;
   // a tile that some row sees in part takes as long as kRest others
@@ -824,15 +825,29 @@ namespace {
 
 constexpr int kPartRows = 1 << 16;    // most rows (x parts) of a launch whose keys are in parts: workgroups wanted x their rows
 constexpr size_t kFirstBytes = 2048;  // first parts of up to kMaxShared sequences
-constexpr int kFewStages = 512;        // (see run_shape)
+constexpr int kFewStages = 512;       // up to as many stages of 32 keys in all every workgroup has one (both sides: head of this file)
+constexpr int kWideSlots = 256;       // workgroups of the straight-line form that run at a time
 // Up to here a workgroup of the combine has one row, whose parts its eight groups share (one token over 4000 entries 12.2 us, against 33.5
 // with a group per row); above, a row per group (16 trees of 31 tokens x 32 heads, 4 parts: 168 us against 196).
 constexpr int kJoinRows = 4096;
 
-// Up to kFewStages stages of 32 keys in all, every workgroup has one (see the head of this file for both sides).  More than 128
-// rows (64 where heads are longer than 128) take the straight-line form, which with 132 or 160 rows does the work of 256 and still is
-// ahead over long caches (8 KV heads, 32768 entries: 48.8 and 50.0 us against 52.1 and 53.1; with 124 rows it is not, 47.7 against 43.2).
-// Over short ones and with 240 rows the other form would be a little faster (4 sequences, 4096 entries: 39.2 against 41.3 us).
+// Whether many rows take the straight-line form (heads of up to 128; longer ones always do).  It is ahead over long caches, by up to 17% (one
+// tree of 2000 tokens x 32 heads over 128000 entries 3.90 ms against 4.60; 8 chains of 256 over 4800 173 us against 186) and behind where
+// tiles that some row sees in part, start and end of a workgroup or an uneven last round weigh more: 16 chains of 256 without a cache 46.5
+// us against 32.5, one tree of 2000 without a cache 195 against 113, 8 chains of 300 over 1200 109 against 89 (five row tiles:
+// 320 workgroups on 256 compute units).  So it has to have 20 whole tiles of keys a part (511 tokens x 32 heads: even at 16, 79 us
+// against 82 at 24), ten times the tiles of the tree (2000 tokens: 3% behind at eight times, 2% ahead at twelve), and the compute units busy:
+// rounds at least three quarters full, and in a single round of a chain, whose last rows see the most keys, no less than 6 / 7 of the
+// longest part's work on average (2000 tokens: 117 against 128 us with as many entries, equal with three times as many).
+bool wide_pays(const KeyArgs &a, int64_t tile_rows) {
+  const int64_t tiles = ((int64_t)a.max_tree * a.G + tile_rows - 1) / tile_rows, groups = (int64_t)a.n_seq * a.Hk * tiles;
+  const int64_t parts = groups < kWideSlots ? kWideSlots / groups : 1, rounds = (groups + kWideSlots - 1) / kWideSlots;
+  const int64_t len = a.max_len, tree = a.max_tree;
+  if (a.tree_mask ? len < 10 * tree || len < 20 * 64 * parts : 2 * len + tree < 2 * 20 * 64 * parts) return false;
+  if (rounds > 1) return 4 * groups >= 3 * kWideSlots * rounds;
+  return a.tree_mask || 7 * (2 * len + tree) >= 6 * 2 * (len + tree);
+}
+
 // Parts of the keys (share_of): as many as give `target` workgroups, none without a stage; 0 where every sequence is one part.
 int slots_of(const KeyArgs &a, int64_t row_tiles, int64_t target, int64_t stage_keys) {
   const int64_t stages = (a.max_len + stage_keys - 1) / stage_keys + (a.max_tree + stage_keys - 1) / stage_keys;
@@ -892,8 +907,8 @@ hipError_t run_shape(const KeyArgs &a, void *out, float *lse, void *ws, hipStrea
   if (rows <= 64)
     return few ? run_attention<T, D, 2, 1, 1>(a, out, lse, ws, st) : run_attention<T, D, 2, S::kWk2, 1>(a, out, lse, ws, st);
   if constexpr (sizeof(T) == 2) {
-    if (rows > (D <= 128 ? 128 : 64))
-      return run_kernel<T, D>(tree_attention_wide_kernel<D>, WideShape<D>::kRows, 256, 64, 256, WideShape<D>::kLds, a, out, lse, ws,
+    if (D <= 128 ? rows > 128 && wide_pays(a, WideShape<D>::kRows) : rows > 64)
+      return run_kernel<T, D>(tree_attention_wide_kernel<D>, WideShape<D>::kRows, kWideSlots, 64, 256, WideShape<D>::kLds, a, out, lse, ws,
                               st);
   }
   if constexpr (sizeof(T) == 4 || D <= 128) return run_attention<T, D, 4, 1, S::kKb4>(a, out, lse, ws, st);

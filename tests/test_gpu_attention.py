@@ -253,3 +253,113 @@ def test_captured_calls_follow_lengths_and_inputs():
 def test_parents_to_masks():
     sees = A.ancestors([-1, 0, 0, 1, -1, 4])
     assert [list(np.flatnonzero(r)) for r in sees] == [[0], [0, 1], [0, 2], [0, 1, 3], [4], [4, 5]]
+
+
+# ---- many rows over long caches: the straight-line form, which takes launches that fill the card
+
+def oracle_64(b):
+    """Batch.oracle() as products of 64-bit matrices on the GPU, for batches that would take its loops minutes."""
+    G, D = b.H // b.Hk, b.D
+    out, bound = (torch.zeros((b.M, b.H, D), dtype=torch.float64, device="cuda") for _ in range(2))
+    lse = torch.full((b.M, b.H), -float("inf"), dtype=torch.float64, device="cuda")
+    spread = torch.zeros((b.M, b.H), dtype=torch.float64, device="cuda")
+    scale = float(np.float32(b.scale))
+    for s, (n, T) in enumerate(zip(b.lens, b.trees)):
+        if T == 0:
+            continue
+        rows = slice(int(b.off[s]), int(b.off[s + 1]))
+        k, v = (torch.cat([c[s, :, :n], t[rows].transpose(0, 1)], dim=1).double().contiguous()
+                for c, t in ((b.kc, b.kt), (b.vc, b.vt)))
+        q = b.q[rows].double().reshape(T, b.Hk, G, D).permute(1, 2, 0, 3).reshape(b.Hk, G * T, D).contiguous()
+        sees = torch.cat([torch.ones((T, n), dtype=torch.bool), torch.from_numpy(np.asarray(b.sees[s]))], dim=1).cuda().repeat(G, 1)
+        kt = k.transpose(1, 2).contiguous()
+        a = torch.where(sees, scale * torch.matmul(q, kt), -float("inf"))
+        top = a.amax(dim=-1, keepdim=True)
+        p = torch.exp(a - torch.where(torch.isinf(top), 0.0, top))
+        total = p.sum(dim=-1, keepdim=True)
+        p = p / torch.where(total == 0, 1.0, total)
+        back = lambda x: x.reshape(b.Hk, G, T, -1).permute(2, 0, 1, 3).reshape(T, b.H, -1)  # noqa: E731
+        out[rows], bound[rows] = back(torch.matmul(p, v)), back(torch.matmul(p, v.abs()))
+        lse[rows] = back(top + torch.log(total))[..., 0]
+        most = torch.where(sees, scale * torch.matmul(q.abs(), kt.abs()), 0.0).amax(dim=-1, keepdim=True)
+        spread[rows] = back(most)[..., 0]
+    return tuple(f64(x) for x in (out, lse, bound, spread))
+
+
+def test_oracle_of_matrices_is_the_oracle():
+    b = Batch("f32", 6, 2, 64, [9, 0, 5], [40, 3, 0], kind="empty", seed=30)
+    for x, y in zip(oracle_64(b), b.oracle()):
+        assert np.allclose(x, y, rtol=1e-12, atol=1e-12)
+
+
+LONG_TREES, LONG_LENS = [70, 1, 0, 33, 70, 64, 65, 69], [1409, 1408, 500, 0, 1, 64, 1281, 63]
+
+
+@pytest.mark.parametrize("kind", ["tree", "chain", "empty"])
+@pytest.mark.parametrize("D", [64, 96, 128])
+def test_many_rows_in_ragged_batches_that_fill_the_card(D, kind):
+    """256 workgroups, one per sequence and KV head; 140 rows: the last waves have some or none."""
+    b = Batch("bf16", 64, 32, D, LONG_TREES, LONG_LENS, kind=kind, seed=D)
+    b.check(*b.attention(), oracle_64(b))
+
+
+@pytest.mark.parametrize("S,H,Hk,T,n", [(1, 64, 16, 40, 20491), (2, 48, 16, 50, 10300), (4, 32, 16, 129, 2650), (1, 64, 16, 131, 6977)])
+@pytest.mark.parametrize("kind", ["tree", "chain"])
+def test_many_rows_over_parts_of_a_long_cache(S, H, Hk, T, n, kind):
+    b = Batch("bf16", H, Hk, 64, [T] + [T - 9] * (S - 1), [n, n // 2, 0, 77][:S], kind=kind, seed=n)
+    b.check(*b.attention(), oracle_64(b))
+
+
+def test_many_rows_of_long_chains_without_a_cache():
+    b = Batch("bf16", 32, 16, 64, [2600, 2570], [0, 0], kind="chain", seed=31)
+    b.check(*b.attention(), oracle_64(b))
+
+
+@pytest.mark.parametrize("q_scale", [0.1, 12.0])
+def test_many_rows_with_a_maximum_that_rises_along_a_long_cache(q_scale):
+    b = Batch("bf16", 64, 32, 128, [70] * 8, [1409] * 8, seed=32, q_scale=q_scale)
+    ramp = torch.linspace(0.05, 1.0, b.kc.shape[2], device="cuda")
+    b.kc.copy_((b.q[::70, ::2, None, :].float() * 0.3 + b.kc.float() * 0.2) * ramp[None, None, :, None])
+    b.kc[:, :, 1409:] = float("nan")
+    b.check(*b.attention(), oracle_64(b))
+
+
+def test_many_rows_and_values_that_are_not_seen_over_a_long_cache():
+    b = Batch("bf16", 64, 32, 64, [70] * 8, [1409] * 8, seed=33)
+    first = torch.arange(8, device="cuda") * 70
+    kt, vt = b.kt, b.vt
+    b.kt, b.vt = kt.clone(), vt.clone()
+    for t in (3, 40, 68):
+        b.kt[first + t], b.vt[first + t] = 0.0, 0.0  # rows that do not see these have the results without them
+    want = oracle_64(b)
+    b.kt[first + 3], b.vt[first + 3] = float("nan"), float("inf")
+    b.vt[first + 40, :, 5] = float("-inf")
+    b.vt[first + 68, :, 9] = float("nan")
+    out, lse = b.attention()
+    sees = np.concatenate(b.sees)
+    clean = ~(sees[:, 3] | sees[:, 40] | sees[:, 68])
+    assert 0 < clean.sum() < len(clean)
+    keep = torch.from_numpy(clean).cuda()
+    got, got_lse = out.clone(), lse.clone()
+    got[~keep], got_lse[~keep] = 0, 0
+    tidy = lambda v: np.where(clean.reshape(-1, *[1] * (v.ndim - 1)), v, 0.0)  # noqa: E731
+    b.check(got, got_lse, tuple(tidy(v) for v in want))
+    assert np.all(np.isnan(f64(out)[sees[:, 3]]))
+    only = sees[:, 40] & ~sees[:, 3] & ~sees[:, 68]
+    got = f64(out)[only]
+    assert np.all(np.isneginf(got[..., 5])) and np.all(np.isfinite(np.delete(got, 5, axis=-1)))
+
+
+def test_many_rows_and_infinities_in_a_long_cache():
+    """In its whole tiles and in its last entry, beside the places behind it that fill the tile; a score of NaN."""
+    b = Batch("bf16", 64, 32, 64, [70] * 8, [1409] * 8, seed=34)
+    b.vc[:, :, 1408, 3], b.vc[:, :, 1408, 7], b.vc[:, :, 700, 9] = float("inf"), float("-inf"), float("inf")
+    out = f64(b.attention()[0])
+    assert np.all(out[:, :, [3, 9]] == np.inf) and np.all(out[:, :, 7] == -np.inf)
+    assert np.all(np.isfinite(np.delete(out, [3, 7, 9], axis=-1)))
+    b = Batch("bf16", 64, 32, 64, [70] * 8, [1409] * 8, seed=34)
+    b.kc[2, :, 30] = float("-inf")  # scores of +-inf: rows of this sequence have no softmax, the others have one
+    b.vc[0, :, 17, 3] = float("nan")
+    out = f64(b.attention()[0]).reshape(8, 70, 64, 64)
+    assert np.all(np.isnan(out[0, :, :, 3])) and np.all(np.isfinite(np.delete(out[0], 3, axis=-1)))
+    assert np.all(np.isfinite(out[[1, 3, 4, 5, 6, 7]])) and np.any(np.isnan(out[2]))
