@@ -166,12 +166,16 @@ __device__ __forceinline__ float half_swap(float v, bool max_) {
 }
 
 // Which of the 32 keys base .. base + 31 (of n) a row sees: all of a cache, a token's ancestors in its tree.
-__device__ __forceinline__ uint32_t keys_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+__host__ __device__ __forceinline__ uint32_t keys_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 __device__ __forceinline__ uint32_t tree_word(const KeyArgs &a, const SeqGeom &g, int t, int base) {
   if (base >= g.T) return 0;
   const uint32_t w = a.tree_mask ? a.tree_mask[(size_t)(g.row0 + t) * a.words + (base >> 5)] : keys_below(t + 1 - base);
   return w & keys_below(g.T - base);
 }
+
+// The bits of 32 places of a tile without those behind the last key (`there` places have one).  Places behind it repeat it in LDS
+// and have nothing of their own in memory.
+__host__ __device__ __forceinline__ uint32_t keys_there(uint32_t bits, int there) { return bits & keys_below(there); }
 
 // What a lane holds of a finished row (elements acc_row(i, half) of every 32; m in units of log 2) written out, or left for the
 // combine where the keys are in parts, of which this is number `index`.

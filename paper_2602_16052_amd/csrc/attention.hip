@@ -140,7 +140,8 @@ __device__ __forceinline__ bool row_not_finite(const unsigned char *tile, int r)
     bad |= sizeof(T) == 2 ? not_finite<uint16_t>(w[e] & 0xffffu) || not_finite<uint16_t>(w[e] >> 16) : not_finite<uint32_t>(w[e]);
   return __ballot(bad) != 0;
 }
-// bad: the keys (of 32, the first one's values at vg) that have such values; seen: those that this row sees.
+// bad: the keys (of 32, the first one's values at vg; each with a row of its own in memory) that have such values; seen: those that this
+// row sees.
 template <typename T, int D>
 __device__ __forceinline__ void add_odd(uint32_t bad, uint32_t seen, const T *vg, int64_t stride, f32x16 (&o)[D / 32]) {
   const int half = (threadIdx.x & 63) >> 5;
@@ -237,7 +238,7 @@ __device__ __forceinline__ void attend_tile(const KeyArgs &a, const SeqGeom &g, 
   if (odd != nullptr && !whole) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      const uint32_t bad = __builtin_amdgcn_readfirstlane(odd[kb]);
+      const uint32_t bad = keys_there(__builtin_amdgcn_readfirstlane(odd[kb]), n - base - 32 * kb);
       if (__builtin_expect(bad != 0, 0)) add_odd<T, D>(bad, word[kb], vg + 32 * kb * vstride, vstride, o);
     }
   }
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
   constexpr int kRowsPerLoad = 64 / R::kSlots, kLoads = kStageKeys / kRowsPerLoad / NW, NB = D / 32, NS = R::kPieces / 2;
   static_assert(kStageKeys % (kRowsPerLoad * NW) == 0, "every wave issues as many loads");
   extern __shared__ __align__(16) unsigned char lds[];
-  uint32_t *const odd = reinterpret_cast<uint32_t *>(lds + 2 * kStage);  // [2][kStageKeys / 32], for a stage and the next one
+  uint32_t *const odd = reinterpret_cast<uint32_t *>(lds + 2 * kStage);  // [2][kStageKeys / 32], for the stages of both places
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
   const int l31 = lane & 31, half = lane >> 5;
   // row tiles that share keys are neighbours on one XCD (workgroup b runs on XCD b mod 8).  The last ones first: in a chain they see the
@@ -270,7 +271,6 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
   const SeqGeom g = seq_geom(a, s);
   const int n_rows = g.T * a.G, r0 = tile * 32 * WR;
   if (r0 >= n_rows) return;
-  if (threadIdx.x < 2 * kStageKeys / 32) odd[threadIdx.x] = 0;
 
   // stages: those of the cache, then those of the tree (of a chain only up to the last row's token)
   const int ct = (g.len + kStageKeys - 1) / kStageKeys, all = ct + (g.T + kStageKeys - 1) / kStageKeys;
@@ -328,22 +328,22 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
 
   for (int st = st0; st < st1; ++st) {
     const int buf = (st - st0) & 1;
-    wait_vm<0>();
-    asm volatile("" ::: "memory");
-    __syncthreads();  // the stage has arrived, everybody's part of it, and nobody reads the other one any more
-    if (st + 1 < st1) issue(st + 1, buf ^ 1);
     const bool tree = st >= ct;
     const int base0 = (tree ? st - ct : st) * kStageKeys, n = tree ? g.T : g.len, base = base0 + wk * KB * 32;
     // keys inside the cache, or in front of every row's own token in a chain, are seen by all rows
     auto seen_whole = [&](int from, int keys) {
       return from + keys <= n && (!tree || (a.tree_mask == nullptr && from + keys - 1 <= first_t));
     };
+    const bool in_part = !seen_whole(base0, kStageKeys);
     uint32_t *const my_odd = odd + buf * (kStageKeys / 32);
-    const bool clean = !seen_whole(base0, kStageKeys) &&
-                       (tree || row_not_finite<T, D>(lds + buf * kStage + kTile, n - 1 - base0));
+    if (in_part && threadIdx.x < kStageKeys / 32) my_odd[threadIdx.x] = 0;  // last read two stages ago
+    wait_vm<0>();
+    asm volatile("" ::: "memory");
+    __syncthreads();  // the stage has arrived, everybody's part of it, and nobody reads the other one any more
+    if (st + 1 < st1) issue(st + 1, buf ^ 1);
+    const bool clean = in_part && (tree || row_not_finite<T, D>(lds + buf * kStage + kTile, n - 1 - base0));
     if (clean) {
       __syncthreads();  // everybody has looked
-      if (threadIdx.x < kStageKeys / 32) odd[(buf ^ 1) * (kStageKeys / 32) + threadIdx.x] = 0;
       clean_values<T, D, kStageKeys, 64 * NW>(lds + buf * kStage + kTile, my_odd);
       __syncthreads();
     }

@@ -1,0 +1,41 @@
+"""Tree attention where a cache, a tree or a row ends: values that are not finite in last places, over one stage of keys and several."""
+import numpy as np
+import pytest
+import torch
+
+from attention_common import Batch, f64
+from test_gpu_attention import oracle_64
+
+pytestmark = pytest.mark.gpu
+
+
+def check_odd_ends(b):
+    """An infinity in the last value of every tree, another in the last entry of every cache (which fills it: no room behind it), a NaN
+    in the tree's middle: each reaches the rows that see it and no other, and nothing else changes."""
+    want = oracle_64(b)
+    tree, cache, middle = (np.zeros(b.M, dtype=bool) for _ in range(3))
+    for s, (T, n) in enumerate(zip(b.trees, b.lens)):
+        first = int(b.off[s])
+        if T:
+            b.vt[first + T - 1, :, 3] = float("inf")
+            b.vt[first + T // 2, :, 5] = float("nan")
+            tree[first:first + T], middle[first:first + T] = b.sees[s][:, T - 1], b.sees[s][:, T // 2]
+        if n:
+            b.vc[s, :, n - 1, 7] = float("-inf")
+            cache[first:first + T] = True
+    out, lse = b.attention()
+    got, want_out = f64(out), want[0]
+    assert np.all(got[tree][:, :, 3] == np.inf) and np.all(got[cache][:, :, 7] == -np.inf) and np.all(np.isnan(got[middle][:, :, 5]))
+    for rows, col in ((tree, 3), (middle, 5), (cache, 7)):
+        got[rows, :, col] = want_out[rows, :, col]
+    b.check(torch.from_numpy(got), lse, want)
+
+
+# rows of a KV head: up to 32, up to 64, more; trees that end inside of a stage of 32, 64 and 128 keys
+@pytest.mark.parametrize("dtype,H,Hk,D,trees,lens", [
+    ("bf16", 2, 2, 64, [9], [45]), ("bf16", 8, 4, 128, [31, 5], [161, 0]), ("bf16", 8, 4, 96, [45, 33], [200, 129]),
+    ("bf16", 8, 2, 64, [200, 71], [90, 1]), ("bf16", 8, 4, 192, [70, 3], [90, 600]), ("bf16", 6, 2, 256, [97], [333]),
+    ("f32", 4, 4, 64, [21], [77]), ("f32", 4, 2, 128, [31], [65]), ("f32", 6, 2, 96, [45, 33], [100, 3]), ("f32", 2, 1, 256, [9], [50])])
+@pytest.mark.parametrize("kind", ["tree", "chain"])
+def test_values_that_are_not_finite_in_last_places(dtype, H, Hk, D, trees, lens, kind):
+    check_odd_ends(Batch(dtype, H, Hk, D, trees, lens, kind=kind, fused=True, room=0, seed=D + H))
