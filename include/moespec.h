@@ -412,7 +412,8 @@ moespec_status moespec_tree_attention(const moespec_attn_desc *desc, const moesp
  * The attention weight that every key received, summed over the tokens and over the query heads of its KV head:
  *   w_j = sum_{t, h} row_weight[t] exp(scale q[t, h] . K_j - lse[t, h])   over the rows that see key j.
  *   lse        [M, H] float in      as written by moespec_tree_attention; a row with -inf has no part
- *   row_weight [M] float in         NULL: 1.  0 for rejected tokens, or the probability of acceptance
+ *   row_weight [M] float in         NULL: 1.  0 for rejected tokens, or the probability of acceptance.  A row of weight 0 has no part,
+ *                                   whatever its queries and its lse hold (NaN and infinities included)
  *   cache_w_in [n_seq, Hk, capacity] float in  NULL: 0.  May be cache_w_out
  *   cache_w_out                     out  decay * cache_w_in + w for the cached keys; entries behind cache_len are left alone
  *   tree_w     [M, Hk] float out    w of the trees' own keys (moespec_cache_commit takes it into the cache); may be NULL

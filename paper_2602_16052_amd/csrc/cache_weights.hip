@@ -196,10 +196,10 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
   auto row_of = [&](f32x16(&sc)[KB], int b, int buf) {
     const float *st = reinterpret_cast<const float *>(lds + buf * kStage + kTile + wave * 512);
     const int row = 32 * b + l31;
-    const float ls = st[l31], rw = st[32 + l31];
-    const bool ok = row < n_rows && ls != -INFINITY;
+    const float ls = st[l31], rw = row_weight ? st[32 + l31] : 1.f;
+    const bool ok = row < n_rows && ls != -INFINITY && rw != 0.f;  // others have no part, whatever they hold
     shift = ok ? ls * 1.4426950408889634f : 0.f;
-    weight = !ok ? 0.f : row_weight ? rw : 1.f;
+    weight = ok ? rw : 0.f;
     if (tree) {  // a branch: as selections in the common path they would double its instructions
       asm volatile("");
 #pragma unroll
