@@ -198,9 +198,21 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
     const int row = 32 * b + l31;
     const float ls = st[l31], rw = row_weight ? st[32 + l31] : 1.f;
     const bool ok = row < n_rows && ls != -INFINITY && rw != 0.f;  // others have no part, whatever they hold
-    shift = ok ? ls * 1.4426950408889634f : 0.f;
-    weight = ok ? rw : 0.f;
-    if (tree) {  // a branch: as selections in the common path they would double its instructions
+    // A lse of NaN, or a weight that is not finite, would reach the keys that the row does not see: those come by scores of -inf, which
+    // only make 0 of numbers.  So what the row gives to the keys that it sees goes into its scores.
+    const bool odd = ok && (ls != ls || !(fabsf(rw) < INFINITY));
+    shift = ok && !odd ? ls * 1.4426950408889634f : 0.f;
+    weight = !ok ? 0.f : odd ? copysignf(1.f, rw) : rw;
+    if (__builtin_expect(__ballot(!ok || odd) != 0, 0)) {
+      asm volatile("");  // a branch: as selections in the common path they would double its instructions
+      const bool infinite = ls == ls && rw == rw;  // an infinity, but for scores of -inf (0 times it) and NaN
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          sc[kb][i] = !ok ? -INFINITY : !odd ? sc[kb][i] : infinite && sc[kb][i] > -INFINITY ? INFINITY : NAN;
+    }
+    if (tree) {  // likewise
       asm volatile("");
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
@@ -211,13 +223,6 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
         for (int i = 0; i < 16; ++i)
           if (!((v >> acc_row(i, 0)) & 1u)) sc[kb][i] = -INFINITY;
       }
-    }
-    if (__builtin_expect(__ballot(!ok) != 0, 0)) {  // rows without a part: also none of their NaN
-      asm volatile("");
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[kb][i] = ok ? sc[kb][i] : -INFINITY;
     }
   };
   constexpr std::true_type yes{};
