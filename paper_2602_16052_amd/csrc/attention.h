@@ -18,7 +18,8 @@ struct KeyArgs {
   const uint32_t *tree_mask;
   int64_t q_stride, kv_stride, capacity;
   int n_seq, M, max_tree, words, max_len, H, Hk, G;
-  float c;  // scale * log2(e): scores in units of log 2
+  float c;         // scale * log2(e): scores in units of log 2
+  float u, u_rest;  // c / scale in two parts: an lse in the same units, with the rounding of c
 };
 
 // One sequence: first token row, rows of its tree, entries of its cache.  Device data, clamped to what the buffers hold.

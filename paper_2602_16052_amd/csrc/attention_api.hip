@@ -1,4 +1,5 @@
 // C ABI of the calls around a verification step's attention: argument checks on the host, before any launch.
+#include <float.h>
 #include <math.h>
 
 #include "attention.h"
@@ -78,6 +79,9 @@ KeyArgs key_args(const moespec_attn_desc &ds, const moespec_tree &t, const void 
   a.Hk = ds.n_kv_heads;
   a.G = ds.n_heads / ds.n_kv_heads;
   a.c = (float)((double)ds.scale * 1.4426950408889634);
+  const double u = a.c >= FLT_MIN ? (double)a.c / ds.scale : 1.4426950408889634;  // (a c without all of its bits says nothing)
+  a.u = (float)u;
+  a.u_rest = (float)(u - a.u);
   return a;
 }
 

@@ -1,4 +1,4 @@
-// The attention weight that every key received: w_j = sum over rows of row_weight 2^(c q.K_j - lse / ln 2).
+// The attention weight that every key received: w_j = sum over rows of row_weight 2^(c q.K_j - lse / ln 2), the exponent rounded once.
 //
 // The softmax statistics of the rows are known (lse), so a column sum needs nothing from other keys: a wave holds its 32 KB keys
 // as matrix operands in registers and walks over the rows, whose tiles of 32 lie in LDS, one ahead.  S^T = K Q^T has a row of
@@ -201,8 +201,11 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
     // A lse of NaN, or a weight that is not finite, would reach the keys that the row does not see: those come by scores of -inf, which
     // only make 0 of numbers.  So what the row gives to the keys that it sees goes into its scores.
     const bool odd = ok && (ls != ls || !(fabsf(rw) < INFINITY));
-    shift = ok && !odd ? ls * 1.4426950408889634f : 0.f;
-    weight = !ok ? 0.f : odd ? copysignf(1.f, rw) : rw;
+    // The exponent c s - u lse is u (scale s - lse) whatever c was rounded to.  u lse is large where the exponent is small, and rounded
+    // to as many bits: what that loses is the same for all keys of the row, and goes into its weight (2^-rest to first order).
+    const float whole = ls * a.u, rest = fminf(fmaxf(fmaf(ls, a.u_rest, fmaf(ls, a.u, -whole)), -0.5f), 0.5f);
+    shift = ok && !odd ? whole : 0.f;
+    weight = !ok ? 0.f : odd ? copysignf(1.f, rw) : rw * fmaf(rest, -0.69314718055994531f, 1.f);
     if (__builtin_expect(__ballot(!ok || odd) != 0, 0)) {
       asm volatile("");  // a branch: as selections in the common path they would double its instructions
       const bool infinite = ls == ls && rw == rw;  // an infinity, but for scores of -inf (0 times it) and NaN

@@ -65,3 +65,27 @@ def test_a_row_with_an_lse_of_nan_reaches_its_own_sequence_and_heads():
     cache_w, tree_w = call(b, lse)
     assert torch.isnan(cache_w[0, 0, :70]).all() and torch.isfinite(cache_w[0, 1, :70]).all()
     assert torch.isfinite(cache_w[1, :, :50]).all() and torch.isfinite(tree_w[:, 1]).all() and torch.isfinite(tree_w[9:]).all()
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 192), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("level", [0.0, 50.0, -50.0])
+def test_weights_of_single_rows_are_as_exact_as_their_scores(dtype, D, level):
+    """One row per KV head, whose scores have no rounding of their own (one product of two short numbers): what is left is the
+    exponential's.  With x the exponent in units of log 2: its rounding and that of its factor, |x| half steps each (times ln 2), two
+    half steps of the exponential, one each of the row's weight, its correction and the product, and one for what is of second order."""
+    S, Hk, n, scale = 8, 16, 200, 0.3
+    g = torch.Generator(device="cuda").manual_seed(D)
+    near = (level / scale / 16 + torch.rand((S, Hk, n), generator=g, device="cuda")).bfloat16()  # scores within some 5 of each other
+    q, kt, kc = (torch.zeros(s, dtype=TORCH[dtype], device="cuda") for s in ((S, Hk, D), (S, Hk, D), (S, Hk, n, D)))
+    q[..., 0], kc[..., 0] = 16.0, near.to(TORCH[dtype])
+    score = float(np.float32(scale)) * 16.0 * f64(near)
+    lse = torch.from_numpy(score.max(axis=2) + 0.37).float().cuda()
+    rw = torch.rand(S, generator=g, device="cuda") + 0.5
+    desc = mb.AttnDesc(Hk, Hk, D, n, CODE[dtype], scale)
+    cache_w, _ = mb.moespec_cache_weights(desc, q, kt, kc, i32([n] * S), lse, tree_off=i32(np.arange(S + 1)), max_tree=1, row_weight=rw)
+    d = score - f64(lse)[:, :, None]
+    want = f64(rw)[:, None, None] * np.exp(d)
+    x = np.abs(d) / np.log(2.0)
+    assert x.max() < 9
+    err = np.abs(f64(cache_w) - want) / want / 2.0 ** -24
+    assert np.all(err <= 2 * np.log(2.0) * x + 6), np.max(err / (2 * np.log(2.0) * x + 6))
