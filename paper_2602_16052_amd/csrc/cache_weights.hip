@@ -9,6 +9,7 @@
 // cores for 32%), which run beside the next tile's matrix instructions: 4 trees of 127 tokens x 8 heads, caches of up to 32749 entries,
 // 164 us (570 TFLOP/s; 193 us with the one behind the other).  For few rows the launch and one trip to memory: 63 tokens x 16
 // heads over 4093 entries 10 us for 17 MB of keys.
+#include <float.h>
 #include <math.h>
 
 #include "attention.h"
@@ -16,6 +17,7 @@
 namespace moespec {
 
 constexpr int kWeightWaves = 4;
+constexpr int kNanClass = 0x003, kZeroClass = 0x060, kInfinityClass = 0x204;  // of v_cmp_class
 
 template <typename T, int D>
 struct WeightShape {
@@ -197,31 +199,42 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
     const float *st = reinterpret_cast<const float *>(lds + buf * kStage + kTile + wave * 512);
     const int row = 32 * b + l31;
     const float ls = st[l31], rw = row_weight ? st[32 + l31] : 1.f;
-    const bool ok = row < n_rows && ls != -INFINITY && rw != 0.f;  // others have no part, whatever they hold
-    // A lse of NaN, or a weight that is not finite, would reach the keys that the row does not see: those come by scores of -inf, which
-    // only make 0 of numbers.  So what the row gives to the keys that it sees goes into its scores.
-    const bool odd = ok && (ls != ls || !(fabsf(rw) < INFINITY));
     // The exponent c s - u lse is u (scale s - lse) whatever c was rounded to.  u lse is large where the exponent is small, and rounded
     // to as many bits: what that loses is the same for all keys of the row, and goes into its weight (2^-rest to first order).
-    const float whole = ls * a.u, rest = fminf(fmaxf(fmaf(ls, a.u_rest, fmaf(ls, a.u, -whole)), -0.5f), 0.5f);
-    shift = ok && !odd ? whole : 0.f;
-    weight = !ok ? 0.f : odd ? copysignf(1.f, rw) : rw * fmaf(rest, -0.69314718055994531f, 1.f);
-    if (__builtin_expect(__ballot(!ok || odd) != 0, 0)) {
+    shift = ls * a.u;
+    const float rest = fmaf(ls, a.u_rest, fmaf(ls, a.u, -shift));
+    weight = rw * fmaf(rest, -0.69314718055994531f, 1.f);
+    // few rows are none of the common ones: past the end, of weight 0, not finite (or so large that rest is not small)
+    const bool common = row < n_rows && fabsf(ls) < 0x1p20f && !__builtin_amdgcn_classf(rw, kNanClass | kInfinityClass | kZeroClass);
+    if (__builtin_expect(__ballot(!common) != 0, 0)) {
       asm volatile("");  // a branch: as selections in the common path they would double its instructions
-      const bool infinite = ls == ls && rw == rw;  // an infinity, but for scores of -inf (0 times it) and NaN
+      const bool ok = row < n_rows && ls != -INFINITY && rw != 0.f;  // others have no part, whatever they hold
+      shift = common ? shift : ok ? fmaxf(shift, -FLT_MAX) : 0.f;
+      weight = common ? weight : !ok ? 0.f : ls != ls ? NAN : rw;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          sc[kb][i] = !ok ? -INFINITY : !odd ? sc[kb][i] : infinite && sc[kb][i] > -INFINITY ? INFINITY : NAN;
+        for (int i = 0; i < 16; ++i) sc[kb][i] = ok ? sc[kb][i] : -INFINITY;
     }
     if (tree) {  // likewise
       asm volatile("");
+      // A lse of NaN, or a weight that is not finite, would reach the keys that the row does not see: those come by scores of -inf,
+      // which only make 0 of numbers.  So what the row gives to the keys that it sees goes into its scores.
+      const bool odd = !(fabsf(weight) < INFINITY);
+      if (__builtin_expect(__ballot(odd) != 0, 0)) {
+        const bool infinite = weight == weight;  // an infinity, but for scores of -inf (0 times it) and NaN
+        shift = odd ? 0.f : shift;
+        weight = odd ? copysignf(1.f, weight) : weight;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[kb][i] = !odd ? sc[kb][i] : infinite && sc[kb][i] > -INFINITY ? INFINITY : NAN;
+      }
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         const int from = base + (wave * KB + kb) * 32;
         uint32_t v = masks ? reinterpret_cast<const uint32_t *>(st)[64 + 32 * kb + l31] : keys_below(row / a.G + 1 - from);
-        v = (ok ? v & keys_below(g.T - from) : 0u) >> (4 * half);
+        v = (v & keys_below(g.T - from)) >> (4 * half);
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (!((v >> acc_row(i, 0)) & 1u)) sc[kb][i] = -INFINITY;
