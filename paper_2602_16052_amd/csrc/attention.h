@@ -185,14 +185,18 @@ __device__ __forceinline__ void finish_row(const KeyArgs &a, const f32x16 (&o)[D
                                            int index, int t, int h, size_t orow, int half, T *out, float *lse, float *part,
                                            float2 *part_ml) {
   if (slots == 0) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const bool none = l == 0.f;  // no key, or scores of -inf alone: 0, also where weights of 0 have met a value that is not finite
+    const float inv = 1.f / l;
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        Elem<T>::store4(out + orow * D + 32 * b + acc_row(i, half),
-                        f32x4{o[b][i] * inv, o[b][i + 1] * inv, o[b][i + 2] * inv, o[b][i + 3] * inv});
-    if (lse && half == 0) lse[orow] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
+      for (int i = 0; i < 16; i += 4) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : o[b][i + e] * inv;
+        Elem<T>::store4(out + orow * D + 32 * b + acc_row(i, half), v);
+      }
+    if (lse && half == 0) lse[orow] = none ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
   } else {
     const size_t at = (size_t)index * a.max_tree * a.H + (size_t)t * a.H + h;
     if (half == 0) part_ml[at] = make_float2(m, l);

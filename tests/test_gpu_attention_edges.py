@@ -39,3 +39,23 @@ def check_odd_ends(b):
 @pytest.mark.parametrize("kind", ["tree", "chain"])
 def test_values_that_are_not_finite_in_last_places(dtype, H, Hk, D, trees, lens, kind):
     check_odd_ends(Batch(dtype, H, Hk, D, trees, lens, kind=kind, fused=True, room=0, seed=D + H))
+
+
+# in one part per sequence, and (caches) in several
+@pytest.mark.parametrize("dtype,H,Hk,D,T,n", [("bf16", 2, 2, 64, 9, 0), ("bf16", 2, 2, 96, 70, 0), ("f32", 4, 2, 128, 9, 0),
+                                              ("bf16", 256, 256, 64, 9, 300), ("f32", 256, 256, 64, 9, 90), ("bf16", 2, 2, 64, 3, 40), ("bf16", 8, 2, 128, 9, 700), ("bf16", 8, 1, 64, 40, 300),
+                                              ("bf16", 4, 1, 192, 30, 130), ("f32", 4, 2, 64, 9, 90), ("f32", 8, 1, 96, 20, 200)])
+def test_rows_whose_every_score_is_minus_infinity_are_zero(dtype, H, Hk, D, T, n):
+    """The sequence's keys are -inf and its queries positive; values of infinity and NaN times weights of 0.  Another sequence is as ever."""
+    b = Batch(dtype, H, Hk, D, [T, T], [n, n], kind="chain", seed=n)
+    b.q[:T] = b.q[:T].abs() + 0.5
+    want = oracle_64(b)
+    b.kt[:T], b.kc[0, :, :n] = -float("inf"), -float("inf")
+    b.vt[0], b.vt[1, :, 5] = float("inf"), float("nan")
+    if n:
+        b.vc[0, :, n // 2], b.vc[0, :, n - 1, 3] = float("nan"), -float("inf")
+    out, lse = b.attention()
+    assert torch.all(out[:T] == 0) and torch.all(torch.isneginf(lse[:T]))
+    for w, empty in zip(want, (0.0, -np.inf, 0.0, 0.0)):
+        w[:T] = empty
+    b.check(out, lse, want)
