@@ -352,6 +352,8 @@ moespec_status moespec_stream_read(const void *buf, size_t bytes, uint32_t *chec
  *   Device data  Lengths, offsets and paths are device data and not checked on the host.  The kernels clamp them to what the
  *             buffers hold (offsets to [0, n_tokens], a tree to max_tree rows, a length to max_len, or to capacity), so
  *             that no value leads to an access outside of a buffer.
+ *   Outputs   and the workspace overlap nothing else that the call uses, unless a call below says so: an overlap, also in part, is
+ *             MOESPEC_ERR_INVALID_ARG.  (Strided rows count from the first to the end of the last one.)
  *   Sums      are in fp32, in an order that depends on the arguments and the device data above alone.
  *   Sizes     A launch that would need 2^32 threads or more is MOESPEC_ERR_UNSUPPORTED_SHAPE, as are strides above 2^20.
  */

@@ -2,6 +2,8 @@
 #include <float.h>
 #include <math.h>
 
+#include <initializer_list>
+
 #include "attention.h"
 
 using namespace moespec;
@@ -16,6 +18,11 @@ constexpr int64_t kMaxThreads = (1ll << 32) - 1024;  // threads of a launch
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 moespec_status from_hip(hipError_t e) { return e == hipSuccess ? MOESPEC_OK : MOESPEC_ERR_HIP; }
+
+double elem_bytes(const moespec_attn_desc &ds) { return ds.dtype == MOESPEC_BF16 ? 2 : 4; }
+double cache_entries(const moespec_attn_desc &ds, double layers, double n_seq) {
+  return layers * n_seq * ds.n_kv_heads * ds.capacity;
+}
 
 moespec_status check_desc(const moespec_attn_desc *ds) {
   if (!ds) return MOESPEC_ERR_INVALID_ARG;
@@ -55,6 +62,28 @@ moespec_status check_ws(const void *ws, size_t have, size_t need) {
   if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return MOESPEC_ERR_INVALID_ARG;
   return have < need ? MOESPEC_ERR_WORKSPACE_TOO_SMALL : MOESPEC_OK;
 }
+
+// Bytes of a call's buffer (none where p is NULL).  In floating point: a size may be beyond 64 bits, and is exact up to 2^53.
+struct Span {
+  const void *p;
+  double bytes;
+};
+bool overlap(const Span &a, const Span &b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && (x <= y ? (double)(y - x) < a.bytes : (double)(x - y) < b.bytes);
+}
+// Whether what a call writes lies apart from everything else that it uses.  Workgroups run in any order, so a result in the place of
+// something that another one still reads would be a wrong one.
+bool apart(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+  for (const Span *w = written.begin(); w != written.end(); ++w) {
+    for (const Span *v = written.begin(); v != w; ++v)
+      if (overlap(*v, *w)) return false;
+    for (const Span &r : read)
+      if (overlap(*w, r)) return false;
+  }
+  return true;
+}
+double rows_bytes(double n, double stride, double row, double es) { return ((n - 1) * stride + row) * es; }
 
 KeyArgs key_args(const moespec_attn_desc &ds, const moespec_tree &t, const void *q, const void *k_tree, const void *v_tree,
                  const void *k_cache, const void *v_cache, const int32_t *cache_len, int32_t max_len) {
@@ -113,12 +142,20 @@ moespec_status moespec_tree_attention(const moespec_attn_desc *desc, const moesp
     return MOESPEC_ERR_INVALID_ARG;
   if (max_len > 0 && (!k_cache || !v_cache || !cache_len || !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(cache_len)))
     return MOESPEC_ERR_INVALID_ARG;
-  if ((s = check_ws(ws, ws_bytes, attn_ws(*desc, tree->n_seq, tree->max_tree, max_len))) != MOESPEC_OK) return s;
+  const size_t need = attn_ws(*desc, tree->n_seq, tree->max_tree, max_len);
+  if ((s = check_ws(ws, ws_bytes, need)) != MOESPEC_OK) return s;
   // workgroups of 256 threads: row tiles of 128 rows or more above 64 rows, parts only where there are few, up to seven more groups
   const int64_t rows = (int64_t)tree->max_tree * (desc->n_heads / desc->n_kv_heads), tiles = rows <= 64 ? 1 : (rows + 127) / 128;
   if ((((int64_t)tree->n_seq * desc->n_kv_heads + 7) * tiles + 1024) * 256 > kMaxThreads) return MOESPEC_ERR_UNSUPPORTED_SHAPE;
-  return from_hip(launch_tree_attention(*desc, key_args(*desc, *tree, q, k_tree, v_tree, k_cache, v_cache, cache_len, max_len),
-                                        out, lse, ws, static_cast<hipStream_t>(hip_stream)));
+  const KeyArgs a = key_args(*desc, *tree, q, k_tree, v_tree, k_cache, v_cache, cache_len, max_len);
+  const double M = a.M, es = elem_bytes(*desc), kv = rows_bytes(M, a.kv_stride, (double)a.Hk * desc->head_dim, es);
+  const double cache = max_len > 0 ? cache_entries(*desc, 1, a.n_seq) * desc->head_dim * es : 0.;
+  if (!apart({{out, M * a.H * desc->head_dim * es}, {lse, 4. * M * a.H}, {ws, (double)need}},
+             {{q, rows_bytes(M, a.q_stride, (double)a.H * desc->head_dim, es)}, {k_tree, kv}, {v_tree, kv}, {k_cache, cache},
+              {v_cache, cache}, {cache_len, max_len > 0 ? 4. * a.n_seq : 0.}, {a.tree_off, 4. * (a.n_seq + 1.)},
+              {a.tree_mask, 4. * M * a.words}}))
+    return MOESPEC_ERR_INVALID_ARG;
+  return from_hip(launch_tree_attention(*desc, a, out, lse, ws, static_cast<hipStream_t>(hip_stream)));
 }
 
 moespec_status moespec_cache_weights(const moespec_attn_desc *desc, const moespec_tree *tree, const void *q,
@@ -133,11 +170,20 @@ moespec_status moespec_cache_weights(const moespec_attn_desc *desc, const moespe
   if (max_len > 0 &&
       (!k_cache || !cache_len || !cache_w_out || !aligned16(k_cache) || !aligned4(cache_len) || !aligned4(cache_w_out)))
     return MOESPEC_ERR_INVALID_ARG;
-  if ((s = check_ws(ws, ws_bytes, attn_ws(*desc, tree->n_seq, tree->max_tree, max_len))) != MOESPEC_OK) return s;
+  const size_t need = attn_ws(*desc, tree->n_seq, tree->max_tree, max_len);
+  if ((s = check_ws(ws, ws_bytes, need)) != MOESPEC_OK) return s;
   const int64_t tiles = ((int64_t)max_len + 127) / 128 + (tree->max_tree + 127) / 128;
   if ((int64_t)tree->n_seq * desc->n_kv_heads * tiles * 256 > kMaxThreads) return MOESPEC_ERR_UNSUPPORTED_SHAPE;
-  return from_hip(launch_cache_weights(*desc, key_args(*desc, *tree, q, k_tree, nullptr, k_cache, nullptr, cache_len, max_len),
-                                       lse, row_weight, decay, cache_w_in, cache_w_out, tree_w, ws,
+  const KeyArgs a = key_args(*desc, *tree, q, k_tree, nullptr, k_cache, nullptr, cache_len, max_len);
+  const double M = a.M, es = elem_bytes(*desc), entries = max_len > 0 ? cache_entries(*desc, 1, a.n_seq) : 0.;
+  if (!apart({{cache_w_out, 4. * entries}, {tree_w, 4. * M * a.Hk}, {ws, (double)need}},
+             {{q, rows_bytes(M, a.q_stride, (double)a.H * desc->head_dim, es)},
+              {k_tree, rows_bytes(M, a.kv_stride, (double)a.Hk * desc->head_dim, es)}, {k_cache, entries * desc->head_dim * es},
+              {cache_len, max_len > 0 ? 4. * a.n_seq : 0.}, {lse, 4. * M * a.H}, {row_weight, 4. * M},
+              {cache_w_in == cache_w_out ? nullptr : cache_w_in, 4. * entries}, {a.tree_off, 4. * (a.n_seq + 1.)},
+              {a.tree_mask, 4. * M * a.words}}))
+    return MOESPEC_ERR_INVALID_ARG;
+  return from_hip(launch_cache_weights(*desc, a, lse, row_weight, decay, cache_w_in, cache_w_out, tree_w, ws,
                                        static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -158,6 +204,13 @@ moespec_status moespec_cache_commit(const moespec_attn_desc *desc, int32_t n_lay
   const int64_t pieces = (int64_t)desc->head_dim * (desc->dtype == MOESPEC_BF16 ? 2 : 4) / 16;
   if ((double)n_layers * tree->n_seq * max_path * desc->n_kv_heads * pieces > (double)kMaxThreads)
     return MOESPEC_ERR_UNSUPPORTED_SHAPE;
+  const double es = elem_bytes(*desc), D = desc->head_dim, M = tree->n_tokens, n_seq = tree->n_seq, Hk = desc->n_kv_heads;
+  const double entries = cache_entries(*desc, n_layers, tree->n_seq);
+  const double kv = rows_bytes(n_layers * M, tree->kv_stride ? (double)tree->kv_stride : Hk * D, Hk * D, es);
+  if (!apart({{k_cache, entries * D * es}, {v_cache, entries * D * es}, {cache_w, 4. * entries}, {new_len, 4. * n_seq}},
+             {{k_tree, kv}, {v_tree, kv}, {tree_w, 4. * n_layers * M * Hk}, {path, 4. * n_seq * max_path}, {n_path, 4. * n_seq},
+              {cache_len, 4. * n_seq}, {tree->tree_off, 4. * (n_seq + 1.)}}))
+    return MOESPEC_ERR_INVALID_ARG;
   return from_hip(launch_cache_commit(*desc, n_layers, *tree, k_tree, v_tree, tree_w, path, n_path, max_path, k_cache, v_cache,
                                       cache_w, cache_len, new_len, static_cast<hipStream_t>(hip_stream)));
 }
@@ -188,6 +241,11 @@ moespec_status moespec_cache_evict(const moespec_attn_desc *desc, int32_t n_laye
   const int64_t heads = (int64_t)n_layers * n_seq * desc->n_kv_heads;
   if (heads * 1024 > kMaxThreads || (double)heads * (((double)budget * pieces) / 1024 + 1) * 256 > (double)kMaxThreads)
     return MOESPEC_ERR_UNSUPPORTED_SHAPE;
+  const double es = elem_bytes(*desc), D = desc->head_dim, in = cache_entries(*desc, n_layers, n_seq), out = (double)heads * out_capacity;
+  const Span list = {kept ? static_cast<void *>(kept) : ws, 4. * heads * budget};
+  if (!apart({{k_out, out * D * es}, {v_out, out * D * es}, {w_out, 4. * out}, list, {new_len, 4. * n_seq}},
+             {{k_cache, in * D * es}, {v_cache, in * D * es}, {cache_w, 4. * in}, {cache_len, 4. * n_seq}}))
+    return MOESPEC_ERR_INVALID_ARG;
   return from_hip(launch_cache_evict(*desc, n_layers, n_seq, k_cache, v_cache, cache_w, cache_len, budget, recent, out_capacity,
                                      k_out, v_out, w_out, kept ? kept : static_cast<int32_t *>(ws), new_len,
                                      static_cast<hipStream_t>(hip_stream)));
@@ -206,6 +264,15 @@ moespec_status moespec_block_norm(const moespec_desc *desc, const moespec_block 
     return MOESPEC_ERR_INVALID_ARG;
   if ((b.gate_kind == MOESPEC_BLOCK_GATE_NONE) != (b.gate == nullptr) || (b.w_post && !b.post_norm)) return MOESPEC_ERR_INVALID_ARG;
   if (!aligned16(b.gate) || !aligned16(b.w_post) || !aligned16(b.w_pre)) return MOESPEC_ERR_INVALID_ARG;
+  // a row is read before it is written: the same buffer is fine, another part of it is not
+  const double es = desc->dtype == MOESPEC_BF16 ? 2 : 4, rows = (double)M * desc->d * es, d = desc->d * es;
+  const bool element = b.gate_kind == MOESPEC_BLOCK_GATE_ELEMENT;
+  const double gate = element ? rows : b.gate_kind == MOESPEC_BLOCK_GATE_TOKEN ? M * es : d;
+  for (const void *o : {r, x})
+    if (!apart({{o, rows}}, {{y == o ? nullptr : y, rows}, {residual == o ? nullptr : residual, rows},
+                             {element && b.gate == o ? nullptr : b.gate, gate}, {b.w_post, d}, {b.w_pre, d},
+                             {o == r ? x : r, rows}}))
+      return MOESPEC_ERR_INVALID_ARG;
   return from_hip(launch_block_norm(*desc, b, y, residual, M, r, x, static_cast<hipStream_t>(hip_stream)));
 }
 

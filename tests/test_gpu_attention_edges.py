@@ -3,6 +3,8 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2602_16052_amd import binding as mb
+
 from attention_common import Batch, f64
 from test_gpu_attention import oracle_64
 
@@ -59,3 +61,29 @@ def test_rows_whose_every_score_is_minus_infinity_are_zero(dtype, H, Hk, D, T, n
     for w, empty in zip(want, (0.0, -np.inf, 0.0, 0.0)):
         w[:T] = empty
     b.check(out, lse, want)
+
+
+def test_buffers_side_by_side_are_apart():
+    """Everything a call uses in one allocation, each right behind the other; what is written lies between what is read."""
+    b = Batch("bf16", 4, 2, 64, [9, 6], [70, 33], seed=5)
+    want = b.attention()
+    n_ws = mb.attn_workspace_bytes(b.desc, 2, b.M, b.max_tree, b.max_len)
+    out, lse = torch.empty_like(want[0]), torch.empty_like(want[1])
+    tw, cw = torch.empty((b.M, 2), device="cuda"), torch.zeros((2, 2, b.desc.capacity), device="cuda")
+    parts = [torch.empty(n_ws, dtype=torch.uint8, device="cuda"), b.q, out, b.kt, lse, b.kc, cw, b.vt, tw, b.vc]
+    arena = torch.empty(sum(-(-t.numel() * t.element_size() // 16) * 16 for t in parts), dtype=torch.uint8, device="cuda")
+    at, inside = 0, []
+    for t in parts:
+        n = t.numel() * t.element_size()
+        v = arena[at:at + n].view(t.dtype).view(t.shape)
+        inside.append(v.copy_(t))
+        at += -(-n // 16) * 16
+    ws, b.q, out, b.kt, lse, b.kc, cw, b.vt, tw, b.vc = inside
+    b.attention(out=out, lse=lse, ws=ws)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    plain = mb.moespec_cache_weights(b.desc, b.q, b.kt, b.kc, b.cache_len, lse, **b.args)
+    mb.moespec_cache_weights(b.desc, b.q, b.kt, b.kc, b.cache_len, lse, ws=ws, cache_w=cw, tree_w=tw, **b.args)
+    assert torch.equal(cw, plain[0]) and torch.equal(tw, plain[1])
+    # one projection's output holds q, k and v of every row; the results have a buffer of their own
+    with pytest.raises(mb.MoeSpecError):
+        b.attention(out=b.q, lse=lse, ws=ws)
