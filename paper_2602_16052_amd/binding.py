@@ -605,6 +605,8 @@ class _Call:
     def __init__(self, name: str, device: torch.device, args, keep, stream):
         self._fn, self._name, self._args, self._keep = getattr(load_library(), name), name, args, keep
         self._device, self._stream = device.index if device.index is not None else torch.cuda.current_device(), stream
+        if stream is not None and getattr(stream, "device_index", self._device) != self._device:
+            raise ValueError(f"stream must belong to cuda:{self._device}, got one of {stream.device}")
 
     def __call__(self):
         if torch.cuda.current_device() == self._device:
