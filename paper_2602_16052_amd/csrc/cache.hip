@@ -266,6 +266,7 @@ __global__ __launch_bounds__(kGatherThreads) void cache_gather_kernel(const uint
     src[u] = list[min(i, total - 1) / pieces];
     src[u] = i < total && src[u] < capacity ? src[u] : -1;  // (a list that somebody else wrote to meanwhile)
   }
+  if (list[0] < 0) return;  // no entry at all: nothing of this cache is read
 #pragma unroll
   for (int u = 0; u < 4; ++u) {  // places that stay empty load the first entry
     const int64_t at = in + (int64_t)max(src[u], 0) * pieces + (i0 + u * kGatherThreads) % pieces;
