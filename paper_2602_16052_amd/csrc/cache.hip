@@ -246,7 +246,8 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(const floa
     select_entries<0>(w, n, want, hist, wave_sum, wave_eq, found, w_out, kept);
 }
 
-// The rows of the kept entries copied: kRowsPerGroup of them per workgroup, every thread with four loads of each cache in flight.
+// The rows of the kept entries copied: a workgroup takes 4 kGatherThreads pieces of 16 bytes of each cache, whole rows or not, every
+// thread four of each, whose loads are in flight together.
 constexpr int kGatherThreads = 256;
 __global__ __launch_bounds__(kGatherThreads) void cache_gather_kernel(const uint4 *__restrict__ k_in,
                                                                       const uint4 *__restrict__ v_in,

@@ -1,7 +1,7 @@
 // The attention weight that every key received: w_j = sum over rows of row_weight 2^(c q.K_j - lse / ln 2), the exponent rounded once.
 //
 // The softmax statistics of the rows are known (lse), so a column sum needs nothing from other keys: a wave holds its 32 KB keys
-// as matrix operands in registers and walks over the rows, whose tiles of 32 lie in LDS, one ahead.  S^T = K Q^T has a row of
+// as matrix operands in registers and walks over the rows, whose tiles of 32 come through a ring of four places in LDS.  S^T = K Q^T has a row of
 // queries per lane, and the weights of a key add up in one register per lane; the 32 lanes are summed once at the end.  A
 // workgroup is the only writer of its keys, or of its part of the rows, which a second launch adds up in order.
 //
@@ -139,7 +139,8 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
     if (b0 + i < b1) issue(i);
 #pragma unroll
   for (int i = 0; i < KB * NS; ++i) arrived(k[i / NS][i % NS]);
-  // tile b is there, and the place of the one two before it is free
+  // Tile b is there (the first time also the one behind it: four have been fetched, two may be on their way), and every wave has read all
+  // of tile b - 1, whose place is filled next.
   auto tile_there = [&](int b) {
     const int later = min(b1 - 1 - b, 2);
     if (later <= 0) wait_vm<0>();
@@ -205,10 +206,12 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void cache_weights_kernel(
     const float rest = fmaf(ls, a.u_rest, fmaf(ls, a.u, -shift));
     weight = rw * fmaf(rest, -0.69314718055994531f, 1.f);
     // few rows are none of the common ones: past the end, of weight 0, not finite (or so large that rest is not small)
-    const bool common = row < n_rows && fabsf(ls) < 0x1p20f && !__builtin_amdgcn_classf(rw, kNanClass | kInfinityClass | kZeroClass);
-    if (__builtin_expect(__ballot(!common) != 0, 0)) {
+    const bool past = row >= n_rows, far = !(fabsf(ls) < 0x1p20f);
+    const bool special = __builtin_amdgcn_classf(rw, kNanClass | kInfinityClass | kZeroClass);
+    if (__builtin_expect((__ballot(past) | __ballot(far) | __ballot(special)) != 0, 0)) {
       asm volatile("");  // a branch: as selections in the common path they would double its instructions
-      const bool ok = row < n_rows && ls != -INFINITY && rw != 0.f;  // others have no part, whatever they hold
+      const bool common = !past && !far && !special;
+      const bool ok = !past && ls != -INFINITY && rw != 0.f;  // others have no part, whatever they hold
       shift = common ? shift : ok ? fmaxf(shift, -FLT_MAX) : 0.f;
       weight = common ? weight : !ok ? 0.f : ls != ls ? NAN : rw;
 #pragma unroll
