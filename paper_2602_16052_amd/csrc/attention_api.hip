@@ -63,14 +63,15 @@ moespec_status check_ws(const void *ws, size_t have, size_t need) {
   return have < need ? MOESPEC_ERR_WORKSPACE_TOO_SMALL : MOESPEC_OK;
 }
 
-// Bytes of a call's buffer (none where p is NULL).  In floating point: a size may be beyond 64 bits, and is exact up to 2^53.
+// Bytes of a call's buffer (none where p is NULL, 0 where the call does not touch it).  In floating point: a size may be beyond 64 bits, and is exact up to 2^53.
 struct Span {
   const void *p;
   double bytes;
 };
 bool overlap(const Span &a, const Span &b) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-  return a.p && b.p && (x <= y ? (double)(y - x) < a.bytes : (double)(x - y) < b.bytes);
+  if (!a.p || !b.p || !(a.bytes > 0.) || !(b.bytes > 0.)) return false;
+  return x <= y ? (double)(y - x) < a.bytes : (double)(x - y) < b.bytes;
 }
 // Whether what a call writes lies apart from everything else that it uses.  Workgroups run in any order, so a result in the place of
 // something that another one still reads would be a wrong one.

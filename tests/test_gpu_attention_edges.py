@@ -87,3 +87,13 @@ def test_buffers_side_by_side_are_apart():
     # one projection's output holds q, k and v of every row; the results have a buffer of their own
     with pytest.raises(mb.MoeSpecError):
         b.attention(out=b.q, lse=lse, ws=ws)
+
+
+def test_a_cache_that_is_not_used_may_lie_anywhere():
+    b = Batch("bf16", 1, 1, 64, [12], [0], kind="chain", seed=6, room=11)
+    assert b.desc.capacity == 12
+    want = b.attention()
+    out = torch.empty_like(want[0])
+    place = out.view(1, 1, 12, 64)
+    mb.moespec_tree_attention(b.desc, b.q, b.kt, b.vt, place, place, b.cache_len, out=out, **{**b.args, "max_len": 0})
+    assert torch.equal(out, want[0])
