@@ -10,9 +10,9 @@
 // order of keys (bf16: transposing reads).
 // Keys and values go from memory straight into LDS, one stage ahead of the products.
 //
-// What bounds it: few rows, the stream of keys and values (16 trees of up to 31 tokens x 4 heads, caches of up to 16381 entries: 175 us, 4.7
-// TB/s, what a large copy reaches; one token over 65521 entries 30 us, 4.4 TB/s); short caches, launches and trips to memory
-// (one token over 1021 entries 9.2 us in two launches, of which the kernels are 5.5 and 3.8).
+// What bounds it: few rows, the stream of keys and values (16 trees of up to 31 tokens x 4 heads, caches of up to 16381 entries: 175 to
+// 182 us, 4.6 to 4.7 TB/s, what a large copy reaches; one token over 65521 entries 30 us, 4.4 TB/s); short caches, launches and trips
+// to memory (one token over 1021 entries 9.2 us in two launches, of which the kernels are 5.4 and 3.5 to 4.1).
 // Key waves side by side share one stage: for up to 64 rows, workgroups of a stage of 32 keys each with nothing to join took 24.4
 // us where these take 19.6 (63 rows x 16 heads, 4093 entries; 72 against 63 with 32768), but win where all keys make one round of
 // them (one token over 1021 entries 9.5 us against 11.2).  A third stage ahead, issued behind a second barrier, was slower (25.4 us).
@@ -417,10 +417,11 @@ __global__ __launch_bounds__(64 * WR * WK, (D <= 128 ? 2 : 1)) void tree_attenti
 // S(i), those of O += V^T P(i) beside the rest of them and beside the maxima of S(i + 1).  Keys and values of the tiles come
 // through two places each, K one tile ahead of V; one barrier per tile.
 // Tiles that some row sees in part (the cache's last one, those of the tree) follow one by one.
-// 511-token tree x 8 heads over 65521 entries: 510 to 550 us (1000 to 1070 TFLOP/s; a library product of 8192^3 reaches 1210 here),
-// against 690 us in the form above.  The matrix cores are busy for 46% of the cycles, at 2.0 GHz under this load; what else there is,
-// exponentials first, fills the rest of one wave's issue slots.  Heads of 192 and 256 have 32 rows a wave (their O and Q fill the
-// accumulation registers): 8 trees of 63 over 8192 entries, heads of 256, 176 us (768 TFLOP/s) against 250.
+// 511-token tree x 8 heads over 65521 entries: 510 to 560 us (980 to 1070 TFLOP/s; a library product of 8192^3 reaches 1210 here),
+// against 690 us in the form above.  The matrix cores are busy for 46% of the cycles, at 2.0 GHz under this load, and idle for the rest:
+// one wave a SIMD issues its instructions one by one, 5.6 of the vector ALU to a matrix instruction (counters).  Heads of 192 and
+// 256 have 32 rows a wave (their O and Q fill the accumulation registers): 8 trees of 63 over 8192 entries, heads of 256, 176 us (768
+// TFLOP/s) against 250.
 template <int D>
 struct WideShape {
   static constexpr int RB = D <= 128 ? 2 : 1;  // blocks of 32 rows of a wave

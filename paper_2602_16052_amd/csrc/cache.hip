@@ -1,7 +1,7 @@
 // Writing to a cache of keys and values: the accepted path appended, and a cache cut to its budget.
 // Both are bound by memory traffic (and, for few entries, by the launch): every 16 bytes of a kept row are read and written once.
-// Commit of 8 tokens for 48 layers x 8 sequences x 4 heads: 5 us.  Eviction, 16 heads 4093 -> 2048 entries: 14 us, selection 7.5 and
-// copy 5.8 (5.8 TB/s); 128 heads 32749 -> 4096: 133 us, 27 and 106 (5.1 TB/s).  Selection is bound by the LDS atomics of the first
+// Commit of 8 tokens for 48 layers x 8 sequences x 4 heads: 5 us.  Eviction, 16 heads 4093 -> 2048 entries: 14 us, selection 7.8 and
+// copy 7.2 (4.7 TB/s); 128 heads 32749 -> 4096: 133 us, 27 and 107 (5.0 TB/s).  Selection is bound by the LDS atomics of the first
 // histogram and by barriers; it reads 4 bytes an entry where the copy moves 4 D.
 #include "attention.h"
 

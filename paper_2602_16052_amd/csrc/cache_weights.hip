@@ -1,14 +1,14 @@
-// The attention weight that every key received: w_j = sum over rows of row_weight 2^(c q.K_j - lse / ln 2), the exponent rounded once.
+// The attention weight that every key received: w_j = sum over rows of row_weight 2^(c q.K_j - lse / ln 2).
 //
 // The softmax statistics of the rows are known (lse), so a column sum needs nothing from other keys: a wave holds its 32 KB keys
-// as matrix operands in registers and walks over the rows, whose tiles of 32 come through a ring of four places in LDS.  S^T = K Q^T has a row of
-// queries per lane, and the weights of a key add up in one register per lane; the 32 lanes are summed once at the end.  A
+// as matrix operands in registers and walks over the rows, whose tiles of 32 come through a ring of four places in LDS.  S^T = K Q^T has
+// a row of queries per lane, and the weights of a key add up in one register per lane; the 32 lanes are summed once at the end.  A
 // workgroup is the only writer of its keys, or of its part of the rows, which a second launch adds up in order.
 //
-// What bounds it: for many rows the exponentials and the two multiply-adds per score (VALU busy for 57% of the cycles, the matrix
-// cores for 32%), which run beside the next tile's matrix instructions: 4 trees of 127 tokens x 8 heads, caches of up to 32749 entries,
-// 164 us (570 TFLOP/s; 193 us with the one behind the other).  For few rows the launch and one trip to memory: 63 tokens x 16
-// heads over 4093 entries 10 us for 17 MB of keys.
+// What bounds it: for many rows the exponentials and the two multiply-adds per score, which run beside the next tile's matrix
+// instructions: 4 trees of 127 tokens x 8 heads, caches of 32749 down to 20469 entries, 167 to 175 us (530 to 555 TFLOP/s; 193 us with
+// the one behind the other).  Over 32749 entries each the VALU is busy for 56% of the cycles, the matrix cores for 32%.  For few rows
+// the launch and one trip to memory: 63 tokens x 16 heads over 4093 entries 10 us for 17 MB of keys.
 #include <float.h>
 #include <math.h>
 
