@@ -18,7 +18,9 @@
  * the Oracle ranking of Eq. (6) (moespec_oracle_ranking, an upper bound for analysis) and two analysis
  * quantities of Section 4 (moespec_coverage_curve, moespec_reconstruction_error).  The other half of a verification
  * step - attention of the tree over a cache of keys and values, the cache's upkeep, the norm between two blocks - is at
- * the end: moespec_tree_attention, moespec_cache_weights, moespec_cache_commit, moespec_cache_evict, moespec_block_norm.
+ * the end: moespec_tree_attention, moespec_cache_weights, moespec_cache_commit, moespec_cache_evict, moespec_block_norm; and what
+ * lies around both in a serving step: moespec_head_rope, moespec_paged_write, moespec_paged_read, moespec_paged_attention,
+ * moespec_draft_verify.
  *
  * Conventions (all calls)
  *   Pointers  Every buffer pointer is a DEVICE pointer unless it is a descriptor struct
@@ -494,6 +496,149 @@ typedef struct {
  */
 moespec_status moespec_block_norm(const moespec_desc *desc, const moespec_block *block, const void *y, const void *residual,
                                   int32_t M, void *r, void *x, void *hip_stream);
+
+/*
+ * ---- Around both halves: queries and keys made ready, a paged cache, single tokens over it, the draft's verification ----
+ *
+ * moespec_head_rope makes queries and keys ready for attention.  moespec_paged_write keeps keys and values in pages of a pool that
+ * all sequences share, as they are or in 8 bits; moespec_paged_attention attends from one new token of every sequence over its pages
+ * (a step without a draft), moespec_paged_read lays entries out as the contiguous cache that moespec_tree_attention reads.
+ * moespec_draft_verify turns the target's logits into the accepted path, which moespec_cache_commit and moespec_paged_write take, and
+ * the next token.  The conventions above hold, those of the tree calls among them.
+ */
+
+/* Norm and rotation of queries and keys.  Host struct holding device pointers. */
+typedef struct {
+  int32_t rot_dim;          /* elements of a head that are rotated, the first ones: 0 or a multiple of 16 up to D          */
+  int32_t interleaved;      /* 1: pairs (2i, 2i + 1), 0: pairs (i, i + rot_dim / 2)                                         */
+  int32_t norm;             /* 1: every head is scaled to unit root-mean-square first                                       */
+  float eps;                /* added to the mean square, >= 0; only with norm                                               */
+  const void *w_q, *w_k;    /* [D] dtype or NULL (1); only with norm                                                        */
+  const float *freq;        /* [rot_dim / 2] angle of a pair per place; NULL if rot_dim is 0                                */
+  const int32_t *positions; /* [M] place of every token, or NULL: cache_len[s] + the tokens of its tree that it sees, less 1 */
+  const int32_t *cache_len; /* [n_seq] or NULL (0); only without positions                                                  */
+  int64_t q_out_stride;     /* elements from a token's row of q_out to the next one's; 0: H * D                             */
+  int64_t k_out_stride;     /* the same for k_out; 0: Hk * D                                                                */
+} moespec_rope;
+
+/*
+ * Queries and keys of every token normed for each head and rotated to the token's place:
+ *   z = norm ? w x / sqrt(mean x^2 + eps) : x,   (z_a, z_b) <- (z_a cos - z_b sin, z_b cos + z_a sin),  angle = place freq[i].
+ *   q  [M, H, D] dtype in    rows tree.q_stride apart; NULL (with q_out): keys only
+ *   k  [M, Hk, D] dtype in   rows tree.kv_stride apart; NULL (with k_out): queries only
+ *   q_out, k_out  out        each may be its own input with the same stride (in place, also inside of a longer row that holds q, k
+ *                            and v), and overlaps nothing else
+ * Rows of no sequence, and those past max_tree, are neither read nor written.  Angles are taken in 64 bits and reduced to a turn
+ * before sine and cosine, everything else in fp32 with one rounding at the end.  tree.tree_mask is read without positions only.
+ */
+moespec_status moespec_head_rope(const moespec_attn_desc *desc, const moespec_rope *rope, const moespec_tree *tree, const void *q,
+                                 const void *k, void *q_out, void *k_out, void *hip_stream);
+
+/* How a page holds keys and values. */
+typedef enum {
+  MOESPEC_CACHE_PLAIN = 0, /* dtype of the layer                                                             */
+  MOESPEC_CACHE_I8 = 1,    /* 8-bit integers: x = code * scale                                               */
+  MOESPEC_CACHE_E4M3 = 2   /* 8-bit floats (4 bits of exponent, 3 of mantissa, no infinities): x = code * scale */
+} moespec_cache_code;
+
+/* Keys and values in pages.  Host struct holding device pointers. */
+typedef struct {
+  int32_t code;              /* moespec_cache_code                                                              */
+  int32_t n_pages;           /* pages of the pool                                                               */
+  int32_t page_size;         /* entries of a page: 16, 32, 64, 128 or 256                                       */
+  int32_t max_pages;         /* places of a sequence in the table; max_pages * page_size <= 2^31 - 2^16 entries */
+  void *k_pages, *v_pages;   /* [n_layers, n_pages, Hk, page_size, D] dtype or codes                            */
+  float *k_scale, *v_scale;  /* [n_layers, n_pages, Hk, page_size] with codes, else NULL                        */
+  const int32_t *page_table; /* [n_seq, max_pages]: entry e of a sequence lies in page table[e / page_size]     */
+} moespec_paged_cache;
+
+/*
+ * Appends the accepted path of every sequence, or its whole tree, to the pages of n_layers layers, which share lengths, paths and
+ * table: entry cache_len[s] + i takes token path[s, i] of the tree of s, for i < n_path[s].
+ *   k_tree, v_tree [n_layers, M, Hk, D] dtype in   rows kv_stride apart, layers M * kv_stride apart
+ *   path, n_path, max_path                          as for moespec_cache_commit; path and n_path NULL: all tokens of the tree in order
+ *   new_len  [n_seq] int32 out                      min(cache_len + n_path, max_pages * page_size); may be NULL
+ * A row's scale and codes, with amax its largest magnitude:
+ *   I8    scale = amax / 127, code = x * (127 / amax) to the nearest integer (ties to even; quotients in fp32, the product unrounded)
+ *   E4M3  scale = 2^e, the smallest with amax <= 448 * 2^e and e >= -126, code = x / scale to the nearest
+ * A row with a value that is not finite has the scale NaN and reads as NaN throughout.  Entries whose page is outside of the pool are
+ * dropped.  No two entries that are written may lie in the same place (pages that sequences share hold entries in front of
+ * cache_len).  desc.capacity does not matter here.
+ */
+moespec_status moespec_paged_write(const moespec_attn_desc *desc, int32_t n_layers, const moespec_paged_cache *cache,
+                                   const moespec_tree *tree, const void *k_tree, const void *v_tree, const int32_t *path,
+                                   const int32_t *n_path, int32_t max_path, const int32_t *cache_len, int32_t *new_len,
+                                   void *hip_stream);
+
+/*
+ * Entries first[s] .. cache_len[s] - 1 of every sequence from the pages into a contiguous cache, to the same places.
+ *   first     [n_seq] int32 in   NULL: 0
+ *   cache_len [n_seq] int32 in;  max_len: no sequence has more entries, 0 .. desc.capacity and max_pages * page_size
+ *   k_cache, v_cache [n_layers, n_seq, Hk, capacity, D] dtype out   other entries are left alone
+ * Entries whose page is outside of the pool are 0.
+ */
+moespec_status moespec_paged_read(const moespec_attn_desc *desc, int32_t n_layers, int32_t n_seq,
+                                  const moespec_paged_cache *cache, const int32_t *first, const int32_t *cache_len,
+                                  int32_t max_len, void *k_cache, void *v_cache, void *hip_stream);
+
+/* Bytes of workspace of moespec_paged_attention for up to n_seq sequences of max_len entries (0 on an invalid descriptor or range).  Host only. */
+size_t moespec_paged_attention_workspace_bytes(const moespec_attn_desc *desc, const moespec_paged_cache *cache, int32_t n_seq,
+                                               int32_t max_len);
+
+/*
+ * Attention of one new token of every sequence over the entries in its pages (its own among them, once moespec_paged_write has taken it
+ * in): out[s, h] = sum_j softmax_j(scale q[s, h] . K_j) V_j,  lse[s, h] = log sum_j exp(scale q[s, h] . K_j),  j < cache_len[s].
+ *   cache                one layer's pages
+ *   q    [n_seq, H, D] dtype in   rows q_stride elements apart (0: H * D), multiples of 16 bytes
+ *   cache_len [n_seq] int32 in;  max_len: no sequence has more entries, 0 .. max_pages * page_size; sizes the launch
+ *   out  [n_seq, H, D] dtype out, lse [n_seq, H] float out (natural logarithm; may be NULL)
+ * Entries whose page is outside of the pool are not seen, nor those from cache_len on, whatever they hold.  A token that sees no
+ * key, or whose every score is -inf, gets out = 0 and lse = -inf.  Weights (times the values' scale) enter to 2^-18 in a bf16 layer,
+ * everything else is fp32.  desc.capacity does not matter here.
+ */
+moespec_status moespec_paged_attention(const moespec_attn_desc *desc, const moespec_paged_cache *cache, int32_t n_seq,
+                                       const void *q, int64_t q_stride, const int32_t *cache_len, int32_t max_len, void *out,
+                                       float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* What moespec_draft_verify judges by.  Host struct holding device pointers. */
+typedef struct {
+  int32_t vocab;            /* V tokens, 2 .. 2^24                                                        */
+  int32_t dtype;            /* moespec_dtype of the logits                                                */
+  int64_t logit_stride;     /* elements from a row of logits to the next one; 0: V                        */
+  int64_t draft_stride;     /* the same for draft_logits                                                  */
+  const void *logits;       /* [M, V] the target's, row t for what follows token t                        */
+  const void *draft_logits; /* [M, V] the drafter's, from which the token behind t was drawn; or NULL     */
+  const float *temperature; /* [n_seq] or NULL (1); not above 0: greedy.  Taken within 2^-60 .. 2^60      */
+} moespec_verify;
+
+/* Bytes of workspace of moespec_draft_verify for up to n_seq sequences and M_max tokens (0 on an invalid descriptor or range; a descriptor with draft_logits
+ * needs more).  Host only. */
+size_t moespec_verify_workspace_bytes(const moespec_verify *verify, int32_t n_seq, int32_t M_max);
+
+/*
+ * Accepts drafted tokens against the target's distribution, so that what is kept is distributed as the target's own samples.
+ * Row 0 of a sequence's tree is its root: the last token that was sampled, accepted by definition.  A token's parent is the last token in
+ * front of it that its mask shows (chains: the one in front).  From the root on, with p the target's distribution behind the last
+ * accepted token (softmax of logits / temperature), its children in order:
+ *   accept child c of token x if u_accept[c] q(x) < p(x);  else p <- max(p - q, 0) / sum max(p - q, 0), and the next child
+ * where q is the drafter's distribution (with draft_logits; chains only), or 1 at x and 0 elsewhere.  Where no child is
+ * accepted the path ends, and the next token is the first whose running sum of p exceeds u_sample times the whole sum.  Greedy: p is 1 at the
+ * largest logit (ties to the lowest token), and no number is drawn.
+ *   tokens   [M] int32 in     outside of 0 .. V - 1: rejected
+ *   u_accept [M] double in, u_sample [n_seq] double in   uniform in [0, 1)
+ *   path     [n_seq, max_path] int32 out   places of the accepted tokens in the tree, the root's 0 first; -1 behind n_path
+ *   n_path   [n_seq] int32 out             1 + accepted tokens; 0 for an empty tree.  A path longer than max_path ends there, and next_token is
+ *                                          the accepted token that follows on it
+ *   next_token [n_seq] int32 out           -1 for an empty tree
+ *   accepted [M] float out                 1 for tokens of the path and 0 for others (a row_weight of moespec_cache_weights); may be NULL
+ * Probabilities, sums and decisions are in fp64.  A row of logits with NaN or +inf, or of -inf alone, is no distribution: its children are
+ * rejected, and next_token is -1 where the path ends there; such a row of draft_logits rejects its token and leaves p as it is, as
+ * does a difference p - q without anything above 0.  tree.q_stride and tree.kv_stride do not matter.
+ */
+moespec_status moespec_draft_verify(const moespec_verify *verify, const moespec_tree *tree, const int32_t *tokens,
+                                    const double *u_accept, const double *u_sample, int32_t *path, int32_t *n_path,
+                                    int32_t max_path, int32_t *next_token, float *accepted, void *ws, size_t ws_bytes,
+                                    void *hip_stream);
 
 #ifdef __cplusplus
 }

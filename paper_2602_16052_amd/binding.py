@@ -23,6 +23,7 @@ F32, BF16 = 0, 1
 TRUNCATE, SUBSTITUTE = 0, 1
 GATE_SOFTMAX, GATE_SIGMOID = 0, 1
 BLOCK_GATE_NONE, BLOCK_GATE_CHANNEL, BLOCK_GATE_TOKEN, BLOCK_GATE_ELEMENT = range(4)
+CACHE_PLAIN, CACHE_I8, CACHE_E4M3 = range(3)
 
 EXPORTS = ("moespec_abi_version", "moespec_status_string", "moespec_check_desc", "moespec_workspace_bytes",
            "moespec_route", "moespec_budget", "moespec_expert_ffn", "moespec_layer_forward",
@@ -30,7 +31,9 @@ EXPORTS = ("moespec_abi_version", "moespec_status_string", "moespec_check_desc",
            "moespec_calibration_count", "moespec_static_shortlist", "moespec_coverage_curve",
            "moespec_reconstruction_error", "moespec_oracle_ranking", "moespec_stream_read",
            "moespec_check_attn_desc", "moespec_attn_workspace_bytes", "moespec_tree_attention", "moespec_cache_weights",
-           "moespec_cache_commit", "moespec_evict_workspace_bytes", "moespec_cache_evict", "moespec_block_norm")
+           "moespec_cache_commit", "moespec_evict_workspace_bytes", "moespec_cache_evict", "moespec_block_norm",
+           "moespec_head_rope", "moespec_paged_write", "moespec_paged_read", "moespec_paged_attention_workspace_bytes",
+           "moespec_paged_attention", "moespec_verify_workspace_bytes", "moespec_draft_verify")
 
 
 class MoeSpecError(RuntimeError):
@@ -68,6 +71,22 @@ class Tree(Structure):
 class Block(Structure):
     _fields_ = [("post_norm", c_int32), ("gate_kind", c_int32), ("gate_sigmoid", c_int32), ("scale", c_float),
                 ("eps", c_float), ("w_post", c_void_p), ("gate", c_void_p), ("w_pre", c_void_p)]
+
+
+class Rope(Structure):
+    _fields_ = [("rot_dim", c_int32), ("interleaved", c_int32), ("norm", c_int32), ("eps", c_float), ("w_q", c_void_p),
+                ("w_k", c_void_p), ("freq", c_void_p), ("positions", c_void_p), ("cache_len", c_void_p),
+                ("q_out_stride", c_int64), ("k_out_stride", c_int64)]
+
+
+class CPagedCache(Structure):
+    _fields_ = [("code", c_int32), ("n_pages", c_int32), ("page_size", c_int32), ("max_pages", c_int32), ("k_pages", c_void_p),
+                ("v_pages", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p), ("page_table", c_void_p)]
+
+
+class Verify(Structure):
+    _fields_ = [("vocab", c_int32), ("dtype", c_int32), ("logit_stride", c_int64), ("draft_stride", c_int64),
+                ("logits", c_void_p), ("draft_logits", c_void_p), ("temperature", c_void_p)]
 
 
 TRACE_POINTS = 5
@@ -154,6 +173,22 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                                         P, P, P, c_size_t, P]
     lib.moespec_block_norm.restype = c_int32
     lib.moespec_block_norm.argtypes = [POINTER(Desc), POINTER(Block), P, P, c_int32, P, P, P]
+    lib.moespec_head_rope.restype = c_int32
+    lib.moespec_head_rope.argtypes = [POINTER(CAttnDesc), POINTER(Rope), POINTER(Tree), P, P, P, P, P]
+    lib.moespec_paged_write.restype = c_int32
+    lib.moespec_paged_write.argtypes = [POINTER(CAttnDesc), c_int32, POINTER(CPagedCache), POINTER(Tree), P, P, P, P, c_int32, P, P,
+                                        P]
+    lib.moespec_paged_read.restype = c_int32
+    lib.moespec_paged_read.argtypes = [POINTER(CAttnDesc), c_int32, c_int32, POINTER(CPagedCache), P, P, c_int32, P, P, P]
+    lib.moespec_paged_attention_workspace_bytes.restype = c_size_t
+    lib.moespec_paged_attention_workspace_bytes.argtypes = [POINTER(CAttnDesc), POINTER(CPagedCache), c_int32, c_int32]
+    lib.moespec_paged_attention.restype = c_int32
+    lib.moespec_paged_attention.argtypes = [POINTER(CAttnDesc), POINTER(CPagedCache), c_int32, P, c_int64, P, c_int32, P, P, P,
+                                            c_size_t, P]
+    lib.moespec_verify_workspace_bytes.restype = c_size_t
+    lib.moespec_verify_workspace_bytes.argtypes = [POINTER(Verify), c_int32, c_int32]
+    lib.moespec_draft_verify.restype = c_int32
+    lib.moespec_draft_verify.argtypes = [POINTER(Verify), POINTER(Tree), P, P, P, P, P, c_int32, P, P, P, c_size_t, P]
     if path is None:
         _lib = lib
     return lib
@@ -881,3 +916,283 @@ def moespec_block_norm(desc: LayerDesc, y, residual=None, r=None, x=None, post_n
         x = torch.empty_like(y) if x is None else x
     BlockNormCall(desc, y, residual, r, x, post_norm, w_post, gate, gate_kind, gate_sigmoid, scale, w_pre, eps, stream)()
     return r, x
+
+
+# ---- Around both halves of a serving step: head norm and rotation, a paged cache, single tokens over it, verification.
+
+class HeadRopeCall(_Call):
+    """moespec_head_rope: queries q [M, H, D] and keys k [M, Hk, D] (views with longer rows are taken as they are; one of them may be
+    None, with its output) normed for each head and rotated, into q_out, k_out: the same shapes, views too, or q and k
+    themselves.  freq [rot_dim / 2] float32; w_q, w_k [D] or None; the place of a token is positions [M] int32, or cache_len
+    [n_seq] int32 (None: 0) plus its depth in the tree that tree_off, tree_mask and max_tree describe (TreeAttentionCall)."""
+
+    def __init__(self, desc: AttnDesc, q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_out: Optional[torch.Tensor],
+                 k_out: Optional[torch.Tensor], freq: Optional[torch.Tensor], rot_dim: Optional[int] = None,
+                 interleaved: bool = False, norm: bool = False, w_q: Optional[torch.Tensor] = None,
+                 w_k: Optional[torch.Tensor] = None, eps: float = 0.0, positions: Optional[torch.Tensor] = None,
+                 cache_len: Optional[torch.Tensor] = None, tree_off: Optional[torch.Tensor] = None,
+                 tree_mask: Optional[torch.Tensor] = None, max_tree: Optional[int] = None, stream=None):
+        a, dt, i32, H, Hk, D = _Args(), desc.torch_dtype, torch.int32, desc.n_heads, desc.n_kv_heads, desc.head_dim
+        if q is None and k is None:
+            raise ValueError("q and k must not both be None")
+        M = (k if q is None else q).shape[0]
+        S, most = _sizes(M, tree_off, max_tree)
+        rot = (D if freq is not None else 0) if rot_dim is None else int(rot_dim)
+        rows = lambda t, n, name: (None, 0) if t is None else a.rows(t, dt, (M, n, D), name)  # noqa: E731
+        (qp, qs), (kp, ks) = rows(q, H, "q"), rows(k, Hk, "k")
+        (qop, qos), (kop, kos) = rows(q_out, H, "q_out"), rows(k_out, Hk, "k_out")
+        self._cd, self._tree = desc.c(), _tree(a, M, S, most, qs, ks, tree_off, tree_mask)
+        self._rope = Rope(rot, int(bool(interleaved)), int(bool(norm)), eps, a.ptr(w_q, dt, (D,), "w_q"), a.ptr(w_k, dt, (D,), "w_k"),
+                          a.ptr(freq, torch.float32, (rot // 2,), "freq"), a.ptr(positions, i32, (M,), "positions"),
+                          a.ptr(cache_len, i32, (S,), "cache_len"), qos, kos)
+        args = (ctypes.byref(self._cd), ctypes.byref(self._rope), ctypes.byref(self._tree), qp, kp, qop, kop)
+        super().__init__("moespec_head_rope", a.device, args,
+                         (q, k, q_out, k_out, freq, w_q, w_k, positions, cache_len, tree_off, tree_mask), stream)
+
+
+def moespec_head_rope(desc: AttnDesc, q, k, q_out=None, k_out=None, freq=None, rot_dim=None, interleaved=False, norm=False, w_q=None,
+                      w_k=None, eps=0.0, positions=None, cache_len=None, tree_off=None, tree_mask=None, max_tree=None, stream=None):
+    """Queries and keys made ready for attention (HeadRopeCall).  Returns (q_out, k_out); padding rows of new ones are not written."""
+    with _allocating(stream):
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None and q is not None else q_out
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None and k is not None else k_out
+    HeadRopeCall(desc, q, k, q_out, k_out, freq, rot_dim, interleaved, norm, w_q, w_k, eps, positions, cache_len, tree_off, tree_mask,
+                 max_tree, stream)()
+    return q_out, k_out
+
+
+@dataclass
+class PagedCache:
+    """Keys and values of n_layers layers in pages of a pool (host side of moespec_paged_cache).  k_pages, v_pages [n_layers, n_pages,
+    Hk, page_size, D] in the layer's dtype (CACHE_PLAIN), int8 (CACHE_I8) or float8_e4m3fn (CACHE_E4M3); page_table [n_seq,
+    max_pages] int32: entry e of a sequence lies in page page_table[s, e // page_size]; k_scale, v_scale [n_layers, n_pages, Hk,
+    page_size] float32 with codes, else None."""
+    code: int
+    k_pages: torch.Tensor
+    v_pages: torch.Tensor
+    page_table: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+    @property
+    def n_layers(self) -> int:
+        return self.k_pages.shape[0]
+
+    @property
+    def max_entries(self) -> int:
+        return self.page_table.shape[1] * self.k_pages.shape[3]
+
+    def c(self, a: _Args, desc: AttnDesc, n_seq: int, layer: Optional[int] = None) -> CPagedCache:
+        """The struct with checked pointers: of all layers, or of one."""
+        held = {CACHE_PLAIN: desc.torch_dtype, CACHE_I8: torch.int8, CACHE_E4M3: torch.float8_e4m3fn}.get(self.code)
+        if held is None:
+            raise ValueError(f"unknown cache code {self.code}")
+        if self.k_pages.dim() != 5 or self.page_table.dim() != 2:
+            raise ValueError("k_pages must be [n_layers, n_pages, Hk, page_size, D] and page_table [n_seq, max_pages]")
+        L, n_pages, _, size, _ = self.k_pages.shape
+        if layer is not None and not 0 <= layer < L:
+            raise ValueError(f"layer must be in 0 .. {L - 1}, got {layer}")
+        shape = (L, n_pages, desc.n_kv_heads, size, desc.head_dim)
+        at = lambda t, dt, sh, name: None if t is None else a.ptr(t, dt, sh, name) and t[layer or 0].data_ptr()  # noqa: E731
+        return CPagedCache(self.code, n_pages, size, self.page_table.shape[1], at(self.k_pages, held, shape, "k_pages"),
+                           at(self.v_pages, held, shape, "v_pages"), at(self.k_scale, torch.float32, shape[:-1], "k_scale"),
+                           at(self.v_scale, torch.float32, shape[:-1], "v_scale"),
+                           a.ptr(self.page_table, torch.int32, (n_seq, self.page_table.shape[1]), "page_table"))
+
+    def tensors(self):
+        return (self.k_pages, self.v_pages, self.page_table, self.k_scale, self.v_scale)
+
+
+def alloc_paged_cache(desc: AttnDesc, code: int, n_pages: int, page_size: int, page_table: torch.Tensor,
+                      n_layers: int = 1) -> PagedCache:
+    """A pool of n_pages pages for each layer, on the table's device.  Its contents are undefined."""
+    held = {CACHE_PLAIN: desc.torch_dtype, CACHE_I8: torch.int8, CACHE_E4M3: torch.float8_e4m3fn}[code]
+    shape, dev = (n_layers, n_pages, desc.n_kv_heads, page_size, desc.head_dim), page_table.device
+    pages = [torch.empty(shape, dtype=held, device=dev) for _ in range(2)]
+    scales = [None if code == CACHE_PLAIN else torch.empty(shape[:-1], dtype=torch.float32, device=dev) for _ in range(2)]
+    return PagedCache(code, *pages, page_table, *scales)
+
+
+class PagedWriteCall(_Call):
+    """moespec_paged_write: accepted paths, or whole trees (path and n_path None), appended to the pages of all of the cache's layers.
+    k_tree, v_tree [n_layers, M, Hk, D]; path [n_seq, max_path] int32; n_path, cache_len, new_len [n_seq] int32."""
+
+    def __init__(self, desc: AttnDesc, cache: PagedCache, k_tree: torch.Tensor, v_tree: torch.Tensor, cache_len: torch.Tensor,
+                 path: Optional[torch.Tensor] = None, n_path: Optional[torch.Tensor] = None,
+                 new_len: Optional[torch.Tensor] = None, tree_off: Optional[torch.Tensor] = None,
+                 max_tree: Optional[int] = None, stream=None):
+        a, dt, Hk, D, L, i32 = _Args(), desc.torch_dtype, desc.n_kv_heads, desc.head_dim, cache.n_layers, torch.int32
+        M = k_tree.shape[-3]
+        S, most = _sizes(M, tree_off, max_tree)
+        (kp, ks), (vp, vs) = a.rows(k_tree, dt, (L, M, Hk, D), "k_tree"), a.rows(v_tree, dt, (L, M, Hk, D), "v_tree")
+        if vs != ks:
+            raise ValueError("k_tree and v_tree must have the same row stride")
+        self._cd, self._cache, self._tree = desc.c(), cache.c(a, desc, S), _tree(a, M, S, most, 0, ks, tree_off, None)
+        n = 0 if path is None else path.shape[-1]
+        args = (ctypes.byref(self._cd), L, ctypes.byref(self._cache), ctypes.byref(self._tree), kp, vp,
+                a.ptr(path, i32, (S, n), "path"), a.ptr(n_path, i32, (S,), "n_path"), n, a.ptr(cache_len, i32, (S,), "cache_len"),
+                a.ptr(new_len, i32, (S,), "new_len"))
+        super().__init__("moespec_paged_write", a.device, args,
+                         (*cache.tensors(), k_tree, v_tree, cache_len, path, n_path, new_len, tree_off), stream)
+
+
+def moespec_paged_write(desc: AttnDesc, cache: PagedCache, k_tree, v_tree, cache_len, path=None, n_path=None, new_len=None,
+                        tree_off=None, max_tree=None, stream=None) -> torch.Tensor:
+    """Keys and values appended to the pages, in place (PagedWriteCall).  Returns new_len."""
+    if new_len is None:
+        with _allocating(stream):
+            new_len = torch.empty_like(cache_len)
+    PagedWriteCall(desc, cache, k_tree, v_tree, cache_len, path, n_path, new_len, tree_off, max_tree, stream)()
+    return new_len
+
+
+class PagedReadCall(_Call):
+    """moespec_paged_read: entries first .. cache_len - 1 (first [n_seq] int32 or None: 0) into contiguous caches k_cache, v_cache
+    [n_layers, n_seq, Hk, capacity, D]; max_len: a bound on the lengths, what cache and table have room for if None."""
+
+    def __init__(self, desc: AttnDesc, cache: PagedCache, cache_len: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                 first: Optional[torch.Tensor] = None, max_len: Optional[int] = None, stream=None):
+        a, dt, i32, S = _Args(), desc.torch_dtype, torch.int32, cache_len.numel()
+        dense = (cache.n_layers, S, desc.n_kv_heads, desc.capacity, desc.head_dim)
+        self._cd, self._cache = desc.c(), cache.c(a, desc, S)
+        args = (ctypes.byref(self._cd), cache.n_layers, S, ctypes.byref(self._cache), a.ptr(first, i32, (S,), "first"),
+                a.ptr(cache_len, i32, (S,), "cache_len"), min(desc.capacity, cache.max_entries) if max_len is None else int(max_len),
+                a.ptr(k_cache, dt, dense, "k_cache"), a.ptr(v_cache, dt, dense, "v_cache"))
+        super().__init__("moespec_paged_read", a.device, args, (*cache.tensors(), first, cache_len, k_cache, v_cache), stream)
+
+
+def moespec_paged_read(desc: AttnDesc, cache: PagedCache, cache_len, k_cache=None, v_cache=None, first=None, max_len=None,
+                       stream=None):
+    """Entries in pages laid out as contiguous caches (PagedReadCall).  Returns (k_cache, v_cache); entries of new ones that are not
+    read are 0."""
+    dense = (cache.n_layers, cache_len.numel(), desc.n_kv_heads, desc.capacity, desc.head_dim)
+    with _allocating(stream):
+        k_cache, v_cache = (torch.zeros(dense, dtype=desc.torch_dtype, device=cache_len.device) if t is None else t
+                            for t in (k_cache, v_cache))
+    PagedReadCall(desc, cache, cache_len, k_cache, v_cache, first, max_len, stream)()
+    return k_cache, v_cache
+
+
+def paged_attention_workspace_bytes(desc: AttnDesc, cache: PagedCache, n_seq: int, max_len: int) -> int:
+    c = desc.c()
+    p = CPagedCache(cache.code, cache.k_pages.shape[1], cache.k_pages.shape[3], cache.page_table.shape[1],
+                    *(None if t is None else t.data_ptr() for t in (cache.k_pages, cache.v_pages, cache.k_scale, cache.v_scale)),
+                    cache.page_table.data_ptr())
+    return int(load_library().moespec_paged_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(p), int(n_seq), int(max_len)))
+
+
+def alloc_paged_attention_workspace(desc: AttnDesc, cache: PagedCache, n_seq: int, max_len: int) -> torch.Tensor:
+    n = paged_attention_workspace_bytes(desc, cache, n_seq, max_len)
+    if n == 0:
+        raise MoeSpecError(ERR_INVALID_ARG, "moespec_paged_attention_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=cache.page_table.device)
+
+
+class PagedAttentionCall(_Call):
+    """moespec_paged_attention: one new token of every sequence, q [n_seq, H, D] (a view with longer rows is taken as it is), over the
+    entries in a layer's pages; cache_len [n_seq] int32; out [n_seq, H, D]; lse [n_seq, H] float32 or None; max_len: a bound on
+    the lengths, what the table has room for if None."""
+
+    def __init__(self, desc: AttnDesc, cache: PagedCache, q: torch.Tensor, cache_len: torch.Tensor, ws: torch.Tensor,
+                 out: torch.Tensor, lse: Optional[torch.Tensor] = None, max_len: Optional[int] = None, layer: int = 0, stream=None):
+        a, dt, S, H, D = _Args(), desc.torch_dtype, q.shape[0], desc.n_heads, desc.head_dim
+        qp, qs = a.rows(q, dt, (S, H, D), "q")
+        self._cd, self._cache = desc.c(), cache.c(a, desc, S, int(layer))
+        args = (ctypes.byref(self._cd), ctypes.byref(self._cache), S, qp, qs, a.ptr(cache_len, torch.int32, (S,), "cache_len"),
+                cache.max_entries if max_len is None else int(max_len), a.ptr(out, dt, (S, H, D), "out"),
+                a.ptr(lse, torch.float32, (S, H), "lse"), *a.scratch(ws))
+        super().__init__("moespec_paged_attention", a.device, args, (*cache.tensors(), q, cache_len, ws, out, lse), stream)
+
+
+def moespec_paged_attention(desc: AttnDesc, cache: PagedCache, q, cache_len, ws=None, out=None, lse=None, max_len=None, layer=0,
+                            stream=None):
+    """Attention of one new token of every sequence over its pages (PagedAttentionCall).  Returns (out, lse)."""
+    S, H = q.shape[0], desc.n_heads
+    with _allocating(stream):
+        if out is None:
+            out = torch.empty((S, H, desc.head_dim), dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty((S, H), dtype=torch.float32, device=q.device)
+        if ws is None:
+            ws = alloc_paged_attention_workspace(desc, cache, S, cache.max_entries if max_len is None else max_len)
+    PagedAttentionCall(desc, cache, q, cache_len, ws, out, lse, max_len, layer, stream)()
+    return out, lse
+
+
+@dataclass
+class VerifyDesc:
+    """The vocabulary and the dtype (F32 or BF16) of the logits that drafts are judged by."""
+    vocab: int
+    dtype: int
+
+    @property
+    def torch_dtype(self) -> torch.dtype:
+        return torch.bfloat16 if self.dtype == BF16 else torch.float32
+
+
+def verify_workspace_bytes(desc: VerifyDesc, n_seq: int, M_max: int, sampled: bool = False) -> int:
+    """sampled: with the drafter's logits."""
+    v = Verify(desc.vocab, desc.dtype, 0, 0, None, 16 if sampled else None, None)
+    return int(load_library().moespec_verify_workspace_bytes(ctypes.byref(v), int(n_seq), int(M_max)))
+
+
+def alloc_verify_workspace(desc: VerifyDesc, n_seq: int, M_max: int, sampled: bool = False, device="cuda") -> torch.Tensor:
+    n = verify_workspace_bytes(desc, n_seq, M_max, sampled)
+    if n == 0:
+        raise MoeSpecError(ERR_INVALID_ARG, "moespec_verify_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+class DraftVerifyCall(_Call):
+    """moespec_draft_verify: from the target's logits [M, vocab] (and, for drafts sampled in chains, the drafter's draft_logits [M,
+    vocab]; rows of both may be longer in memory) and the uniform numbers u_accept [M], u_sample [n_seq] float64 to the accepted
+    path [n_seq, max_path] int32, n_path and next_token [n_seq] int32, and accepted [M] float32 (1 or 0) or None.  tokens [M] int32;
+    temperature [n_seq] float32 or None (1); tree_off, tree_mask, max_tree as in TreeAttentionCall, row 0 of a tree its root."""
+
+    def __init__(self, desc: VerifyDesc, logits: torch.Tensor, tokens: torch.Tensor, u_accept: torch.Tensor, u_sample: torch.Tensor,
+                 path: torch.Tensor, n_path: torch.Tensor, next_token: torch.Tensor, ws: torch.Tensor,
+                 draft_logits: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None,
+                 accepted: Optional[torch.Tensor] = None, tree_off: Optional[torch.Tensor] = None,
+                 tree_mask: Optional[torch.Tensor] = None, max_tree: Optional[int] = None, stream=None):
+        a, i32, f64 = _Args(), torch.int32, torch.float64
+        M = logits.shape[0]
+        S, most = _sizes(M, tree_off, max_tree)
+
+        def rows(t, name):
+            if t is None:
+                return None, 0
+            a.on(t, name)
+            if t.dtype != desc.torch_dtype or tuple(t.shape) != (M, desc.vocab):
+                raise ValueError(f"{name} must be {desc.torch_dtype} of shape {(M, desc.vocab)}, got {t.dtype} of {tuple(t.shape)}")
+            if t.stride(1) != 1 or (M > 1 and t.stride(0) < desc.vocab):
+                raise ValueError(f"{name}: the logits of a token must lie in a row")
+            return t.data_ptr(), t.stride(0) if M > 1 else 0
+
+        (lp, ls), (dp, ds) = rows(logits, "logits"), rows(draft_logits, "draft_logits")
+        n = path.shape[-1]
+        self._verify = Verify(desc.vocab, desc.dtype, ls, ds, lp, dp, a.ptr(temperature, torch.float32, (S,), "temperature"))
+        self._tree = _tree(a, M, S, most, 0, 0, tree_off, tree_mask)
+        args = (ctypes.byref(self._verify), ctypes.byref(self._tree), a.ptr(tokens, i32, (M,), "tokens"),
+                a.ptr(u_accept, f64, (M,), "u_accept"), a.ptr(u_sample, f64, (S,), "u_sample"), a.ptr(path, i32, (S, n), "path"),
+                a.ptr(n_path, i32, (S,), "n_path"), n, a.ptr(next_token, i32, (S,), "next_token"),
+                a.ptr(accepted, torch.float32, (M,), "accepted"), *a.scratch(ws))
+        super().__init__("moespec_draft_verify", a.device, args,
+                         (logits, tokens, u_accept, u_sample, path, n_path, next_token, ws, draft_logits, temperature, accepted,
+                          tree_off, tree_mask), stream)
+
+
+def moespec_draft_verify(desc: VerifyDesc, logits, tokens, u_accept, u_sample, max_path, draft_logits=None, temperature=None,
+                         tree_off=None, tree_mask=None, max_tree=None, ws=None, stream=None):
+    """Verification of drafted tokens (DraftVerifyCall).  Returns dict(path, n_path, next_token, accepted); accepted is 0 for rows of
+    no sequence."""
+    M, dev = logits.shape[0], logits.device
+    S, _ = _sizes(M, tree_off, max_tree)
+    with _allocating(stream):
+        path = torch.empty((S, int(max_path)), dtype=torch.int32, device=dev)
+        n_path, next_token = (torch.empty(S, dtype=torch.int32, device=dev) for _ in range(2))
+        accepted = torch.zeros(M, dtype=torch.float32, device=dev)
+        if ws is None:
+            ws = alloc_verify_workspace(desc, S, M, draft_logits is not None, dev)
+    DraftVerifyCall(desc, logits, tokens, u_accept, u_sample, path, n_path, next_token, ws, draft_logits, temperature, accepted,
+                    tree_off, tree_mask, max_tree, stream)()
+    return dict(path=path, n_path=n_path, next_token=next_token, accepted=accepted)

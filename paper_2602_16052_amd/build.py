@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libmoespec.so")
 SOURCES = ("api.hip", "route.hip", "budget.hip", "prologue.hip", "expert_ffn.hip", "expert_wide.hip", "analysis.hip", "stack.hip",
-           "attention.hip", "cache_weights.hip", "cache.hip", "block_norm.hip", "attention_api.hip")
+           "attention.hip", "cache_weights.hip", "cache.hip", "block_norm.hip", "attention_api.hip",
+           "head_rope.hip", "paged_cache.hip", "paged_attention.hip", "draft_verify.hip", "serving_api.hip")
 
 # The first 14 words of a kernel's arguments arrive in scalar registers (kernarg preload) instead of by a load from cold
 # memory: 0.1 to 0.2 us of every launch.  Kernels name the arguments that their first loads need first.

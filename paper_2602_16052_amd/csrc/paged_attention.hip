@@ -1,0 +1,484 @@
+// Attention of one new token of every sequence over its pages of keys and values, which may be held in 8 bits.
+//
+// Bound by the stream of keys and values: each is read once for all query heads that share it.  One pass with a running maximum m and
+// sum l for each head (in units of log 2): p = 2^(c q.k - m), l += p, O += p V, out = O / l; the scale of a key's row multiplies its
+// score, that of a value's row its weight.  The keys are split into parts (few sequences) that a second kernel joins.
+//
+// The query heads of a KV head are the 16 columns of matrix instructions (unused ones repeat a head and are not written).  S = K Q^T
+// takes keys as they come from memory: lane l holds 16 bytes of key l % 16, piece l / 16, and queries are loaded in the
+// same order of elements.  A lane's scores, key 4 (l / 16) + i of head l % 16, are already the right operand of O^T = V^T P^T.
+// Values lie in rows and are needed in columns: a wave lays its own through LDS (rows of D elements and a pad that keeps the
+// transposing reads off each other's banks).  Waves share nothing until their results are joined at the end.
+#include "serving.h"
+
+namespace moespec {
+
+namespace {
+
+struct PagedAttnArgs {
+  KeyArgs keys;  // q, cache_len, lengths and heads (one token of every sequence)
+  Pages pages;
+  int head_tiles, slots;  // tiles of 16 query heads; parts of all sequences together, 0: every sequence is one part
+};
+
+template <typename T, int CODE, int D>
+struct PagedShape {
+  static constexpr bool kCodes = CODE != MOESPEC_CACHE_PLAIN, kBf16 = sizeof(T) == 2;
+  static constexpr int kWaves = 4;
+  static constexpr int kHalves = kBf16 ? 2 : 1, kKeys = 16 * kHalves;  // keys of a wave's tile
+  static constexpr int kUnit = kKeys * kWaves;                         // ... of a workgroup's
+  static constexpr int kHeld = kCodes ? 1 : (int)sizeof(T);            // bytes of an element in a page
+  static constexpr int kRowBytes = D * kHeld;
+  static constexpr int kLoads = (kRowBytes + 63) / 64;     // loads of 64 bytes of 16 keys; the last one may be of 32
+  static constexpr bool kTail = kRowBytes % 64 != 0;       // (8-bit rows of 96: 8 bytes a lane)
+  static constexpr int kPiece = 16 / kHeld;                // elements of a lane's 16 bytes
+  static constexpr int kStride = D * (int)sizeof(T) + (kBf16 ? 32 : 16);  // bytes of a value's row in LDS
+  static constexpr int kTileLds = kKeys * kStride;
+  static constexpr int kValueLanes = kRowBytes / 16;       // lanes that hold a row of values
+  static constexpr int kValueRows = 64 / pow2_ceil(kValueLanes) < kKeys ? 64 / pow2_ceil(kValueLanes) : kKeys;  // rows of a load
+  static constexpr int kValueLoads = kKeys / kValueRows;
+  static constexpr int kJoin = kWaves * 16 * (D + 2) * (int)sizeof(float);
+  static constexpr int kLds = kWaves * kTileLds > kJoin ? kWaves * kTileLds : kJoin;
+  static constexpr int kQ = D / 4;  // query elements of a lane
+};
+
+// Two bytes' worth of codes, and four, as values.
+template <int CODE>
+__device__ __forceinline__ float code_value(uint32_t w, int e) {
+  if (CODE == MOESPEC_CACHE_I8) return (float)(int8_t)(w >> (8 * e));
+  switch (e) {
+    case 0: return __builtin_amdgcn_cvt_f32_fp8(w, 0);
+    case 1: return __builtin_amdgcn_cvt_f32_fp8(w, 1);
+    case 2: return __builtin_amdgcn_cvt_f32_fp8(w, 2);
+    default: return __builtin_amdgcn_cvt_f32_fp8(w, 3);
+  }
+}
+// Eight codes as bf16 (exact: both have no more bits).
+template <int CODE>
+__device__ __forceinline__ bf16x8 codes_bf16(uint32_t a, uint32_t b) {
+  bf16x8 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[e] = (__bf16)code_value<CODE>(a, e);
+    v[4 + e] = (__bf16)code_value<CODE>(b, e);
+  }
+  return v;
+}
+
+// v of the lanes that hold the same head, l ^ 16 and l ^ 32, combined.
+__device__ __forceinline__ float head_max(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  return half_swap(v, true);
+}
+__device__ __forceinline__ float head_sum(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  return half_swap(v, false);
+}
+
+template <typename T, int CODE, int D>
+__global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T *__restrict__ out, float *__restrict__ lse,
+                                                              float *__restrict__ part, float2 *__restrict__ part_ml,
+                                                              int32_t *__restrict__ first_of) {
+  typedef PagedShape<T, CODE, D> P;
+  constexpr int NB = D / 16;
+  extern __shared__ __align__(16) unsigned char lds[];
+  const KeyArgs &ka = a.keys;
+  const Pages &pg = a.pages;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g4 = lane >> 4;
+  // head tiles that share keys are neighbours on one XCD (workgroup b runs on XCD b mod 8)
+  const int slot = blockIdx.x / 8, group = slot / a.head_tiles * 8 + (int)(blockIdx.x % 8), tile = slot % a.head_tiles;
+  const int n_parts = a.slots == 0 ? ka.n_seq : a.slots, index = group % n_parts, hk = group / n_parts;
+  if (hk >= ka.Hk) return;
+  auto units = [&](const SeqGeom &g) { return (g.len + P::kUnit - 1) / P::kUnit; };
+  const Share share = share_of(ka, a.slots, index, units, blockIdx.x == 0 ? first_of : nullptr);
+  const int s = share.s;
+  if (s < 0) return;
+  const int len = seq_geom(ka, s).len, all = (len + P::kUnit - 1) / P::kUnit;
+  const int u0 = share.first(all), u1 = share.last(all);
+  const int h = hk * ka.G + min(tile * 16 + n16, ka.G - 1);
+
+  // queries, in the order of a lane's keys
+  typename std::conditional<P::kBf16, bf16x8, f32x4>::type q[P::kBf16 ? D / 32 : D / 16];
+  {
+    const T *qp = static_cast<const T *>(ka.q) + (int64_t)s * ka.q_stride + h * D;
+    if constexpr (P::kBf16 && !P::kCodes) {
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) q[i] = *reinterpret_cast<const bf16x8 *>(qp + 32 * i + 8 * g4);
+    } else if constexpr (P::kBf16) {
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+        q[i] = *reinterpret_cast<const bf16x8 *>(qp + (P::kTail && i == D / 32 - 1 ? 32 * i + 8 * g4 : i / 2 * 64 + 16 * g4 + 8 * (i % 2)));
+    } else if constexpr (!P::kCodes) {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const f32x4 *>(qp + 16 * i + 4 * g4);
+    } else {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+        q[i] = *reinterpret_cast<const f32x4 *>(qp + (P::kTail && i >= D / 64 * 4 ? D / 64 * 64 + 8 * g4 + 4 * (i - D / 64 * 4)
+                                                                                  : i / 4 * 64 + 16 * g4 + 4 * (i % 4)));
+    }
+  }
+
+  f32x4 o[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  unsigned char *const my = lds + wave * P::kTileLds;
+  const uint32_t my_lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)my);
+
+  uint4 kr[P::kHalves][P::kLoads], vr[P::kValueLoads];
+  f32x4 ks[P::kHalves], vs[P::kHalves];
+  const int vrow = lane / pow2_ceil(P::kValueLanes), vpiece = lane % pow2_ceil(P::kValueLanes);
+  // Row (of D elements) in the pool of the first of 16 entries from e on; entries behind the last page or outside of the pool: of
+  // some page that is there, `there` says so.
+  auto rows_at = [&](int e, bool &there) -> int64_t {
+    const int at = min(e, len - 1);
+    const int p = pg.page_of(s, at);
+    there = p >= 0 && e < len;
+    return pg.row(0, max(p, 0), hk, e & ~15);
+  };
+  auto load_keys = [&](int e0) {
+#pragma unroll
+    for (int x = 0; x < P::kHalves; ++x) {
+      bool there;
+      const int64_t row = rows_at(e0 + 16 * x, there);
+      const unsigned char *at = pg.k + (row + n16) * P::kRowBytes;
+#pragma unroll
+      for (int i = 0; i < P::kLoads; ++i) {
+        if (P::kTail && i == P::kLoads - 1) {
+          const uint2 two = *reinterpret_cast<const uint2 *>(at + 64 * i + 8 * g4);
+          kr[x][i] = make_uint4(two.x, two.y, 0, 0);
+        } else {
+          kr[x][i] = *reinterpret_cast<const uint4 *>(at + 64 * i + 16 * g4);
+        }
+      }
+      if (P::kCodes) ks[x] = *reinterpret_cast<const f32x4 *>(pg.k_scale + row + 4 * g4);
+    }
+  };
+  auto load_values = [&](int e0) {
+#pragma unroll
+    for (int i = 0; i < P::kValueLoads; ++i) {
+      const int r = i * P::kValueRows + vrow;
+      bool there;
+      const int64_t row = rows_at(e0 + (r & ~15), there);
+      vr[i] = make_uint4(0, 0, 0, 0);
+      // what is not seen must meet weights of 0 as numbers
+      if (vpiece < P::kValueLanes && there && e0 + r < len)
+        vr[i] = *reinterpret_cast<const uint4 *>(pg.v + (row + (r & 15)) * P::kRowBytes + 16 * vpiece);
+    }
+    if (P::kCodes) {
+#pragma unroll
+      for (int x = 0; x < P::kHalves; ++x) {
+        bool there;
+        vs[x] = *reinterpret_cast<const f32x4 *>(pg.v_scale + rows_at(e0 + 16 * x, there) + 4 * g4);
+      }
+    }
+  };
+
+  for (int u = u0; u < u1; ++u) {
+    const int e0 = u * P::kUnit + wave * P::kKeys;
+    if (e0 >= len) break;
+    load_keys(e0);
+    load_values(e0);
+    f32x4 sc[P::kHalves];
+#pragma unroll
+    for (int x = 0; x < P::kHalves; ++x) {
+      sc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const uint32_t *w = reinterpret_cast<const uint32_t *>(kr[x]);
+      if constexpr (P::kBf16) {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          bf16x8 k;
+          if constexpr (P::kCodes) k = codes_bf16<CODE>(w[2 * i], w[2 * i + 1]);
+          else k = __builtin_bit_cast(bf16x8, kr[x][i]);
+          sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[i], sc[x], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < D / 4; ++i) {
+          const float k = P::kCodes ? code_value<CODE>(w[i / 4], i % 4) : __uint_as_float(w[i]);
+          sc[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(k, q[i / 4][i % 4], sc[x], 0, 0, 0);
+        }
+      }
+    }
+    // values to LDS
+#pragma unroll
+    for (int i = 0; i < P::kValueLoads; ++i) {
+      unsigned char *to = my + (i * P::kValueRows + vrow) * P::kStride;
+      if (vpiece < P::kValueLanes) {
+        const uint32_t w[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
+        if constexpr (!P::kCodes) {
+          *reinterpret_cast<uint4 *>(to + 16 * vpiece) = vr[i];
+        } else if constexpr (P::kBf16) {
+          *reinterpret_cast<bf16x8 *>(to + 32 * vpiece) = codes_bf16<CODE>(w[0], w[1]);
+          *reinterpret_cast<bf16x8 *>(to + 32 * vpiece + 16) = codes_bf16<CODE>(w[2], w[3]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<f32x4 *>(to + 64 * vpiece + 16 * j) =
+                f32x4{code_value<CODE>(w[j], 0), code_value<CODE>(w[j], 1), code_value<CODE>(w[j], 2), code_value<CODE>(w[j], 3)};
+        }
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < P::kHalves; ++x) {
+      bool there;
+      rows_at(e0 + 16 * x, there);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (P::kCodes) sc[x][i] *= ks[x][i];
+        const bool seen = there && e0 + 16 * x + 4 * g4 + i < len;
+        if (!seen) sc[x][i] = -INFINITY;
+        if (P::kCodes && !seen) vs[x][i] = 0.f;
+        mx = fmaxf(mx, sc[x][i]);
+      }
+    }
+    mx = head_max(mx) * ka.c;
+    // raised only when it is passed by more than 2^8: until then weights stay below 2^8, as exact as below 1, and O is not rescaled
+    const bool raise = mx > m + 8.f;
+    if (__ballot(raise) != 0) {
+      const float alpha = raise ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
+      m = raise ? mx : m;
+      l *= alpha;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[b][i] *= alpha;
+    }
+    const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int x = 0; x < P::kHalves; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sc[x][i] = __builtin_amdgcn_exp2f(fmaf(sc[x][i], ka.c, -mu));
+        l += sc[x][i];
+        if (P::kCodes) sc[x][i] *= vs[x][i];
+      }
+    asm volatile("" ::: "memory");  // the wave's own rows: LDS keeps their order
+    if constexpr (P::kBf16) {
+      // The matrix instructions take bf16 weights beside bf16 values: a weight goes in as its rounding and what that leaves (off by 2^-18 of
+      // it at most), so that outputs are as exact as their own rounding.  With the rounding alone they are 0.0023 off (root of the mean
+      // square, relative) where that leaves 0.0017; the second product is hidden behind the stream of keys and values.
+      bf16x8 p, p_rest;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = (__bf16)sc[i / 4][i % 4];
+        p_rest[i] = (__bf16)(sc[i / 4][i % 4] - (float)p[i]);
+      }
+      // lane i of 16 points at 4 elements of row i / 4 and receives element i of 4 rows
+      typedef __attribute__((address_space(3))) bf16x4 lds4;
+      const uint32_t at = my_lds + (4 * g4 + (n16 >> 2)) * P::kStride + 8 * (n16 & 3);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(uintptr_t)(at + 32 * b));
+        const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(uintptr_t)(at + 16 * P::kStride + 32 * b));
+        const bf16x8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o[b], 0, 0, 0);
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_rest, o[b], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float v = *reinterpret_cast<const float *>(my + (4 * g4 + i) * P::kStride + 64 * b + 4 * n16);
+          o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, sc[0][i], o[b], 0, 0, 0);
+        }
+    }
+    asm volatile("" ::: "memory");
+  }
+  l = head_sum(l);
+  if (m == -INFINITY && l != 0.f) m = 0.f;  // scores that are all NaN: so is the row
+
+  // the waves' results joined: [wave][head]{m, l}, then [wave][head][D]
+  __syncthreads();
+  float2 *ml = reinterpret_cast<float2 *>(lds);
+  float *op = reinterpret_cast<float *>(lds + P::kWaves * 16 * sizeof(float2));
+  if (g4 == 0) ml[wave * 16 + n16] = make_float2(m, l);
+#pragma unroll
+  for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4 *>(op + (wave * 16 + n16) * D + 16 * b + 4 * g4) = o[b];
+  __syncthreads();
+  const int heads = min(16, ka.G - tile * 16);
+  for (int id = threadIdx.x; id < heads * (D / 4); id += 256) {
+    const int n = id / (D / 4), d = 4 * (id % (D / 4));
+    float mt = -INFINITY, lt = 0.f;
+#pragma unroll
+    for (int w = 0; w < P::kWaves; ++w) mt = fmaxf(mt, ml[w * 16 + n].x);
+    const float mu = mt == -INFINITY ? 0.f : mt;
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < P::kWaves; ++w) {
+      const float2 x = ml[w * 16 + n];
+      const float f = __builtin_amdgcn_exp2f(x.x - mu);
+      lt = fmaf(x.y, f, lt);
+      const f32x4 y = *reinterpret_cast<const f32x4 *>(op + (w * 16 + n) * D + d);
+      if (x.x != -INFINITY) {  // a wave without keys has no values
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(y[e], f, v[e]);
+      }
+    }
+    const int head = hk * ka.G + tile * 16 + n;
+    if (a.slots == 0) {
+      const size_t row = (size_t)s * ka.H + head;
+      const float inv = lt == 0.f ? 0.f : 1.f / lt;
+      Elem<T>::store4(out + row * D + d, lt == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
+      if (lse && d == 0) lse[row] = lt == 0.f ? -INFINITY : (mt + __log2f(lt)) * 0.69314718055994531f;
+    } else {
+      const size_t row = (size_t)index * ka.H + head;
+      *reinterpret_cast<f32x4 *>(part + row * D + d) = v;
+      if (d == 0) part_ml[row] = make_float2(mt, lt);
+    }
+  }
+}
+
+// The parts of a token's keys joined: a workgroup of D / 4 x kGroups threads per head, the parts shared out to the groups.
+constexpr int kGroups = 8;
+template <typename T, int D>
+__global__ __launch_bounds__(kGroups *D / 4) void paged_join_kernel(KeyArgs a, int slots, const float *__restrict__ part,
+                                                                   const float2 *__restrict__ part_ml,
+                                                                   const int32_t *__restrict__ first_of, T *__restrict__ out,
+                                                                   float *__restrict__ lse) {
+  constexpr int kCols = D / 4;
+  __shared__ float2 ml[kGroups];
+  __shared__ f32x4 po[kGroups][kCols];
+  const int col = threadIdx.x % kCols, grp = threadIdx.x / kCols, head = blockIdx.x, s = blockIdx.y;
+  const int p0 = a.n_seq == 1 ? 0 : first_of[s], n = a.n_seq == 1 ? slots : first_of[s + 1] - p0;
+  float m = -INFINITY, l = 0.f;
+  f32x4 o{0.f, 0.f, 0.f, 0.f};
+  for (int i0 = grp; i0 < n; i0 += 4 * kGroups) {
+    float2 x[4];
+    f32x4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const size_t row = (size_t)(p0 + min(i0 + j * kGroups, n - 1)) * a.H + head;
+      x[j] = part_ml[row];
+      v[j] = *reinterpret_cast<const f32x4 *>(part + row * D + 4 * col);
+    }
+    float top = m;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = fmaxf(top, i0 + j * kGroups < n ? x[j].x : -INFINITY);
+    const float mu = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f(m - mu);
+    l *= f0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= f0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (i0 + j * kGroups >= n || x[j].x == -INFINITY) continue;
+      const float f = __builtin_amdgcn_exp2f(x[j].x - mu);
+      l = fmaf(f, x[j].y, l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(f, v[j][e], o[e]);
+    }
+    m = top;
+  }
+  po[grp][col] = o;
+  if (col == 0) ml[grp] = make_float2(m, l);
+  __syncthreads();
+  if (grp > 0) return;
+  float top = m;
+#pragma unroll
+  for (int g = 1; g < kGroups; ++g) top = fmaxf(top, ml[g].x);
+  const float mu = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f(m - mu);
+  l *= f0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] *= f0;
+#pragma unroll
+  for (int g = 1; g < kGroups; ++g) {
+    const float f = __builtin_amdgcn_exp2f(ml[g].x - mu);
+    l = fmaf(f, ml[g].y, l);
+    const f32x4 v = po[g][col];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = fmaf(f, v[e], o[e]);
+  }
+  const size_t row = (size_t)s * a.H + head;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  Elem<T>::store4(out + row * D + 4 * col, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
+  if (lse && col == 0) lse[row] = l == 0.f ? -INFINITY : (top + __log2f(l)) * 0.69314718055994531f;
+}
+
+constexpr int kTarget = 1024;         // workgroups wanted
+constexpr size_t kFirstBytes = 2048;  // first parts of up to kMaxShared sequences
+
+// Parts of all sequences together: enough for kTarget workgroups, none without a unit of keys; 0 where every sequence is one part.
+int slots_of(int64_t n_seq, int64_t Hk, int64_t head_tiles, int64_t max_len, int64_t unit) {
+  const int64_t units = (max_len + unit - 1) / unit;
+  int64_t n = kTarget / (Hk * head_tiles);
+  if (n > n_seq * units) n = n_seq * units;
+  if (n_seq == 1 && n > kMaxParts) n = kMaxParts;
+  return n <= n_seq || n_seq > kMaxShared ? 0 : (int)n;
+}
+
+template <typename T, int CODE, int D>
+hipError_t run_paged(const PagedAttnArgs &args, void *out, float *lse, void *ws, hipStream_t st) {
+  typedef PagedShape<T, CODE, D> P;
+  PagedAttnArgs a = args;
+  const KeyArgs &k = a.keys;
+  a.slots = slots_of(k.n_seq, k.Hk, a.head_tiles, k.max_len, P::kUnit);
+  auto kern = paged_attention_kernel<T, CODE, D>;
+  static_assert(P::kLds <= 160 * 1024, "LDS of a compute unit");
+  if (P::kLds > 64 * 1024) {
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, P::kLds);
+    if (e != hipSuccess) return e;
+  }
+  int32_t *first_of = static_cast<int32_t *>(ws);
+  float *part = reinterpret_cast<float *>(static_cast<char *>(ws) + kFirstBytes);
+  float2 *ml = reinterpret_cast<float2 *>(part + (size_t)a.slots * k.H * D);
+  const int64_t groups = (int64_t)k.Hk * (a.slots == 0 ? k.n_seq : a.slots);
+  kern<<<(unsigned)((groups + 7) / 8 * 8 * a.head_tiles), 256, P::kLds, st>>>(a, static_cast<T *>(out), lse, part, ml, first_of);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.slots == 0) return e;
+  paged_join_kernel<T, D><<<dim3(k.H, k.n_seq), kGroups * D / 4, 0, st>>>(k, a.slots, part, ml, first_of, static_cast<T *>(out), lse);
+  return hipGetLastError();
+}
+
+template <typename T, int CODE>
+hipError_t run_head(int D, const PagedAttnArgs &a, void *out, float *lse, void *ws, hipStream_t st) {
+  switch (D) {
+    case 64: return run_paged<T, CODE, 64>(a, out, lse, ws, st);
+    case 96: return run_paged<T, CODE, 96>(a, out, lse, ws, st);
+    case 128: return run_paged<T, CODE, 128>(a, out, lse, ws, st);
+    case 192: return run_paged<T, CODE, 192>(a, out, lse, ws, st);
+    default: return run_paged<T, CODE, 256>(a, out, lse, ws, st);
+  }
+}
+template <typename T>
+hipError_t run_code(int code, int D, const PagedAttnArgs &a, void *out, float *lse, void *ws, hipStream_t st) {
+  return code == MOESPEC_CACHE_PLAIN ? run_head<T, MOESPEC_CACHE_PLAIN>(D, a, out, lse, ws, st)
+         : code == MOESPEC_CACHE_I8  ? run_head<T, MOESPEC_CACHE_I8>(D, a, out, lse, ws, st)
+                                     : run_head<T, MOESPEC_CACHE_E4M3>(D, a, out, lse, ws, st);
+}
+
+}  // namespace
+
+// Room for the parts: no more workgroups than kTarget, and no more than units of 64 keys.  Neither bound grows where a call gets smaller.
+size_t paged_attention_ws(const moespec_attn_desc &ds, const moespec_paged_cache &, int n_seq, int max_len) {
+  const int64_t G = ds.n_heads / ds.n_kv_heads, units = (max_len + 63) / 64 * (int64_t)(n_seq < kMaxShared ? n_seq : kMaxShared);
+  const int64_t most = kTarget / (ds.n_kv_heads * ((G + 15) / 16)), slots = units < most ? units : most;
+  return kFirstBytes + (size_t)slots * ds.n_heads * (sizeof(float) * ds.head_dim + sizeof(float2));
+}
+
+hipError_t launch_paged_attention(const moespec_attn_desc &ds, const moespec_paged_cache &cache, int n_seq, const void *q,
+                                  int64_t q_stride, const int32_t *cache_len, int max_len, void *out, float *lse, void *ws,
+                                  hipStream_t st) {
+  PagedAttnArgs a{};
+  a.keys.q = q;
+  a.keys.cache_len = cache_len;
+  a.keys.q_stride = q_stride ? q_stride : (int64_t)ds.n_heads * ds.head_dim;
+  a.keys.n_seq = n_seq;
+  a.keys.M = n_seq;
+  a.keys.max_tree = 1;
+  a.keys.max_len = max_len;
+  a.keys.H = ds.n_heads;
+  a.keys.Hk = ds.n_kv_heads;
+  a.keys.G = ds.n_heads / ds.n_kv_heads;
+  a.keys.c = (float)((double)ds.scale * 1.4426950408889634);
+  a.pages = pages_of(ds, cache);
+  a.head_tiles = (a.keys.G + 15) / 16;
+  return ds.dtype == MOESPEC_BF16 ? run_code<uint16_t>(cache.code, ds.head_dim, a, out, lse, ws, st)
+                                  : run_code<float>(cache.code, ds.head_dim, a, out, lse, ws, st);
+}
+
+}  // namespace moespec

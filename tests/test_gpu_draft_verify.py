@@ -1,0 +1,251 @@
+"""Draft verification against the fp64 oracle's walk: every decision equal."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention_oracle as A
+from oracle import serving_oracle as V
+from paper_2602_16052_amd import binding as mb
+from attention_common import CODE, TORCH, f64, i32, random_tree
+
+pytestmark = pytest.mark.gpu
+
+
+class Batch:
+    """Random trees (or chains) over a vocabulary; tokens of a tree are raised so that some are accepted."""
+
+    def __init__(self, trees, vocab, dtype="f32", sampled=False, pad=0, extra=0, seed=0, heat=None, lift=3.0, back=3, chain=False):
+        rng = np.random.default_rng(seed)
+        self.off = np.concatenate([[0], np.cumsum(trees)]).astype(np.int64)
+        self.M, self.V, self.trees = int(self.off[-1]) + extra, vocab, trees
+        self.sees = []
+        for n in trees:
+            if sampled or chain or n == 0:
+                self.sees.append(A.chain(n))
+            else:
+                self.sees.append(A.ancestors([max(t - int(rng.integers(1, back + 1)), 0) if t else -1 for t in range(n)]))
+        logits = rng.standard_normal((self.M, vocab + pad)) * 2
+        self.tokens = rng.integers(0, vocab, self.M)
+        for s, see in enumerate(self.sees):
+            for t in range(1, len(see)):
+                parent = max(j for j in range(t) if see[t, j])
+                logits[self.off[s] + parent, self.tokens[self.off[s] + t]] = np.log(vocab) + lift + rng.uniform(-2, 1)
+        self.chain = sampled or chain
+        dt = TORCH[dtype]
+        self.logits = torch.from_numpy(logits).to(dt).cuda()[:, :vocab]
+        self.draft = None
+        if sampled:
+            self.draft = torch.from_numpy(logits + rng.standard_normal(logits.shape) * 0.7).to(dt).cuda()[:, :vocab]
+        self.u_accept, self.u_sample = rng.random(self.M), rng.random(len(trees))
+        self.heat = None if heat is None else np.asarray(heat, dtype=np.float32)
+        self.desc = mb.VerifyDesc(vocab, CODE[dtype])
+
+    def run(self, max_path=16, **kw):
+        most = max(max(self.trees), 1)
+        mask = None if self.chain else torch.from_numpy(A.pack(self.sees, self.M, most, fill=1)).cuda()
+        return mb.moespec_draft_verify(
+            self.desc, self.logits, i32(self.tokens), torch.from_numpy(self.u_accept).cuda(), torch.from_numpy(self.u_sample).cuda(), max_path,
+            draft_logits=self.draft, temperature=None if self.heat is None else torch.from_numpy(self.heat).cuda(),
+            tree_off=i32(self.off), tree_mask=mask, max_tree=most, **kw)
+
+    def check(self, got, max_path=16):
+        path, n_path, token, accepted = (got[k].cpu().numpy() for k in ("path", "n_path", "next_token", "accepted"))
+        logits, draft = f64(self.logits), None if self.draft is None else f64(self.draft)
+        on = np.zeros(self.M)
+        lengths = []
+        for s in range(len(self.trees)):
+            rows = slice(self.off[s], self.off[s + 1])
+            heat = 1.0 if self.heat is None else float(self.heat[s])
+            want, follows = V.verify(logits[rows], self.tokens[rows], self.sees[s], self.u_accept[rows], self.u_sample[s], max_path, heat,
+                                     None if draft is None else draft[rows])
+            assert n_path[s] == len(want) and path[s].tolist() == want + [-1] * (max_path - len(want)), (s, path[s], want)
+            assert token[s] == follows, (s, token[s], follows)
+            on[[self.off[s] + t for t in want]] = 1
+            lengths.append(len(want))
+        assert np.array_equal(accepted, on)
+        return lengths
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sampled", [False, True])
+def test_batches_of_trees_and_chains(dtype, sampled):
+    lengths = []
+    for seed in range(12):
+        trees = [[1], [2, 7], [30, 0, 1, 12], [63] * 3, [5] * 20][seed % 5]
+        b = Batch(trees, [1000, 4096, 4097, 12289, 777][seed % 5], dtype, sampled, pad=[0, 1, 8][seed % 3], extra=seed % 3, seed=seed,
+                  heat=None if seed % 2 else [[1.0, 0.7, 0.0, 1.5][i % 4] for i in range(len(trees))])
+        lengths += b.check(b.run())
+    assert max(lengths) > 3 and min(lengths) <= 1  # the walk was walked
+
+
+@pytest.mark.parametrize("vocab", [2, 3, 63, 64, 65, 1023, 4095, 4096, 4097, 65537, 262145])
+def test_vocabularies(vocab):
+    for sampled in (False, True):
+        b = Batch([9, 4], vocab, "bf16", sampled, pad=1, seed=vocab, lift=1.0)
+        b.check(b.run())
+
+
+def test_many_draws_of_the_same_rows():
+    """The next token over the whole range of its random number, through tokens without a weight."""
+    for sampled in (False, True):
+        for seed in range(40):
+            b = Batch([2] * 4, 9000, "f32", sampled, seed=seed, lift=0.0)
+            b.logits[:, 100:8000] = -float("inf")
+            b.u_sample = np.array([0.0, (seed + 0.5) / 40, 1 - 2.0 ** -53, seed / 40])
+            b.check(b.run())
+
+
+def test_children_in_order_and_the_same_token_twice():
+    b = Batch([6], 50, seed=3)
+    b.sees = [A.ancestors([-1, 0, 0, 0, 0, 2])]
+    b.tokens = np.array([0, 7, 9, 7, 11, 3])
+    b.logits[0] = 0
+    b.logits[0, 7], b.logits[0, 9], b.logits[0, 11] = 5.0, 4.0, 3.5
+    for first in (0.0, 0.9999):
+        for second in (0.0, 0.9999):
+            for third in (0.0, 0.9999):
+                b.u_accept = np.array([0.5, first, second, 0.0, third, 0.0])
+                for u in (0.0, 0.3, 0.7, 0.99):
+                    b.u_sample = np.array([u])
+                    b.check(b.run())
+
+
+def test_greedy_ties_go_to_the_lowest_token():
+    b = Batch([4, 4], 9000, "bf16", heat=[0.0, -1.0], seed=4)
+    b.logits[:, [77, 5000, 8999]] = 50.0
+    b.tokens[:] = 5000
+    assert b.check(b.run()) == [1, 1]
+    b.tokens[:] = 77
+    assert max(b.check(b.run())) > 1
+
+
+def test_paths_that_are_cut():
+    for max_path in (1, 2, 3):
+        b = Batch([30] * 6, 500, chain=True, seed=6, lift=9.0)
+        assert max(b.check(b.run(max_path), max_path)) == max_path
+
+
+def test_tokens_outside_of_the_vocabulary_are_rejected():
+    b = Batch([5, 5], 100, seed=7, lift=9.0, chain=True)
+    b.tokens[[1, 7]] = [-1, 100]
+    b.u_accept[:] = 0
+    assert b.check(b.run()) == [1, 2]
+
+
+@pytest.mark.parametrize("heat", [1.0, 0.0])
+def test_rows_that_are_no_distribution(heat):
+    """NaN, +inf and -inf alone, at the root, on the way and beside the path."""
+    for place in (0, 1, 3):
+        for value in (float("nan"), float("inf"), -float("inf")):
+            b = Batch([4], 5000, chain=True, seed=8, lift=12.0, heat=[heat])
+            b.u_accept[:] = 0.0
+            if value == -float("inf"):
+                b.logits[place] = value
+            else:
+                b.logits[place, 4500] = value
+            assert b.check(b.run()) == [place + 1] and int(b.run()["next_token"][0]) == -1
+
+
+def test_drafts_that_are_no_distribution_reject_their_token():
+    b = Batch([3], 5000, sampled=True, seed=9, lift=12.0)
+    b.draft[0, 17] = float("nan")
+    assert b.check(b.run()) == [1]
+    b.draft[0] = -float("inf")
+    assert b.check(b.run()) == [1]
+
+
+def test_drafters_that_are_the_target_and_their_opposite():
+    b = Batch([6] * 3, 3000, sampled=True, seed=10)
+    b.draft = b.logits.clone()
+    b.tokens[:] = 5
+    assert b.check(b.run()) == [6] * 3  # p = q: always accepted
+    b.logits[:, 1500:] = -float("inf")
+    b.draft[:, :1500] = -float("inf")
+    b.tokens[:] = 2000
+    assert b.check(b.run()) == [1] * 3
+
+
+def test_numbers_and_temperatures_out_of_range():
+    b = Batch([3] * 6, 700, seed=11, lift=1.0, heat=[1e-30, float("inf"), float("nan"), -float("inf"), 1e30, 2.0])
+    b.u_accept[:] = 0.999
+    b.u_sample = np.array([0.5, 0.25, 0.5, 0.5, 0.75, 0.1])
+    b.logits[:, 5] = -float("inf")
+    b.check(b.run())
+    b.heat = None
+    b.u_sample = np.array([float("nan"), -1.0, 1.0, 2.0, 0.5, 0.5])
+    got = b.run()["next_token"].cpu().numpy()
+    assert np.all((got >= 0) & (got < 700))
+
+
+def test_large_trees_and_their_limit():
+    b = Batch([4096, 300], 300, seed=12, lift=1.0, back=40)
+    b.check(b.run(64), 64)
+    b = Batch([700], 40000, "bf16", seed=13, chain=True, lift=8.0)
+    assert b.check(b.run(1000), 1000)[0] > 3
+
+
+def test_trees_cut_at_the_bound_and_rows_of_no_sequence():
+    b = Batch([8, 8], 600, seed=14, extra=3, chain=True, lift=9.0)
+    accepted = torch.full((19,), 5.0, device="cuda")
+    path, n = torch.empty((2, 6), dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+    token = torch.empty_like(n)
+    mb.DraftVerifyCall(b.desc, b.logits, i32(b.tokens), torch.from_numpy(b.u_accept).cuda(), torch.from_numpy(b.u_sample).cuda(), path, n,
+                       token, mb.alloc_verify_workspace(b.desc, 2, 19), accepted=accepted, tree_off=i32(b.off), max_tree=3)()
+    for s in range(2):
+        rows = slice(8 * s, 8 * s + 3)
+        want, follows = V.verify(f64(b.logits)[rows], b.tokens[rows], A.chain(3), b.u_accept[rows], b.u_sample[s], 6)
+        assert path[s].tolist() == want + [-1] * (6 - len(want)) and int(token[s]) == follows
+        assert torch.all(accepted[8 * s + 3:8 * s + 8] == 5)
+    assert torch.all(accepted[16:] == 5)
+
+
+def test_accepted_tokens_are_distributed_as_the_target():
+    """Chains of one drafted token: the first token behind the root, accepted or drawn, follows the target's distribution (chi square
+    of 30000 draws over 12 tokens, 11 degrees of freedom: above 40 once in 30000 such tests)."""
+    rng = np.random.default_rng(15)
+    n, vocab = 30000, 12
+    p, q = rng.standard_normal(vocab), rng.standard_normal(vocab)
+    for sampled in (True, False):
+        logits = torch.from_numpy(np.tile(p, (2 * n, 1))).float().cuda()
+        draft = torch.from_numpy(np.tile(q, (2 * n, 1))).float().cuda() if sampled else None
+        tokens = np.zeros(2 * n, dtype=np.int64)
+        tokens[1::2] = rng.choice(vocab, size=n, p=np.exp(q) / np.exp(q).sum())
+        got = mb.moespec_draft_verify(mb.VerifyDesc(vocab, mb.F32), logits, i32(tokens), torch.from_numpy(rng.random(2 * n)).cuda(),
+                                      torch.from_numpy(rng.random(n)).cuda(), 2, draft_logits=draft, tree_off=i32(np.arange(n + 1) * 2),
+                                      max_tree=2)
+        first = np.where(got["n_path"].cpu().numpy() == 2, tokens[1::2], got["next_token"].cpu().numpy())
+        want = np.exp(p) / np.exp(p).sum() * n
+        chi = ((np.bincount(first, minlength=vocab) - want) ** 2 / want).sum()
+        assert chi < 40, chi
+
+
+def test_graph_replays_and_a_shared_workspace():
+    b, c = Batch([20, 3], 6000, "bf16", seed=16), Batch([4, 6], 6000, "bf16", sampled=True, seed=17)
+    ws = mb.alloc_verify_workspace(b.desc, 2, 23, True)
+
+    def call(x):
+        out = dict(path=torch.zeros((2, 8), dtype=torch.int32, device="cuda"), n_path=i32([0, 0]), next_token=i32([0, 0]),
+                   accepted=torch.zeros(x.M, device="cuda"))
+        mask = None if x.chain else torch.from_numpy(A.pack(x.sees, x.M, max(x.trees), fill=1)).cuda()
+        u = torch.from_numpy(x.u_accept).cuda(), torch.from_numpy(x.u_sample).cuda()
+        return mb.DraftVerifyCall(x.desc, x.logits, i32(x.tokens), *u, out["path"], out["n_path"], out["next_token"], ws, x.draft,
+                                  accepted=out["accepted"], tree_off=i32(x.off), tree_mask=mask, max_tree=max(x.trees)), out, u
+    calls = [call(b), call(c)]
+    graphs, stream = [torch.cuda.CUDAGraph() for _ in calls], torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    rng = np.random.default_rng(18)
+    with torch.cuda.stream(stream):
+        for g, (run, _, _) in zip(graphs, calls):
+            with torch.cuda.graph(g, stream=stream):
+                run()
+        for _ in range(4):
+            for x, (_, out, u) in zip((b, c), calls):
+                x.u_accept, x.u_sample = rng.random(x.M), rng.random(2)
+                u[0].copy_(torch.from_numpy(x.u_accept)), u[1].copy_(torch.from_numpy(x.u_sample))
+                for t in out.values():
+                    t.fill_(3)
+            for g in graphs:
+                g.replay()
+            stream.synchronize()
+            for x, (_, out, _) in zip((b, c), calls):
+                x.check(out, 8)
