@@ -631,9 +631,9 @@ size_t moespec_verify_workspace_bytes(const moespec_verify *verify, int32_t n_se
  *                                          the accepted token that follows on it
  *   next_token [n_seq] int32 out           -1 for an empty tree
  *   accepted [M] float out                 1 for tokens of the path and 0 for others (a row_weight of moespec_cache_weights); may be NULL
- * Probabilities, sums and decisions are in fp64.  A row of logits with NaN or +inf, or of -inf alone, is no distribution: its children are
+ * Probabilities, sums and decisions are in fp64; a token below 2^-1022 of the largest has the probability 0.  A row of logits with NaN or +inf, or of -inf alone, is no distribution: its children are
  * rejected, and next_token is -1 where the path ends there; such a row of draft_logits rejects its token and leaves p as it is, as
- * does a difference p - q without anything above 0.  tree.q_stride and tree.kv_stride do not matter.
+ * does a difference p - q without anything above 0.  tree.max_tree is at most 2048; tree.q_stride and tree.kv_stride do not matter.
  */
 moespec_status moespec_draft_verify(const moespec_verify *verify, const moespec_tree *tree, const int32_t *tokens,
                                     const double *u_accept, const double *u_sample, int32_t *path, int32_t *n_path,

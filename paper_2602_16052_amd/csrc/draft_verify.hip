@@ -1,9 +1,10 @@
 // Verification of drafted tokens: from the target's logits and given random numbers to the accepted path and the next token.
 //
-// Two launches.  The first reads every row of logits once, which bounds it: largest logit and sum of exponentials of each chunk of a row
-// (which rows lie on the path is known only behind this).  The second, one workgroup a sequence, joins the chunks of its rows, walks
-// the tree in LDS, and draws the next token: the chunk in which the running sum passes its target is found from the chunks' sums, and only
-// that chunk is read again.  With a drafter's distribution the difference p - q of the last row is summed over chunks there too.
+// The first launch reads every row of logits once: largest logit and sum of exponentials of each chunk of a row (which rows lie on the
+// path is known only behind it).  The second, one workgroup a sequence, joins the chunks of its rows, walks the tree in LDS, and draws the
+// next token: the chunk in which the running sum passes its target is found from the chunks' sums, and only that chunk is read again.  With
+// a drafter's distribution the difference p - q of the last row is summed over its chunks by workgroups side by side, and a third
+// launch draws from it.
 // Probabilities are in fp64: accepting and drawing are decisions, and have to fall the same way whatever the order of the sums.
 #include "serving.h"
 
@@ -11,15 +12,20 @@ namespace moespec {
 
 namespace {
 
-constexpr int kChunk = 4096;       // logits of a workgroup's chunk
+constexpr int kChunk = kVerifyChunk;
 constexpr int kStatThreads = 256, kWalkThreads = 1024;
 constexpr int kEach = kChunk / kStatThreads;
 
-// A chunk of a row: largest logit, its first place, sum of exp((logit - largest) / temperature).
+// A chunk of a row: largest logit, its first place (greedy), sum of 2^((logit - largest) k).
 struct ChunkStat {
   double sum;
   float top;
   int arg;
+};
+
+// What the walk leaves for the draw from p - q: the path's last row, 0 where nothing is to be drawn.
+struct WalkEnd {
+  int row, draw;
 };
 
 struct VerifyArgs {
@@ -31,14 +37,41 @@ struct VerifyArgs {
   int32_t *path, *n_path, *next_token;
   float *accepted;
   ChunkStat *stats;  // [1 or 2 (draft)][M][chunks]
+  double *rest;      // [n_seq][chunks] sums of p - q (draft)
+  WalkEnd *ends;     // [n_seq] (draft)
   int64_t logit_stride, draft_stride;
   int V, chunks, n_seq, M, max_tree, words, max_path;
 };
 
-// 1 / temperature of a sequence; 0 where it is greedy.
-__device__ __forceinline__ double inverse_heat(const VerifyArgs &a, int s) {
+// log2(e) / temperature of a sequence: probabilities are 2^((logit - largest) k) over their sum.  0 where it is greedy.
+__device__ __forceinline__ double heat_of(const VerifyArgs &a, int s) {
   const float t = a.temperature ? a.temperature[s] : 1.f;
-  return t > 0.f ? 1.0 / (double)fminf(fmaxf(t, 0x1p-60f), 0x1p60f) : 0.0;
+  return t > 0.f ? 1.4426950408889634 / (double)fminf(fmaxf(t, 0x1p-60f), 0x1p60f) : 0.0;
+}
+
+// 2^t for t <= 0: t = n + r with |r| <= 1/2 (the sum with 1.5 * 2^52 rounds, and holds n in its low word), the polynomial of degree 10
+// through 2^r at the Chebyshev nodes (off by 3.2e-16 relative at most), n added to the exponent.  Below -1020: 2^-1020.  Drops a NaN.  19
+// instructions of the fp64 pipes with the logit's part: they, not the bytes, bound the sums of a row.
+__device__ __forceinline__ double exp2_sum(double t) {
+  const double c = fmax(t, -1020.0), shifted = c + 6755399441055744.0, r = c - (shifted - 6755399441055744.0);
+  double p = 7.072585949269223e-09;
+  p = fma(p, r, 1.0208690299958306e-07);
+  p = fma(p, r, 1.321544258792169e-06);
+  p = fma(p, r, 1.5252657260200837e-05);
+  p = fma(p, r, 0.0001540353044173605);
+  p = fma(p, r, 0.0013333558230164974);
+  p = fma(p, r, 0.009618129107606888);
+  p = fma(p, r, 0.05550410866444772);
+  p = fma(p, r, 0.24022650695910097);
+  p = fma(p, r, 0.69314718055995);
+  p = fma(p, r, 1.0);
+  return __hiloint2double(__double2hiint(p) + (__double2loint(shifted) << 20), __double2loint(p));
+}
+
+// The same for a single token: 0 below 2^-1022 and for -inf.  (Rows with NaN or +inf are told by their sums.)
+__device__ __forceinline__ double weight_of(float x, float top, double k) {
+  const double t = ((double)x - (double)top) * k;
+  return t < -1022.0 ? 0.0 : exp2_sum(t);
 }
 
 template <typename T>
@@ -46,21 +79,45 @@ __device__ __forceinline__ float logit_at(const void *row, int64_t i) {
   return Elem<T>::load(static_cast<const T *>(row) + i);
 }
 
-struct Best {
-  float top;
-  int arg;
-};
-__device__ __forceinline__ Best better(Best a, Best b) { return b.top > a.top || (b.top == a.top && b.arg < a.arg) ? b : a; }
-
-// exp((x - top) * inverse): 0 for -inf, NaN for NaN and for x = top = +inf.
-__device__ __forceinline__ double weight_of(float x, float top, double inverse) {
-  return x == -INFINITY ? 0.0 : exp_nonpos(((double)x - (double)top) * inverse);
+// Lane `l`'s value in every lane.
+__device__ __forceinline__ double from_lane(double v, int l) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), l), __builtin_amdgcn_readlane(__double2loint(v), l));
 }
-
 __device__ __forceinline__ double wave_sum64(double v) {
   v = row16_sum(v);
-  v += __shfl_xor(v, 16, kWave);
-  return v + __shfl_xor(v, 32, kWave);
+  return (from_lane(v, 0) + from_lane(v, 16)) + (from_lane(v, 32) + from_lane(v, 48));
+}
+__device__ __forceinline__ float row16_top(float v) {
+  auto step = [&](auto ctrl) {
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false)));
+  };
+  step(std::integral_constant<int, kDppXor1>{});
+  step(std::integral_constant<int, kDppXor2>{});
+  step(std::integral_constant<int, kDppHalfMirror>{});
+  step(std::integral_constant<int, kDppMirror>{});
+  return v;
+}
+__device__ __forceinline__ float wave_top(float v) {
+  v = row16_top(v);
+  auto of = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+  return fmaxf(fmaxf(of(0), of(16)), fmaxf(of(32), of(48)));
+}
+// Sum of the lanes up to this one: rows of 16 by shifts, then the rows in front.
+template <int N>
+__device__ __forceinline__ double add_from_below(double v) {  // v of lane - N of the same row of 16, 0 where there is none
+  constexpr int kShift = 0x110 + N;
+  const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), kShift, 0xf, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), kShift, 0xf, 0xf, false);
+  return v + __hiloint2double(hi, lo);
+}
+__device__ __forceinline__ double wave_scan64(double v) {
+  v = add_from_below<1>(v);
+  v = add_from_below<2>(v);
+  v = add_from_below<4>(v);
+  v = add_from_below<8>(v);
+  const double r0 = from_lane(v, 15), r1 = r0 + from_lane(v, 31), r2 = r1 + from_lane(v, 47);
+  const int row = (threadIdx.x & 63) >> 4;
+  return v + (row == 0 ? 0.0 : row == 1 ? r0 : row == 2 ? r1 : r2);
 }
 
 // kVec: rows start at multiples of 16 bytes.
@@ -72,167 +129,318 @@ __global__ __launch_bounds__(kStatThreads) void logit_stats_kernel(VerifyArgs a)
   const T *x = static_cast<const T *>(draft ? a.draft : a.logits) + (int64_t)row * (draft ? a.draft_stride : a.logit_stride);
   const int base = chunk * kChunk;
   float v[kEach];
-  int at[kEach];
+  auto place = [&](int i) {  // of this thread's value i
+    return kVec ? base + (i / E * kStatThreads + (int)threadIdx.x) * E + i % E : base + i * kStatThreads + (int)threadIdx.x;
+  };
   if constexpr (kVec) {
 #pragma unroll
-    for (int i = 0; i < kEach / E; ++i) {
-      const int j = base + (i * kStatThreads + (int)threadIdx.x) * E;
+    for (int i = 0; i < kEach; i += E) {
+      const int j = place(i);
       if (j + E <= a.V) {
 #pragma unroll
         for (int e = 0; e < E; e += 4) {
           const f32x4 f = Elem<T>::load4(x + j + e);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[i * E + e + k] = f[k];
+          for (int k = 0; k < 4; ++k) v[i + e + k] = f[k];
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[i * E + e] = j + e < a.V ? Elem<T>::load(x + j + e) : -INFINITY;
+        for (int e = 0; e < E; ++e) v[i + e] = j + e < a.V ? Elem<T>::load(x + j + e) : -INFINITY;
       }
-#pragma unroll
-      for (int e = 0; e < E; ++e) at[i * E + e] = j + e;
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      at[i] = base + i * kStatThreads + (int)threadIdx.x;
-      v[i] = at[i] < a.V ? Elem<T>::load(x + at[i]) : -INFINITY;
-    }
+    for (int i = 0; i < kEach; ++i) v[i] = place(i) < a.V ? Elem<T>::load(x + place(i)) : -INFINITY;
   }
   const int s = seq_of_row(a.tree_off, a.n_seq, row);
   if (s >= a.n_seq) return;
-  const double inverse = inverse_heat(a, s);
-  __shared__ Best best_of[kStatThreads / kWave];
+  const double k = heat_of(a, s);
+  __shared__ float top_of[kStatThreads / kWave];
   __shared__ double sum_of[kStatThreads / kWave];
-  Best b{v[0], at[0]};
+  __shared__ int arg_of[kStatThreads / kWave];
+  float top = -INFINITY;
+  bool nan = false;
 #pragma unroll
-  for (int i = 1; i < kEach; ++i)
-    if (v[i] > b.top) b = Best{v[i], at[i]};  // (places ascend)
-  if (!(b.top >= -INFINITY)) {  // the first one is NaN: the comparisons above have all been false
-    b.top = -INFINITY;
-#pragma unroll
-    for (int i = 1; i < kEach; ++i)
-      if (v[i] > b.top) b = Best{v[i], at[i]};
+  for (int i = 0; i < kEach; ++i) {
+    top = fmaxf(top, v[i]);
+    nan |= v[i] != v[i];
   }
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) b = better(b, Best{__shfl_xor(b.top, m, kWave), __shfl_xor(b.arg, m, kWave)});
-  if (lane == 0) best_of[wave] = b;
+  top = wave_top(top);
+  if (lane == 0) top_of[wave] = top;
   __syncthreads();
-  b = best_of[0];
 #pragma unroll
-  for (int w = 1; w < kStatThreads / kWave; ++w) b = better(b, best_of[w]);
+  for (int w = 0; w < kStatThreads / kWave; ++w) top = fmaxf(top, top_of[w]);
+  nan |= top == INFINITY;
   double sum = 0.0;
-  if (inverse > 0.0) {
+  int arg = 0x7fffffff;
+  if (k > 0.0) {
+    if (top > -INFINITY && top < INFINITY) {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) sum += weight_of(v[i], b.top, inverse);
-  } else {  // greedy: whether the row is a distribution
+      for (int i = 0; i < kEach; ++i) sum += exp2_sum(((double)v[i] - (double)top) * k);
+    }
+  } else {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) sum += v[i] < INFINITY ? (v[i] == b.top && v[i] > -INFINITY ? 1.0 : 0.0) : __builtin_nan("");
+    for (int i = 0; i < kEach; ++i)
+      if (v[i] == top) arg = min(arg, place(i));
+#pragma unroll
+    for (int m = 1; m < kWave; m <<= 1) arg = min(arg, __shfl_xor(arg, m, kWave));
+    sum = top > -INFINITY ? 1.0 : 0.0;
   }
+  if (nan) sum = __builtin_nan("");
   sum = wave_sum64(sum);
-  if (lane == 0) sum_of[wave] = sum;
+  if (lane == 0) {
+    sum_of[wave] = sum;
+    arg_of[wave] = arg;
+  }
   __syncthreads();
   if (threadIdx.x == 0) {
-    double total = sum_of[0];
-    for (int w = 1; w < kStatThreads / kWave; ++w) total += sum_of[w];
-    a.stats[((int64_t)blockIdx.z * a.M + row) * a.chunks + chunk] = ChunkStat{total, b.top, b.arg};
+    for (int w = 1; w < kStatThreads / kWave; ++w) {
+      sum += sum_of[w];
+      arg = min(arg, arg_of[w]);
+    }
+    a.stats[((int64_t)blockIdx.z * a.M + row) * a.chunks + chunk] = ChunkStat{sum, top, arg};
   }
 }
 
-// A whole row from its chunks: largest logit, its first place, sum; a row that is no distribution has the sum NaN.  All lanes of a wave
-// work on one row and end with the same bits.
+// A whole row from its chunks, by the 16 lanes of a row of lanes (kWide: by a wave); all of them end with the same bits.  A row of logits
+// that is no distribution has the sum NaN.
 struct RowStat {
   double sum;
   float top;
   int arg;
 };
-__device__ __forceinline__ RowStat join_chunks(const ChunkStat *c, int chunks, double inverse) {
-  const int lane = threadIdx.x & 63;
-  Best b{-INFINITY, 0x7fffffff};
-  for (int i = lane; i < chunks; i += kWave) b = better(b, Best{c[i].top, c[i].arg});
+template <bool kWide>
+__device__ __forceinline__ RowStat join_chunks(const ChunkStat *c, int chunks, double k) {
+  constexpr int kLanes = kWide ? kWave : 16;
+  const int first = threadIdx.x & (kLanes - 1);
+  ChunkStat mine{0.0, -INFINITY, 0x7fffffff};
+  if (first < chunks) mine = c[first];
+  float top = mine.top;
+  int arg = mine.arg;
+  if constexpr (kWide)
+    for (int i = first + kLanes; i < chunks; i += kLanes) {
+      const ChunkStat x = c[i];
+      if (x.top > top) {  // (places ascend)
+        top = x.top;
+        arg = x.arg;
+      }
+    }
+  const float mine_top = top;
+  top = kWide ? wave_top(top) : row16_top(top);
+  if (k == 0.0) {
+    arg = mine_top == top ? arg : 0x7fffffff;
 #pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) b = better(b, Best{__shfl_xor(b.top, m, kWave), __shfl_xor(b.arg, m, kWave)});
-  double sum = 0.0;
-  for (int i = lane; i < chunks; i += kWave) sum += c[i].sum * weight_of(c[i].top, b.top, inverse);
-  sum = wave_sum64(sum);
-  return RowStat{sum > 0.0 && sum < INFINITY ? sum : __builtin_nan(""), b.top, b.arg};
+    for (int m = 1; m < kLanes; m <<= 1) arg = min(arg, __shfl_xor(arg, m, kWave));
+  }
+  double sum = mine.sum * weight_of(mine.top, top, k);
+  if constexpr (kWide) {
+    for (int i = first + kLanes; i < chunks; i += kLanes) sum += c[i].sum * weight_of(c[i].top, top, k);
+    sum = wave_sum64(sum);
+  } else {
+    sum = row16_sum(sum);
+  }
+  return RowStat{sum > 0.0 && sum < INFINITY ? sum : __builtin_nan(""), top, arg};
 }
 
-// What the last row's tokens weigh: p, without the tokens in `gone`; or what p has over q.
+// What the last row's tokens weigh: p, or what p has over q.
 template <typename T>
 struct Rest {
-  const VerifyArgs *a;
-  const void *p, *q;  // q NULL: p without the tokens that are gone
+  const void *p, *q;  // q NULL: p
   RowStat ps, qs;
-  double inverse, p_scale, q_scale;
-  const int32_t *gone;  // LDS: tokens that are gone
+  double k, p_scale, q_scale;
+  const int32_t *gone;  // LDS: tokens that weigh nothing
   int n_gone;
+  __device__ __forceinline__ double of(float x, float y) const {
+    const double w = weight_of(x, ps.top, k);
+    return q ? fmax(w * p_scale - weight_of(y, qs.top, k) * q_scale, 0.0) : w;
+  }
   __device__ __forceinline__ double operator()(int i) const {
-    double w = weight_of(logit_at<T>(p, i), ps.top, inverse) * p_scale;
-    if (q) w = fmax(w - weight_of(logit_at<T>(q, i), qs.top, inverse) * q_scale, 0.0);
-    for (int k = 0; k < n_gone; ++k) w = gone[k] == i ? 0.0 : w;
+    double w = of(logit_at<T>(p, i), q ? logit_at<T>(q, i) : 0.f);
+    for (int j = 0; j < n_gone; ++j) w = gone[j] == i ? 0.0 : w;
     return w;
   }
 };
 
+struct WalkShared {
+  double scan[kWalkThreads / kWave];
+  int hit[kWalkThreads / kWave], some[kWalkThreads / kWave];
+  int last, n_gone, next, found;
+};
+
+// Sum of v over the workgroup, the same bits in every thread.
+__device__ __forceinline__ double group_sum64(double v, double *scan) {
+  v = wave_sum64(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) scan[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return wave_sum64((threadIdx.x & 63) < kWalkThreads / kWave ? scan[threadIdx.x & (kWalkThreads / kWave - 1)] : 0.0);
+}
+
+// The next token of sequence s from its chunks' sums (LDS) of what is left.
 template <typename T>
-__global__ __launch_bounds__(kWalkThreads) void draft_walk_kernel(VerifyArgs a) {
+__device__ __forceinline__ void draw_token(const VerifyArgs &a, int s, const Rest<T> &rest, const double *chunk_sum, WalkShared &sh) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   constexpr int kWaves = kWalkThreads / kWave;
+  const double u = a.u_sample[s];
+  double total = 0.0;
+  for (int c = 0; c < a.chunks; c += kWave) total += wave_sum64(c + lane < a.chunks ? chunk_sum[c + lane] : 0.0);
+  const double goal = (u > 0.0 ? fmin(u, 1.0) : 0.0) * total;  // (NaN: 0)
+  double before = 0.0;
+  int chunk = -1, most = 0;  // most: the last chunk with anything
+  for (int c = 0; c < a.chunks && chunk < 0; c += kWave) {
+    const double v = c + lane < a.chunks ? chunk_sum[c + lane] : 0.0, sum = wave_scan64(v);
+    const uint64_t hit = __ballot(before + sum > goal && v > 0.0), some = __ballot(v > 0.0);
+    if (hit != 0) {
+      const int f = __builtin_ctzll(hit);
+      chunk = c + f;
+      before += f > 0 ? from_lane(sum, f - 1) : 0.0;
+    } else {
+      before += from_lane(sum, 63);
+    }
+    if (some != 0) most = c + 63 - __clzll((long long)some);
+  }
+  const bool past = chunk < 0;  // lost to rounding: the last token with a weight
+  if (past) chunk = most;
+  // the chunk's tokens: kChunk / kWalkThreads in a row to a thread
+  constexpr int N = kChunk / kWalkThreads;
+  double w[N], sum = 0.0;
+  float x[N], y[N] = {};
+  const int first = chunk * kChunk + (int)threadIdx.x * N;
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = logit_at<T>(rest.p, min(first + i, a.V - 1));
+  if (rest.q) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = logit_at<T>(rest.q, min(first + i, a.V - 1));
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = first + i < a.V ? rest.of(x[i], y[i]) : 0.0;
+  for (int j = 0; j < rest.n_gone; ++j) {
+    const int at = rest.gone[j] - first;
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = at == i ? 0.0 : w[i];
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum += w[i];
+  const double scan = wave_scan64(sum);
+  __syncthreads();
+  if (lane == 63) sh.scan[wave] = scan;
+  __syncthreads();
+  const double waves = wave_scan64(lane < kWaves ? sh.scan[min(lane, kWaves - 1)] : 0.0);
+  if (wave > 0) before += from_lane(waves, wave - 1);
+  double run = before + scan - sum;
+  int mine = -1, positive = -1;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    run += w[i];
+    if (w[i] > 0.0) {
+      positive = first + i;
+      if (mine < 0 && run > goal) mine = first + i;
+    }
+  }
+  // threads hold ascending places: the first hit, and the last token with a weight
+  const uint64_t hits = __ballot(mine >= 0 && !past), some = __ballot(positive >= 0);
+  if (lane == 0) {
+    sh.hit[wave] = hits ? __builtin_amdgcn_readlane(mine, __builtin_ctzll(hits)) : -1;
+    sh.some[wave] = some ? __builtin_amdgcn_readlane(positive, 63 - __clzll((long long)some)) : -1;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    const int h = lane < kWaves ? sh.hit[lane] : -1, p = lane < kWaves ? sh.some[lane] : -1;
+    const uint64_t hb = __ballot(h >= 0), pb = __ballot(p >= 0);
+    const int token = hb ? __builtin_amdgcn_readlane(h, __builtin_ctzll(hb)) : pb ? __builtin_amdgcn_readlane(p, 63 - __clzll((long long)pb)) : -1;
+    if (lane == 0) a.next_token[s] = token;
+  }
+}
+
+// The walk of sequence blockIdx.y.  kSampled: with a drafter's distribution; the workgroups of a sequence then all walk its chain, and
+// sum p - q over chunks of the last row between them; the draw follows in draft_draw_kernel.
+template <typename T, bool kSampled, bool kWide>
+__global__ __launch_bounds__(kWalkThreads) void draft_walk_kernel(VerifyArgs a) {
+  constexpr int lanes = kWide ? kWave : 16;
   extern __shared__ __align__(16) unsigned char lds[];
-  // [max_tree] each: probability of the token behind its parent (times q in u's place: see below), token, parent, rejected tokens
-  double *const mine = reinterpret_cast<double *>(lds);
-  int32_t *const token = reinterpret_cast<int32_t *>(mine + a.max_tree);
-  int32_t *const parent = token + a.max_tree;
-  int32_t *const gone = parent + a.max_tree;
-  double *const chunk_sum = reinterpret_cast<double *>(gone + a.max_tree + (a.max_tree & 1));  // [chunks]
-  __shared__ double scan_of[kWaves];
-  __shared__ int last_s, n_gone_s, next_s, found_s;
-  const int s = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // [max_tree] each: probability of a token behind its parent, its random number, the row's sum, its largest logit, token, parent, and
+  // the place of the largest logit (greedy) or the list of tokens that are gone (else); sampled: sum and largest logit of the drafter's
+  // row.  [chunks]: sums
+  double *const mine = reinterpret_cast<double *>(lds), *const number = mine + a.max_tree, *const row_sum = number + a.max_tree;
+  float *const row_top = reinterpret_cast<float *>(row_sum + a.max_tree);
+  int32_t *const token = reinterpret_cast<int32_t *>(row_top + a.max_tree), *const parent = token + a.max_tree;
+  int32_t *const gone = parent + a.max_tree, *const row_arg = gone;
+  double *const chunk_sum = reinterpret_cast<double *>(gone + a.max_tree), *const draft_sum = chunk_sum;  // (one or the other)
+  float *const draft_top = reinterpret_cast<float *>(draft_sum + a.max_tree);
+  __shared__ WalkShared sh;
+  const int s = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool first_group = blockIdx.x == 0;
   const SeqRows g = seq_rows(a.tree_off, s, a.M, a.max_tree);
+  const double k = heat_of(a, s);
+  const bool greedy = k == 0.0, sampled = kSampled && !greedy;
   int32_t *const path = a.path + (int64_t)s * a.max_path;
-  if (a.accepted)
-    for (int t = threadIdx.x; t < g.T; t += kWalkThreads) a.accepted[g.row0 + t] = t == 0 ? 1.f : 0.f;
-  for (int i = threadIdx.x; i < a.max_path; i += kWalkThreads) path[i] = i == 0 && g.T > 0 ? 0 : -1;
   if (g.T == 0) {
-    if (threadIdx.x == 0) {
-      a.n_path[s] = 0;
-      a.next_token[s] = -1;
+    if (first_group) {
+      for (int i = threadIdx.x; i < a.max_path; i += kWalkThreads) path[i] = -1;
+      if (threadIdx.x == 0) {
+        a.n_path[s] = 0;
+        a.next_token[s] = -1;
+        if (kSampled) a.ends[s] = WalkEnd{0, 0};
+      }
     }
     return;
   }
-  const double inverse = inverse_heat(a, s);
-  const bool greedy = inverse == 0.0, sampled = a.draft != nullptr && !greedy;
-  for (int t = threadIdx.x; t < g.T; t += kWalkThreads) {
-    int p = t - 1;
-    if (a.tree_mask && t > 0) {
-      p = -1;
-      for (int w = t >> 5; w >= 0 && p < 0; --w) {
-        const uint32_t bits = a.tree_mask[(int64_t)(g.row0 + t) * a.words + w] & keys_below(t - 32 * w);
-        if (bits) p = 32 * w + 31 - __clz((int)bits);
-      }
-    }
-    parent[t] = p;  // -1: of no token's
-    token[t] = a.tokens[g.row0 + t];
-  }
-  __syncthreads();
-  // every token's probability, a wave per token; the rows of the parents are joined where they are needed
-  for (int t = 1 + wave; t < g.T; t += kWaves) {
-    const int u = parent[t], x = token[t];
-    double p = 0.0;
-    if (u >= 0 && x >= 0 && x < a.V) {
-      const int64_t row = g.row0 + u;
-      const RowStat r = join_chunks(a.stats + row * a.chunks, a.chunks, inverse);
-      if (greedy) {
-        p = r.sum > 0.0 && r.arg == x ? 1.0 : 0.0;
-      } else if (r.sum > 0.0) {
-        p = weight_of(logit_at<T>(static_cast<const T *>(a.logits) + row * a.logit_stride, x), r.top, inverse) / r.sum;
-        if (sampled) {
-          const RowStat d = join_chunks(a.stats + (a.M + row) * a.chunks, a.chunks, inverse);
-          const double q = weight_of(logit_at<T>(static_cast<const T *>(a.draft) + row * a.draft_stride, x), d.top, inverse) / d.sum;
-          p = a.u_accept[row + 1] * q < p ? 2.0 : 0.0;  // (a chain: decided here.  NaN is no)
+  // tokens, their parents and logits (of a sampled chain the drafter's too), before the rows are joined: loads that wait for none of that
+  for (int t0 = 0; t0 < g.T; t0 += kWalkThreads) {
+    const int t = t0 + (int)threadIdx.x;
+    if (t < g.T) {
+      int p = t - 1;
+      if (!kSampled && a.tree_mask && t > 0) {
+        p = -1;
+        const uint32_t *words = a.tree_mask + (int64_t)(g.row0 + t) * a.words;
+        for (int w = (t - 1) >> 5; w >= 0 && p < 0; w -= 2) {
+          const uint32_t high = words[w] & keys_below(t - 32 * w), low = w > 0 ? words[w - 1] : 0;
+          if (high) p = 32 * w + 31 - __clz((int)high);
+          else if (low) p = 32 * (w - 1) + 31 - __clz((int)low);
         }
       }
+      const int x = a.tokens[g.row0 + t];
+      const bool ok = p >= 0 && x >= 0 && x < a.V;
+      parent[t] = p;  // -1: of no token's
+      token[t] = x;
+      number[t] = greedy ? 0.5 : a.u_accept[g.row0 + t];
+      float l[2] = {-INFINITY, -INFINITY};
+      if (ok && !greedy) {
+        l[0] = logit_at<T>(static_cast<const T *>(a.logits) + (int64_t)(g.row0 + p) * a.logit_stride, x);
+        if (kSampled) l[1] = logit_at<T>(static_cast<const T *>(a.draft) + (int64_t)(g.row0 + p) * a.draft_stride, x);
+      }
+      mine[t] = __hiloint2double(__float_as_int(l[0]), __float_as_int(l[1]));  // until the rows are there
+      if (first_group && a.accepted) a.accepted[g.row0 + t] = t == 0 ? 1.f : 0.f;
     }
-    if (lane == 0) mine[t] = p;
+  }
+  if (first_group)
+    for (int i = threadIdx.x; i < a.max_path; i += kWalkThreads) path[i] = i == 0 ? 0 : -1;
+  for (int u = threadIdx.x / lanes; u < g.T; u += kWalkThreads / lanes) {
+    const RowStat r = join_chunks<kWide>(a.stats + (int64_t)(g.row0 + u) * a.chunks, a.chunks, k);
+    if ((threadIdx.x & (lanes - 1)) == 0) {
+      row_sum[u] = r.sum;
+      row_top[u] = r.top;
+      if (greedy) row_arg[u] = r.arg;
+    }
+    if (sampled) {
+      const RowStat d = join_chunks<kWide>(a.stats + (int64_t)(a.M + g.row0 + u) * a.chunks, a.chunks, k);
+      if ((threadIdx.x & (lanes - 1)) == 0) {
+        draft_sum[u] = d.sum;
+        draft_top[u] = d.top;
+      }
+    }
+  }
+  __syncthreads();
+  for (int t = threadIdx.x; t < g.T; t += kWalkThreads) {
+    const int u = parent[t];
+    double p = 0.0;
+    if (u >= 0 && row_sum[u] > 0.0)
+      p = greedy ? (row_arg[u] == token[t] ? 1.0 : 0.0) : weight_of(__int_as_float(__double2hiint(mine[t])), row_top[u], k) / row_sum[u];
+    if (sampled) {  // a chain: decided here (NaN is no)
+      const double q = u >= 0 ? weight_of(__int_as_float(__double2loint(mine[t])), draft_top[u], k) / draft_sum[u] : 0.0;
+      p = number[t] * q < p ? INFINITY : 0.0;
+    }
+    mine[t] = p;
   }
   __syncthreads();
   // the walk, one wave
@@ -249,13 +457,13 @@ __global__ __launch_bounds__(kWalkThreads) void draft_walk_kernel(VerifyArgs a) 
         for (; kids != 0 && step < 0; kids &= kids - 1) {
           const int t = base + __builtin_ctzll(kids), x = token[t];
           bool again = false;  // a token that has been rejected already
-          for (int k = lane; k < n_gone; k += kWave) again |= gone[k] == x;
+          for (int i = lane; i < n_gone; i += kWave) again |= gone[i] == x;
           if (__ballot(again) != 0) continue;
           const double p = mine[t];
-          const double u = greedy || sampled ? 0.5 : a.u_accept[g.row0 + t];
-          if (u * (1.0 - left) < p) {
+          if (number[t] * (1.0 - left) < p) {
             step = t;
           } else {
+            if (greedy) continue;
             left += p;
             if (lane == 0) gone[n_gone] = x;
             ++n_gone;
@@ -271,136 +479,123 @@ __global__ __launch_bounds__(kWalkThreads) void draft_walk_kernel(VerifyArgs a) 
         break;
       }
       last = step;
-      if (lane == 0) {
+      if (lane == 0 && first_group) {
         path[length] = step;
         if (a.accepted) a.accepted[g.row0 + step] = 1.f;
       }
       ++length;
     }
     if (lane == 0) {
-      a.n_path[s] = length;
-      last_s = last;
-      n_gone_s = n_gone;
-      next_s = cut ? next : -1;
-      found_s = cut;
+      if (first_group) a.n_path[s] = length;
+      sh.last = last;
+      sh.n_gone = n_gone;
+      sh.next = next;
+      sh.found = cut;
     }
   }
   __syncthreads();
-  const int64_t row = g.row0 + last_s;
-  const RowStat ps = join_chunks(a.stats + row * a.chunks, a.chunks, inverse);
-  if (found_s || !(ps.sum > 0.0) || greedy) {
-    if (threadIdx.x == 0) a.next_token[s] = found_s ? next_s : ps.sum > 0.0 ? ps.arg : -1;
-    return;
+  const int64_t row = g.row0 + sh.last;
+  const RowStat ps{row_sum[sh.last], row_top[sh.last], greedy ? row_arg[sh.last] : 0};
+  const bool done = sh.found || !(ps.sum > 0.0) || greedy;
+  if (first_group && threadIdx.x == 0) {
+    if (done) a.next_token[s] = sh.found ? sh.next : ps.sum > 0.0 ? ps.arg : -1;
+    if (kSampled) a.ends[s] = WalkEnd{(int)row, done ? 0 : sh.n_gone > 0 ? 2 : 1};
   }
-  Rest<T> rest{&a, static_cast<const T *>(a.logits) + row * a.logit_stride, nullptr, ps, RowStat{}, inverse, 1.0, 0.0, gone, n_gone_s};
-  if (sampled) {
-    rest.n_gone = 0;
-    if (n_gone_s > 0) {
-      rest.qs = join_chunks(a.stats + (a.M + row) * a.chunks, a.chunks, inverse);
-      if (rest.qs.sum > 0.0) {
-        rest.q = static_cast<const T *>(a.draft) + row * a.draft_stride;
-        rest.p_scale = 1.0 / ps.sum;
-        rest.q_scale = 1.0 / rest.qs.sum;
-      }
-    }
-  }
-  // sums of the chunks of what is left; where there is nothing, of p itself
-  auto whole_chunks = [&]() {
-    for (int c = threadIdx.x; c < a.chunks; c += kWalkThreads) {
-      const ChunkStat st = a.stats[row * a.chunks + c];
-      chunk_sum[c] = st.sum * weight_of(st.top, ps.top, inverse);
-    }
-  };
-  auto some_left = [&]() {
-    bool any = false;
-    for (int c = lane; c < a.chunks; c += kWave) any |= chunk_sum[c] > 0.0;
-    return __ballot(any) != 0;
-  };
-  if (rest.q || rest.n_gone > 0) {
-    for (int c = wave; c < a.chunks; c += kWaves) {
+  if (done) return;
+  Rest<T> rest{static_cast<const T *>(a.logits) + row * a.logit_stride, nullptr, ps, RowStat{}, k, 1.0, 0.0, gone, 0};
+  if constexpr (kSampled) {
+    if (sh.n_gone == 0) return;
+    rest.qs = RowStat{draft_sum[sh.last], draft_top[sh.last], 0};
+    const bool some = rest.qs.sum > 0.0;  // else: p as it is
+    rest.q = static_cast<const T *>(a.draft) + row * a.draft_stride;
+    rest.p_scale = 1.0 / ps.sum;
+    rest.q_scale = 1.0 / rest.qs.sum;
+    for (int c = blockIdx.x; c < a.chunks; c += gridDim.x) {
       double sum = 0.0;
-      for (int i = c * kChunk + lane; i < min((c + 1) * kChunk, a.V); i += kWave) sum += rest(i);
-      sum = wave_sum64(sum);
-      if (lane == 0) chunk_sum[c] = sum;
-    }
-    __syncthreads();
-    if (!some_left()) {
-      __syncthreads();
-      rest.q = nullptr;
-      rest.n_gone = 0;
-      rest.p_scale = 1.0;
-      whole_chunks();
+      if (some)
+        for (int i = c * kChunk + (int)threadIdx.x; i < min((c + 1) * kChunk, a.V); i += kWalkThreads) sum += rest(i);
+      sum = group_sum64(sum, sh.scan);
+      if (threadIdx.x == 0) a.rest[(int64_t)s * a.chunks + c] = sum;
     }
   } else {
-    whole_chunks();
-  }
-  __syncthreads();
-  // the running sum over chunks, by every wave for itself
-  double total = 0.0;
-  for (int c = 0; c < a.chunks; c += kWave) {
-    double v = c + lane < a.chunks ? chunk_sum[c + lane] : 0.0;
-    total += wave_sum64(v);
-  }
-  const double u = a.u_sample[s];
-  const double goal = (u > 0.0 ? fmin(u, 1.0) : 0.0) * total;  // (NaN: 0)
-  double before = 0.0;
-  int chunk = -1, most = -1;  // most: the last chunk with anything
-  for (int c = 0; c < a.chunks && chunk < 0; c += kWave) {
-    const double v = c + lane < a.chunks ? chunk_sum[c + lane] : 0.0;
-    double sum = v;
-#pragma unroll
-    for (int m = 1; m < kWave; m <<= 1) {
-      const double up = __shfl_up(sum, m, kWave);
-      if (lane >= m) sum += up;
+    const int n_gone = rest.n_gone = sh.n_gone;
+    auto whole = [&](int c) {
+      const ChunkStat st = a.stats[row * a.chunks + c];
+      return st.sum * weight_of(st.top, ps.top, k);
+    };
+    // The sums of the chunks without the tokens that are gone.  Where these leave less than 2^-10 of a chunk, it is summed again: the
+    // difference would have lost ten bits.
+    uint64_t again = 0;
+    for (int c0 = 0; c0 < a.chunks; c0 += kWalkThreads) {
+      const int c = c0 + (int)threadIdx.x;
+      if (c < a.chunks) {
+        const double all = whole(c);
+        double sum = all;
+        for (int j = 0; j < n_gone; ++j)
+          if (gone[j] >= 0 && gone[j] < a.V && gone[j] / kChunk == c)
+            sum -= weight_of(logit_at<T>(rest.p, gone[j]), ps.top, k);
+        const bool lost = sum < all * 0x1p-10;
+        chunk_sum[c] = lost ? -1.0 : sum;
+      }
     }
-    const uint64_t hit = __ballot(before + sum > goal && v > 0.0), some = __ballot(v > 0.0);
-    if (hit != 0) {
-      const int f = __builtin_ctzll(hit);
-      chunk = c + f;
-      before += __shfl(sum, f, kWave) - __shfl(v, f, kWave);
-    } else {
-      before += __shfl(sum, 63, kWave);
+    __syncthreads();
+    for (int c0 = 0; c0 < a.chunks && n_gone > 0; c0 += kWave) {
+      again = __ballot(c0 + lane < a.chunks && chunk_sum[min(c0 + lane, a.chunks - 1)] < 0.0);
+      __syncthreads();
+      for (; again != 0; again &= again - 1) {
+        const int c = c0 + __builtin_ctzll(again);
+        double sum = 0.0;
+        for (int i = c * kChunk + (int)threadIdx.x; i < min((c + 1) * kChunk, a.V); i += kWalkThreads) sum += rest(i);
+        sum = group_sum64(sum, sh.scan);
+        if (threadIdx.x == 0) chunk_sum[c] = sum;
+      }
     }
-    if (some != 0) most = c + 63 - __clzll((long long)some);
-  }
-  const bool past = chunk < 0;  // lost to rounding: the last token with a weight
-  if (past) chunk = most;
-  // the chunk's tokens: kChunk / kWalkThreads in a row to a thread
-  constexpr int N = kChunk / kWalkThreads;
-  double w[N], sum = 0.0;
-  const int first = chunk * kChunk + (int)threadIdx.x * N;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    w[i] = chunk >= 0 && first + i < a.V ? rest(first + i) : 0.0;
-    sum += w[i];
-  }
-  double scan = sum;
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) {
-    const double up = __shfl_up(scan, m, kWave);
-    if (lane >= m) scan += up;
-  }
-  if (lane == 63) scan_of[wave] = scan;
-  if (threadIdx.x == 0) {
-    found_s = 0x7fffffff;
-    next_s = -1;
-  }
-  __syncthreads();
-  for (int k = 0; k < wave; ++k) before += scan_of[k];
-  double run = before + scan - sum;
-  int mine_is = 0x7fffffff, positive = -1;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    run += w[i];
-    if (w[i] > 0.0) {
-      positive = first + i;
-      if (!past && run > goal && mine_is == 0x7fffffff) mine_is = first + i;
+    __syncthreads();
+    bool any = false;
+    for (int c = lane; c < a.chunks; c += kWave) any |= chunk_sum[c] > 0.0;
+    if (__ballot(any) == 0) {  // nothing: p as it is
+      __syncthreads();
+      rest.n_gone = 0;
+      for (int c = threadIdx.x; c < a.chunks; c += kWalkThreads) chunk_sum[c] = whole(c);
+      __syncthreads();
     }
+    draw_token(a, s, rest, chunk_sum, sh);
   }
-  if (mine_is != 0x7fffffff) atomicMin(&found_s, mine_is);
-  if (positive >= 0) atomicMax(&next_s, positive);
-  __syncthreads();
-  if (threadIdx.x == 0) a.next_token[s] = found_s != 0x7fffffff ? found_s : next_s;
+}
+
+// Sampled drafts: the next token of sequence blockIdx.x where the path ended, from p - q or, where no token was rejected or p has nothing over
+// q, from p.
+template <typename T>
+__global__ __launch_bounds__(kWalkThreads) void draft_draw_kernel(VerifyArgs a) {
+  extern __shared__ __align__(16) double chunk_sums[];
+  __shared__ WalkShared sh;
+  const int s = blockIdx.x, lane = threadIdx.x & 63;
+  const WalkEnd end = a.ends[s];
+  if (end.draw == 0) return;
+  const double k = heat_of(a, s);
+  const int64_t row = end.row;
+  Rest<T> rest{static_cast<const T *>(a.logits) + row * a.logit_stride, nullptr, RowStat{}, RowStat{}, k, 1.0, 0.0, nullptr, 0};
+  rest.ps = join_chunks<true>(a.stats + row * a.chunks, a.chunks, k);
+  bool any = false;
+  if (end.draw == 2) {
+    for (int c = threadIdx.x; c < a.chunks; c += kWalkThreads) chunk_sums[c] = a.rest[(int64_t)s * a.chunks + c];
+    __syncthreads();
+    for (int c = lane; c < a.chunks; c += kWave) any |= chunk_sums[c] > 0.0;
+  }
+  if (__ballot(any) != 0) {
+    rest.qs = join_chunks<true>(a.stats + (a.M + row) * a.chunks, a.chunks, k);
+    rest.q = static_cast<const T *>(a.draft) + row * a.draft_stride;
+    rest.p_scale = 1.0 / rest.ps.sum;
+    rest.q_scale = 1.0 / rest.qs.sum;
+  } else {
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.chunks; c += kWalkThreads) {
+      const ChunkStat st = a.stats[row * a.chunks + c];
+      chunk_sums[c] = st.sum * weight_of(st.top, rest.ps.top, k);
+    }
+    __syncthreads();
+  }
+  draw_token(a, s, rest, chunk_sums, sh);
 }
 
 int chunks_of(const moespec_verify &v) { return (v.vocab + kChunk - 1) / kChunk; }
@@ -413,20 +608,30 @@ hipError_t run_verify(const VerifyArgs &a, hipStream_t st) {
   else logit_stats_kernel<T, false><<<grid, kStatThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const size_t smem = (size_t)a.max_tree * 20 + 4 + (size_t)a.chunks * 8;
-  auto kern = draft_walk_kernel<T>;
+  const int groups = a.chunks < kVerifyGroups ? a.chunks : kVerifyGroups;
+  const size_t sums = (size_t)a.chunks * sizeof(double), smem = (size_t)a.max_tree * 40 + (a.draft ? (size_t)a.max_tree * 12 : sums);
+  const bool wide = a.chunks > 16;
+  auto walk = a.draft ? (wide ? draft_walk_kernel<T, true, true> : draft_walk_kernel<T, true, false>)
+                      : (wide ? draft_walk_kernel<T, false, true> : draft_walk_kernel<T, false, false>);
   if (smem > 60 * 1024) {
-    e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(walk), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != hipSuccess) return e;
   }
-  kern<<<a.n_seq, kWalkThreads, smem, st>>>(a);
+  walk<<<dim3(a.draft ? groups : 1, a.n_seq), kWalkThreads, smem, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess || !a.draft) return e;
+  draft_draw_kernel<T><<<a.n_seq, kWalkThreads, sums, st>>>(a);
   return hipGetLastError();
+}
+
+size_t stats_bytes(const moespec_verify &v, int M) {
+  return align_up(sizeof(ChunkStat) * (size_t)M * chunks_of(v) * (v.draft_logits ? 2 : 1), 256);
 }
 
 }  // namespace
 
-size_t draft_verify_ws(const moespec_verify &v, int, int M) {
-  return sizeof(ChunkStat) * (size_t)M * chunks_of(v) * (v.draft_logits ? 2 : 1);
+size_t draft_verify_ws(const moespec_verify &v, int n_seq, int M) {
+  return stats_bytes(v, M) + (v.draft_logits ? (sizeof(double) * chunks_of(v) + sizeof(WalkEnd)) * (size_t)n_seq : 0);
 }
 
 hipError_t launch_draft_verify(const moespec_verify &v, const moespec_tree &tree, const int32_t *tokens, const double *u_accept,
@@ -446,6 +651,8 @@ hipError_t launch_draft_verify(const moespec_verify &v, const moespec_tree &tree
   a.next_token = next_token;
   a.accepted = accepted;
   a.stats = static_cast<ChunkStat *>(ws);
+  a.rest = reinterpret_cast<double *>(static_cast<char *>(ws) + stats_bytes(v, tree.n_tokens));
+  a.ends = reinterpret_cast<WalkEnd *>(a.rest + (size_t)tree.n_seq * chunks_of(v));
   a.logit_stride = v.logit_stride ? v.logit_stride : v.vocab;
   a.draft_stride = v.draft_stride ? v.draft_stride : v.vocab;
   a.V = v.vocab;

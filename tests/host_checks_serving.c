@@ -265,7 +265,7 @@ static void verify_arguments(void) {
   t.tree_mask = NULL;
   t.tree_off = NULL;
   BAD((void)0, INVALID);
-  t = make_tree(2, 65535, 4097);
+  t = make_tree(2, 65535, 2049);
   BAD((void)0, UNSUPPORTED);
   t = make_tree(2, 16, 17);
   BAD((void)0, INVALID);

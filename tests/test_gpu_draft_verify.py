@@ -178,7 +178,7 @@ def test_numbers_and_temperatures_out_of_range():
 
 
 def test_large_trees_and_their_limit():
-    b = Batch([4096, 300], 300, seed=12, lift=1.0, back=40)
+    b = Batch([2048, 300], 300, seed=12, lift=1.0, back=40)
     b.check(b.run(64), 64)
     b = Batch([700], 40000, "bf16", seed=13, chain=True, lift=8.0)
     assert b.check(b.run(1000), 1000)[0] > 3
