@@ -131,57 +131,69 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
   uint4 kr[P::kHalves][P::kLoads], vr[P::kValueLoads];
   f32x4 ks[P::kHalves], vs[P::kHalves];
   const int vrow = lane / pow2_ceil(P::kValueLanes), vpiece = lane % pow2_ceil(P::kValueLanes);
-  // Row (of D elements) in the pool of the first of 16 entries from e on; entries behind the last page or outside of the pool: of
-  // some page that is there, `there` says so.
-  auto rows_at = [&](int e, bool &there) -> int64_t {
-    const int at = min(e, len - 1);
-    const int p = pg.page_of(s, at);
-    there = p >= 0 && e < len;
-    return pg.row(0, max(p, 0), hk, e & ~15);
+  const uint32_t kat = n16 * P::kRowBytes, vat = vrow * P::kRowBytes + 16 * min(vpiece, P::kValueLanes - 1);
+  // Pages of this wave's next tiles, one half of a tile to a lane: the table is read once every 64 / kHalves tiles.
+  int ids = 0;
+  auto page_ids = [&](int u) {
+    const int64_t e = (int64_t)(u + lane / P::kHalves) * P::kUnit + wave * P::kKeys + 16 * (lane % P::kHalves);
+    ids = pg.table[(int64_t)s * pg.max_pages + ((int)min(e, (int64_t)len - 1) >> pg.log_page)];
   };
-  auto load_keys = [&](int e0) {
+  // First row (of D elements) of 16 entries from e on in the pool; of some page that is there where theirs is not.
+  auto page_there = [&](int u, int x) {
+    const int p = __builtin_amdgcn_readlane(ids, ((u - u0) * P::kHalves + x) & 63);
+    return p >= 0 && p < pg.n_pages;
+  };
+  auto row_of = [&](int u, int x) {
+    const int p = __builtin_amdgcn_readlane(ids, ((u - u0) * P::kHalves + x) & 63);
+    const int e = u * P::kUnit + wave * P::kKeys + 16 * x;
+    return pg.row(0, p >= 0 && p < pg.n_pages ? p : 0, hk, e);
+  };
+  auto load_keys = [&](int u) {
 #pragma unroll
     for (int x = 0; x < P::kHalves; ++x) {
-      bool there;
-      const int64_t row = rows_at(e0 + 16 * x, there);
-      const unsigned char *at = pg.k + (row + n16) * P::kRowBytes;
+      const int64_t row = row_of(u, x);
+      const unsigned char *at = pg.k + row * P::kRowBytes;
 #pragma unroll
       for (int i = 0; i < P::kLoads; ++i) {
         if (P::kTail && i == P::kLoads - 1) {
-          const uint2 two = *reinterpret_cast<const uint2 *>(at + 64 * i + 8 * g4);
+          const uint2 two = *reinterpret_cast<const uint2 *>(at + (kat + 8 * g4) + 64 * i);
           kr[x][i] = make_uint4(two.x, two.y, 0, 0);
         } else {
-          kr[x][i] = *reinterpret_cast<const uint4 *>(at + 64 * i + 16 * g4);
+          kr[x][i] = *reinterpret_cast<const uint4 *>(at + (kat + 16 * g4) + 64 * i);
         }
       }
       if (P::kCodes) ks[x] = *reinterpret_cast<const f32x4 *>(pg.k_scale + row + 4 * g4);
     }
   };
-  auto load_values = [&](int e0) {
+  auto load_values = [&](int u) {
 #pragma unroll
-    for (int i = 0; i < P::kValueLoads; ++i) {
-      const int r = i * P::kValueRows + vrow;
-      bool there;
-      const int64_t row = rows_at(e0 + (r & ~15), there);
-      vr[i] = make_uint4(0, 0, 0, 0);
-      // what is not seen must meet weights of 0 as numbers
-      if (vpiece < P::kValueLanes && there && e0 + r < len)
-        vr[i] = *reinterpret_cast<const uint4 *>(pg.v + (row + (r & 15)) * P::kRowBytes + 16 * vpiece);
-    }
-    if (P::kCodes) {
+    for (int x = 0; x < P::kHalves; ++x) {
+      const int64_t row = row_of(u, x);
+      const unsigned char *at = pg.v + row * P::kRowBytes;
 #pragma unroll
-      for (int x = 0; x < P::kHalves; ++x) {
-        bool there;
-        vs[x] = *reinterpret_cast<const f32x4 *>(pg.v_scale + rows_at(e0 + 16 * x, there) + 4 * g4);
-      }
+      for (int j = 0; j < P::kValueLoads / P::kHalves; ++j)
+        vr[x * (P::kValueLoads / P::kHalves) + j] = *reinterpret_cast<const uint4 *>(at + vat + j * P::kValueRows * P::kRowBytes);
+      if (P::kCodes) vs[x] = *reinterpret_cast<const f32x4 *>(pg.v_scale + row + 4 * g4);
     }
   };
 
-  for (int u = u0; u < u1; ++u) {
+  const int mine = min(u1, (len - wave * P::kKeys + P::kUnit - 1) / P::kUnit);  // units in which this wave has a key
+  if (u0 < mine) {
+    page_ids(u0);
+    load_keys(u0);
+    load_values(u0);
+  }
+  for (int u = u0; u < mine; ++u) {
     const int e0 = u * P::kUnit + wave * P::kKeys;
-    if (e0 >= len) break;
-    load_keys(e0);
-    load_values(e0);
+    bool there[P::kHalves], whole = e0 + P::kKeys <= len;
+#pragma unroll
+    for (int x = 0; x < P::kHalves; ++x) {
+      there[x] = page_there(u, x);
+      whole &= there[x];
+    }
+    // (the table's next pages, behind the last use of these)
+    const bool more = u + 1 < mine;
+    if (more && (u + 1 - u0) % (64 / P::kHalves) == 0) page_ids(u + 1);
     f32x4 sc[P::kHalves];
 #pragma unroll
     for (int x = 0; x < P::kHalves; ++x) {
@@ -202,12 +214,36 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
           sc[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(k, q[i / 4][i % 4], sc[x], 0, 0, 0);
         }
       }
+      if (P::kCodes)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[x][i] *= ks[x][i];
+    }
+    if (more) load_keys(u + 1);  // into the registers that the products have left
+    f32x4 vscale[P::kHalves];
+#pragma unroll
+    for (int x = 0; x < P::kHalves; ++x) vscale[x] = vs[x];
+    if (!whole) {  // what is not seen has no score, and must meet weights of 0 as numbers
+#pragma unroll
+      for (int x = 0; x < P::kHalves; ++x) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool seen = there[x] && e0 + 16 * x + 4 * g4 + i < len;
+          sc[x][i] = seen ? sc[x][i] : -INFINITY;
+          vscale[x][i] = seen ? vscale[x][i] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < P::kValueLoads / P::kHalves; ++j) {
+          const bool seen = there[x] && e0 + 16 * x + j * P::kValueRows + vrow < len;
+          uint4 &v = vr[x * (P::kValueLoads / P::kHalves) + j];
+          v = make_uint4(seen ? v.x : 0u, seen ? v.y : 0u, seen ? v.z : 0u, seen ? v.w : 0u);
+        }
+      }
     }
     // values to LDS
+    if (vpiece < P::kValueLanes) {
 #pragma unroll
-    for (int i = 0; i < P::kValueLoads; ++i) {
-      unsigned char *to = my + (i * P::kValueRows + vrow) * P::kStride;
-      if (vpiece < P::kValueLanes) {
+      for (int i = 0; i < P::kValueLoads; ++i) {
+        unsigned char *to = my + (i * P::kValueRows + vrow) * P::kStride;
         const uint32_t w[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
         if constexpr (!P::kCodes) {
           *reinterpret_cast<uint4 *>(to + 16 * vpiece) = vr[i];
@@ -222,20 +258,12 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
         }
       }
     }
+    if (more) load_values(u + 1);
     float mx = -INFINITY;
 #pragma unroll
-    for (int x = 0; x < P::kHalves; ++x) {
-      bool there;
-      rows_at(e0 + 16 * x, there);
+    for (int x = 0; x < P::kHalves; ++x)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (P::kCodes) sc[x][i] *= ks[x][i];
-        const bool seen = there && e0 + 16 * x + 4 * g4 + i < len;
-        if (!seen) sc[x][i] = -INFINITY;
-        if (P::kCodes && !seen) vs[x][i] = 0.f;
-        mx = fmaxf(mx, sc[x][i]);
-      }
-    }
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[x][i]);
     mx = head_max(mx) * ka.c;
     // raised only when it is passed by more than 2^8: until then weights stay below 2^8, as exact as below 1, and O is not rescaled
     const bool raise = mx > m + 8.f;
@@ -255,7 +283,7 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
       for (int i = 0; i < 4; ++i) {
         sc[x][i] = __builtin_amdgcn_exp2f(fmaf(sc[x][i], ka.c, -mu));
         l += sc[x][i];
-        if (P::kCodes) sc[x][i] *= vs[x][i];
+        if (P::kCodes) sc[x][i] *= vscale[x][i];
       }
     asm volatile("" ::: "memory");  // the wave's own rows: LDS keeps their order
     if constexpr (P::kBf16) {
