@@ -23,7 +23,11 @@ struct PagedAttnArgs {
 
 template <typename T, int CODE, int D>
 struct PagedShape {
-  static constexpr bool kCodes = CODE != MOESPEC_CACHE_PLAIN, kBf16 = sizeof(T) == 2;
+  static constexpr bool kCodes = CODE != MOESPEC_CACHE_PLAIN;
+  // Codes are exact in bf16, and so an fp32 layer over codes takes bf16 products too, with queries and weights in three parts (24 bits):
+  // fp32 products of 16 requests, 8 heads of 96 over up to 3000 entries took 35.8 us, these 22.3.
+  static constexpr bool kBf16 = sizeof(T) == 2 || kCodes;
+  static constexpr int kQParts = sizeof(T) == 2 || !kBf16 ? 1 : 3, kPParts = sizeof(T) == 2 ? 2 : 3;
   static constexpr int kWaves = 4;
   static constexpr int kHalves = kBf16 ? 2 : 1, kKeys = 16 * kHalves;  // keys of a wave's tile
   static constexpr int kUnit = kKeys * kWaves;                         // ... of a workgroup's
@@ -32,14 +36,14 @@ struct PagedShape {
   static constexpr int kLoads = (kRowBytes + 63) / 64;     // loads of 64 bytes of 16 keys; the last one may be of 32
   static constexpr bool kTail = kRowBytes % 64 != 0;       // (8-bit rows of 96: 8 bytes a lane)
   static constexpr int kPiece = 16 / kHeld;                // elements of a lane's 16 bytes
-  static constexpr int kStride = D * (int)sizeof(T) + (kBf16 ? 32 : 16);  // bytes of a value's row in LDS
+  static constexpr int kStride = kBf16 ? 2 * D + 32 : 4 * D + 16;  // bytes of a value's row in LDS
   static constexpr int kTileLds = kKeys * kStride;
   static constexpr int kValueLanes = kRowBytes / 16;       // lanes that hold a row of values
   static constexpr int kValueRows = 64 / pow2_ceil(kValueLanes) < kKeys ? 64 / pow2_ceil(kValueLanes) : kKeys;  // rows of a load
   static constexpr int kValueLoads = kKeys / kValueRows;
-  static constexpr int kJoin = kWaves * 16 * (D + 2) * (int)sizeof(float);
+  static constexpr int kJoinRow = D + 4;  // floats; the pad keeps the 16 heads of a store off each other's banks
+  static constexpr int kJoin = kWaves * 16 * (kJoinRow + 2) * (int)sizeof(float);
   static constexpr int kLds = kWaves * kTileLds > kJoin ? kWaves * kTileLds : kJoin;
-  static constexpr int kQ = D / 4;  // query elements of a lane
 };
 
 // Two bytes' worth of codes, and four, as values.
@@ -63,6 +67,18 @@ __device__ __forceinline__ bf16x8 codes_bf16(uint32_t a, uint32_t b) {
     v[4 + e] = (__bf16)code_value<CODE>(b, e);
   }
   return v;
+}
+
+// Eight numbers as the sum of N bf16 ones: each is the rounding of what those before it leave.
+template <int N>
+__device__ __forceinline__ void split(float (&v)[8], bf16x8 (&part)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      part[j][i] = (__bf16)v[i];
+      v[i] -= (float)part[j][i];
+    }
 }
 
 // v of the lanes that hold the same head, l ^ 16 and l ^ 32, combined.
@@ -100,24 +116,27 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
   const int h = hk * ka.G + min(tile * 16 + n16, ka.G - 1);
 
   // queries, in the order of a lane's keys
-  typename std::conditional<P::kBf16, bf16x8, f32x4>::type q[P::kBf16 ? D / 32 : D / 16];
+  typename std::conditional<P::kBf16, bf16x8, f32x4>::type q[P::kQParts][P::kBf16 ? D / 32 : D / 16];
   {
     const T *qp = static_cast<const T *>(ka.q) + (int64_t)s * ka.q_stride + h * D;
-    if constexpr (P::kBf16 && !P::kCodes) {
+    if constexpr (!P::kBf16) {
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) q[i] = *reinterpret_cast<const bf16x8 *>(qp + 32 * i + 8 * g4);
-    } else if constexpr (P::kBf16) {
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-        q[i] = *reinterpret_cast<const bf16x8 *>(qp + (P::kTail && i == D / 32 - 1 ? 32 * i + 8 * g4 : i / 2 * 64 + 16 * g4 + 8 * (i % 2)));
-    } else if constexpr (!P::kCodes) {
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const f32x4 *>(qp + 16 * i + 4 * g4);
+      for (int i = 0; i < D / 16; ++i) q[0][i] = *reinterpret_cast<const f32x4 *>(qp + 16 * i + 4 * g4);
     } else {
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i)
-        q[i] = *reinterpret_cast<const f32x4 *>(qp + (P::kTail && i >= D / 64 * 4 ? D / 64 * 64 + 8 * g4 + 4 * (i - D / 64 * 4)
-                                                                                  : i / 4 * 64 + 16 * g4 + 4 * (i % 4)));
+      for (int i = 0; i < D / 32; ++i) {
+        const int at = !P::kCodes || (P::kTail && i == D / 32 - 1) ? 32 * i + 8 * g4 : i / 2 * 64 + 16 * g4 + 8 * (i % 2);
+        if constexpr (sizeof(T) == 2) {
+          q[0][i] = *reinterpret_cast<const bf16x8 *>(qp + at);
+        } else {
+          const f32x4 lo = *reinterpret_cast<const f32x4 *>(qp + at), hi = *reinterpret_cast<const f32x4 *>(qp + at + 4);
+          float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+          bf16x8 part[P::kQParts];
+          split<P::kQParts>(v, part);
+#pragma unroll
+          for (int j = 0; j < P::kQParts; ++j) q[j][i] = part[j];
+        }
+      }
     }
   }
 
@@ -205,13 +224,13 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
           bf16x8 k;
           if constexpr (P::kCodes) k = codes_bf16<CODE>(w[2 * i], w[2 * i + 1]);
           else k = __builtin_bit_cast(bf16x8, kr[x][i]);
-          sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[i], sc[x], 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < P::kQParts; ++j) sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[j][i], sc[x], 0, 0, 0);
         }
       } else {
 #pragma unroll
         for (int i = 0; i < D / 4; ++i) {
-          const float k = P::kCodes ? code_value<CODE>(w[i / 4], i % 4) : __uint_as_float(w[i]);
-          sc[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(k, q[i / 4][i % 4], sc[x], 0, 0, 0);
+          sc[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[i]), q[0][i / 4][i % 4], sc[x], 0, 0, 0);
         }
       }
       if (P::kCodes)
@@ -247,14 +266,9 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
         const uint32_t w[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
         if constexpr (!P::kCodes) {
           *reinterpret_cast<uint4 *>(to + 16 * vpiece) = vr[i];
-        } else if constexpr (P::kBf16) {
+        } else {
           *reinterpret_cast<bf16x8 *>(to + 32 * vpiece) = codes_bf16<CODE>(w[0], w[1]);
           *reinterpret_cast<bf16x8 *>(to + 32 * vpiece + 16) = codes_bf16<CODE>(w[2], w[3]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            *reinterpret_cast<f32x4 *>(to + 64 * vpiece + 16 * j) =
-                f32x4{code_value<CODE>(w[j], 0), code_value<CODE>(w[j], 1), code_value<CODE>(w[j], 2), code_value<CODE>(w[j], 3)};
         }
       }
     }
@@ -288,14 +302,14 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
     asm volatile("" ::: "memory");  // the wave's own rows: LDS keeps their order
     if constexpr (P::kBf16) {
       // The matrix instructions take bf16 weights beside bf16 values: a weight goes in as its rounding and what that leaves (off by 2^-18 of
-      // it at most), so that outputs are as exact as their own rounding.  With the rounding alone they are 0.0023 off (root of the mean
-      // square, relative) where that leaves 0.0017; the second product is hidden behind the stream of keys and values.
-      bf16x8 p, p_rest;
+      // it at most; fp32 layers: in three parts), so that outputs are as exact as their own rounding.  With the rounding alone they are 0.0023
+      // off (root of the mean square, relative) where that leaves 0.0017; the other products are hidden behind the stream of keys
+      // and values.
+      bf16x8 p[P::kPParts];
+      float weights[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[i] = (__bf16)sc[i / 4][i % 4];
-        p_rest[i] = (__bf16)(sc[i / 4][i % 4] - (float)p[i]);
-      }
+      for (int i = 0; i < 8; ++i) weights[i] = sc[i / 4][i % 4];
+      split<P::kPParts>(weights, p);
       // lane i of 16 points at 4 elements of row i / 4 and receives element i of 4 rows
       typedef __attribute__((address_space(3))) bf16x4 lds4;
       const uint32_t at = my_lds + (4 * g4 + (n16 >> 2)) * P::kStride + 8 * (n16 & 3);
@@ -304,8 +318,8 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
         const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(uintptr_t)(at + 32 * b));
         const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4 *)(uintptr_t)(at + 16 * P::kStride + 32 * b));
         const bf16x8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o[b], 0, 0, 0);
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_rest, o[b], 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < P::kPParts; ++j) o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[j], o[b], 0, 0, 0);
       }
     } else {
 #pragma unroll
@@ -327,7 +341,7 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
   float *op = reinterpret_cast<float *>(lds + P::kWaves * 16 * sizeof(float2));
   if (g4 == 0) ml[wave * 16 + n16] = make_float2(m, l);
 #pragma unroll
-  for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4 *>(op + (wave * 16 + n16) * D + 16 * b + 4 * g4) = o[b];
+  for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4 *>(op + (wave * 16 + n16) * P::kJoinRow + 16 * b + 4 * g4) = o[b];
   __syncthreads();
   const int heads = min(16, ka.G - tile * 16);
   for (int id = threadIdx.x; id < heads * (D / 4); id += 256) {
@@ -342,7 +356,7 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
       const float2 x = ml[w * 16 + n];
       const float f = __builtin_amdgcn_exp2f(x.x - mu);
       lt = fmaf(x.y, f, lt);
-      const f32x4 y = *reinterpret_cast<const f32x4 *>(op + (w * 16 + n) * D + d);
+      const f32x4 y = *reinterpret_cast<const f32x4 *>(op + (w * 16 + n) * P::kJoinRow + d);
       if (x.x != -INFINITY) {  // a wave without keys has no values
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = fmaf(y[e], f, v[e]);
@@ -427,7 +441,7 @@ __global__ __launch_bounds__(kGroups *D / 4) void paged_join_kernel(KeyArgs a, i
   if (lse && col == 0) lse[row] = l == 0.f ? -INFINITY : (top + __log2f(l)) * 0.69314718055994531f;
 }
 
-constexpr int kTarget = 1024;         // workgroups wanted
+constexpr int kTarget = 512;          // workgroups wanted: what the compute units hold at a time
 constexpr size_t kFirstBytes = 2048;  // first parts of up to kMaxShared sequences
 
 // Parts of all sequences together: enough for kTarget workgroups, none without a unit of keys; 0 where every sequence is one part.
