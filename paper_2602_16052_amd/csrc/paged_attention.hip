@@ -41,6 +41,10 @@ struct PagedShape {
   static constexpr int kValueLanes = kRowBytes / 16;       // lanes that hold a row of values
   static constexpr int kValueRows = 64 / pow2_ceil(kValueLanes) < kKeys ? 64 / pow2_ceil(kValueLanes) : kKeys;  // rows of a load
   static constexpr int kValueLoads = kKeys / kValueRows;
+  // Workgroups wanted: one round of what the compute units hold by registers, two each, or one with long rows.  us with 512 and with 256:
+  // 48 requests over int8 rows of 128 135 and 214, one over 131071 e4m3 rows of 128 36.1 and 41.4; bf16 rows of 192 46.5 and 41.5, fp32
+  // ones of 256 36.5 and 30.9, int8 ones of 256 56.2 and 51.6.
+  static constexpr int kTarget = D >= 192 || kRowBytes >= 512 ? 256 : 512;
   static constexpr int kJoinRow = D + 4;  // floats; the pad keeps the 16 heads of a store off each other's banks
   static constexpr int kJoin = kWaves * 16 * (kJoinRow + 2) * (int)sizeof(float);
   static constexpr int kLds = kWaves * kTileLds > kJoin ? kWaves * kTileLds : kJoin;
@@ -441,13 +445,13 @@ __global__ __launch_bounds__(kGroups *D / 4) void paged_join_kernel(KeyArgs a, i
   if (lse && col == 0) lse[row] = l == 0.f ? -INFINITY : (top + __log2f(l)) * 0.69314718055994531f;
 }
 
-constexpr int kTarget = 512;          // workgroups wanted: what the compute units hold at a time
+constexpr int kMostGroups = 512;      // workgroups wanted, at most
 constexpr size_t kFirstBytes = 2048;  // first parts of up to kMaxShared sequences
 
-// Parts of all sequences together: enough for kTarget workgroups, none without a unit of keys; 0 where every sequence is one part.
-int slots_of(int64_t n_seq, int64_t Hk, int64_t head_tiles, int64_t max_len, int64_t unit) {
+// Parts of all sequences together: enough for `target` workgroups, none without a unit of keys; 0 where every sequence is one part.
+int slots_of(int64_t target, int64_t n_seq, int64_t Hk, int64_t head_tiles, int64_t max_len, int64_t unit) {
   const int64_t units = (max_len + unit - 1) / unit;
-  int64_t n = kTarget / (Hk * head_tiles);
+  int64_t n = target / (Hk * head_tiles);
   if (n > n_seq * units) n = n_seq * units;
   if (n_seq == 1 && n > kMaxParts) n = kMaxParts;
   return n <= n_seq || n_seq > kMaxShared ? 0 : (int)n;
@@ -458,7 +462,7 @@ hipError_t run_paged(const PagedAttnArgs &args, void *out, float *lse, void *ws,
   typedef PagedShape<T, CODE, D> P;
   PagedAttnArgs a = args;
   const KeyArgs &k = a.keys;
-  a.slots = slots_of(k.n_seq, k.Hk, a.head_tiles, k.max_len, P::kUnit);
+  a.slots = slots_of(P::kTarget, k.n_seq, k.Hk, a.head_tiles, k.max_len, P::kUnit);
   auto kern = paged_attention_kernel<T, CODE, D>;
   static_assert(P::kLds <= 160 * 1024, "LDS of a compute unit");
   if (P::kLds > 64 * 1024) {
@@ -495,10 +499,10 @@ hipError_t run_code(int code, int D, const PagedAttnArgs &a, void *out, float *l
 
 }  // namespace
 
-// Room for the parts: no more workgroups than kTarget, and no more than units of 64 keys.  Neither bound grows where a call gets smaller.
+// Room for the parts: no more workgroups than kMostGroups, and no more than units of 64 keys.  Neither bound grows where a call gets smaller.
 size_t paged_attention_ws(const moespec_attn_desc &ds, const moespec_paged_cache &, int n_seq, int max_len) {
   const int64_t G = ds.n_heads / ds.n_kv_heads, units = (max_len + 63) / 64 * (int64_t)(n_seq < kMaxShared ? n_seq : kMaxShared);
-  const int64_t most = kTarget / (ds.n_kv_heads * ((G + 15) / 16)), slots = units < most ? units : most;
+  const int64_t most = kMostGroups / (ds.n_kv_heads * ((G + 15) / 16)), slots = units < most ? units : most;
   return kFirstBytes + (size_t)slots * ds.n_heads * (sizeof(float) * ds.head_dim + sizeof(float2));
 }
 
