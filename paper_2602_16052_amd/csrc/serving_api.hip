@@ -143,8 +143,8 @@ moespec_status moespec_paged_read(const moespec_attn_desc *desc, int32_t n_layer
   if (!cache_len || !k_cache || !v_cache || !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(first) || !aligned4(cache_len) ||
       max_len < 0 || max_len > desc->capacity || max_len > entries_of(*cache))
     return MOESPEC_ERR_INVALID_ARG;
-  const int64_t rows = rows_of_group(*desc), blocks = ((int64_t)max_len + rows - 1) / rows;
-  if ((double)(blocks < 512 ? blocks : 512) * desc->n_kv_heads * n_seq * n_layers * 256. > (double)kMaxThreads) return MOESPEC_ERR_UNSUPPORTED_SHAPE;
+  // a workgroup of 256 threads a head at least, several where there are few
+  if ((double)desc->n_kv_heads * n_seq * n_layers * 256. + 4096. * 256. > (double)kMaxThreads) return MOESPEC_ERR_UNSUPPORTED_SHAPE;
   const double dense = cache_entries(*desc, n_layers, n_seq) * desc->head_dim * elem_bytes(*desc);
   if (!apart({{k_cache, dense}, {v_cache, dense}},
              {{cache->k_pages, pool.pages}, {cache->v_pages, pool.pages}, {cache->k_scale, pool.scales}, {cache->v_scale, pool.scales},
