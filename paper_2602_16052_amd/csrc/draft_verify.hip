@@ -12,9 +12,9 @@ namespace moespec {
 
 namespace {
 
-constexpr int kChunk = kVerifyChunk;
+constexpr int kChunk = kVerifyChunk;  // logits of a wave
 constexpr int kStatThreads = 256, kWalkThreads = 1024;
-constexpr int kEach = kChunk / kStatThreads;
+constexpr int kEach = kChunk / kWave;
 
 // A chunk of a row: largest logit, its first place (greedy), sum of 2^((logit - largest) k).
 struct ChunkStat {
@@ -49,23 +49,34 @@ __device__ __forceinline__ double heat_of(const VerifyArgs &a, int s) {
   return t > 0.f ? 1.4426950408889634 / (double)fminf(fmaxf(t, 0x1p-60f), 0x1p60f) : 0.0;
 }
 
-// 2^t for t <= 0: t = n + r with |r| <= 1/2 (the sum with 1.5 * 2^52 rounds, and holds n in its low word), the polynomial of degree 10
-// through 2^r at the Chebyshev nodes (off by 3.2e-16 relative at most), n added to the exponent.  Below -1020: 2^-1020.  Drops a NaN.  19
-// instructions of the fp64 pipes with the logit's part: they, not the bytes, bound the sums of a row.
+// N sums' terms 2^t side by side, t <= 0 (or just above): t = n + r with |r| <= 1/2 (the sum with 1.5 * 2^52 rounds, and holds n in its
+// low word), the polynomial of degree 10 through 2^r at the Chebyshev nodes (off by 3.2e-16 relative at most), n added to the
+// exponent.  Below -1020: 2^-1020.  Drops a NaN.
+template <int N>
+__device__ __forceinline__ void exp2_of(double (&t)[N]) {
+  constexpr double kCoef[] = {7.072585949269223e-09, 1.0208690299958306e-07, 1.321544258792169e-06, 1.5252657260200837e-05,
+                              0.0001540353044173605, 0.0013333558230164974, 0.009618129107606888, 0.05550410866444772,
+                              0.24022650695910097, 0.69314718055995, 1.0};
+  double r[N];
+  int n[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const double c = fmax(t[i], -1020.0), shifted = c + 6755399441055744.0;
+    n[i] = __double2loint(shifted);
+    r[i] = c - (shifted - 6755399441055744.0);
+    t[i] = kCoef[0];
+  }
+#pragma unroll
+  for (int d = 1; d <= 10; ++d)
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i] = fma(t[i], r[i], kCoef[d]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) t[i] = __hiloint2double(__double2hiint(t[i]) + (n[i] << 20), __double2loint(t[i]));
+}
 __device__ __forceinline__ double exp2_sum(double t) {
-  const double c = fmax(t, -1020.0), shifted = c + 6755399441055744.0, r = c - (shifted - 6755399441055744.0);
-  double p = 7.072585949269223e-09;
-  p = fma(p, r, 1.0208690299958306e-07);
-  p = fma(p, r, 1.321544258792169e-06);
-  p = fma(p, r, 1.5252657260200837e-05);
-  p = fma(p, r, 0.0001540353044173605);
-  p = fma(p, r, 0.0013333558230164974);
-  p = fma(p, r, 0.009618129107606888);
-  p = fma(p, r, 0.05550410866444772);
-  p = fma(p, r, 0.24022650695910097);
-  p = fma(p, r, 0.69314718055995);
-  p = fma(p, r, 1.0);
-  return __hiloint2double(__double2hiint(p) + (__double2loint(shifted) << 20), __double2loint(p));
+  double v[1] = {t};
+  exp2_of(v);
+  return v[0];
 }
 
 // The same for a single token: 0 below 2^-1022 and for -inf.  (Rows with NaN or +inf are told by their sums.)
@@ -120,17 +131,18 @@ __device__ __forceinline__ double wave_scan64(double v) {
   return v + (row == 0 ? 0.0 : row == 1 ? r0 : row == 2 ? r1 : r2);
 }
 
-// kVec: rows start at multiples of 16 bytes.
+// A wave takes a chunk.  kVec: rows start at multiples of 16 bytes.
 template <typename T, bool kVec>
 __global__ __launch_bounds__(kStatThreads) void logit_stats_kernel(VerifyArgs a) {
   constexpr int E = 16 / (int)sizeof(T);
-  const int row = blockIdx.y, chunk = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = blockIdx.y, lane = threadIdx.x & 63;
+  const int chunk = __builtin_amdgcn_readfirstlane(blockIdx.x * (kStatThreads / kWave) + (int)(threadIdx.x >> 6));
+  if (chunk >= a.chunks) return;
   const bool draft = blockIdx.z == 1;
   const T *x = static_cast<const T *>(draft ? a.draft : a.logits) + (int64_t)row * (draft ? a.draft_stride : a.logit_stride);
-  const int base = chunk * kChunk;
   float v[kEach];
-  auto place = [&](int i) {  // of this thread's value i
-    return kVec ? base + (i / E * kStatThreads + (int)threadIdx.x) * E + i % E : base + i * kStatThreads + (int)threadIdx.x;
+  auto place = [&](int i) {  // of this lane's value i
+    return chunk * kChunk + (kVec ? (i / E * kWave + lane) * E + i % E : i * kWave + lane);
   };
   if constexpr (kVec) {
 #pragma unroll
@@ -155,28 +167,31 @@ __global__ __launch_bounds__(kStatThreads) void logit_stats_kernel(VerifyArgs a)
   const int s = seq_of_row(a.tree_off, a.n_seq, row);
   if (s >= a.n_seq) return;
   const double k = heat_of(a, s);
-  __shared__ float top_of[kStatThreads / kWave];
-  __shared__ double sum_of[kStatThreads / kWave];
-  __shared__ int arg_of[kStatThreads / kWave];
   float top = -INFINITY;
   bool nan = false;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    top = fmaxf(top, v[i]);
-    nan |= v[i] != v[i];
+  for (int i = 0; i < kEach; i += 2) {
+    top = fmaxf(fmaxf(top, v[i]), v[i + 1]);
+    nan |= __builtin_isunordered(v[i], v[i + 1]);
   }
   top = wave_top(top);
-  if (lane == 0) top_of[wave] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kStatThreads / kWave; ++w) top = fmaxf(top, top_of[w]);
-  nan |= top == INFINITY;
   double sum = 0.0;
   int arg = 0x7fffffff;
   if (k > 0.0) {
     if (top > -INFINITY && top < INFINITY) {
+      // 2^(x k - c) with c = top k rounded, one instruction less than from x - top; what c has lost is the same for all
+      const double c = (double)top * k;
+      constexpr int kSide = 4;  // in flight at a time; more of them, and their registers cost waves
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) sum += exp2_sum(((double)v[i] - (double)top) * k);
+      for (int i = 0; i < kEach; i += kSide) {
+        double w[kSide];
+#pragma unroll
+        for (int j = 0; j < kSide; ++j) w[j] = fma((double)v[i + j], k, -c);
+        exp2_of(w);
+        sum += (w[0] + w[1]) + (w[2] + w[3]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      sum *= exp2_sum(-fma((double)top, k, -c));
     }
   } else {
 #pragma unroll
@@ -186,24 +201,14 @@ __global__ __launch_bounds__(kStatThreads) void logit_stats_kernel(VerifyArgs a)
     for (int m = 1; m < kWave; m <<= 1) arg = min(arg, __shfl_xor(arg, m, kWave));
     sum = top > -INFINITY ? 1.0 : 0.0;
   }
-  if (nan) sum = __builtin_nan("");
+  if (nan || top == INFINITY) sum = __builtin_nan("");
   sum = wave_sum64(sum);
-  if (lane == 0) {
-    sum_of[wave] = sum;
-    arg_of[wave] = arg;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < kStatThreads / kWave; ++w) {
-      sum += sum_of[w];
-      arg = min(arg, arg_of[w]);
-    }
-    a.stats[((int64_t)blockIdx.z * a.M + row) * a.chunks + chunk] = ChunkStat{sum, top, arg};
-  }
+  if (lane == 0) a.stats[((int64_t)blockIdx.z * a.M + row) * a.chunks + chunk] = ChunkStat{sum, top, arg};
 }
 
-// A whole row from its chunks, by the 16 lanes of a row of lanes (kWide: by a wave); all of them end with the same bits.  A row of logits
-// that is no distribution has the sum NaN.
+// A whole row from its chunks, by the 16 lanes of a row of lanes (kWide: by a wave); all of them end with the same bits.  A lane holds its
+// first four chunks, so that rows of up to 64 (256) chunks take one trip to memory.  A row of logits that is no distribution has the sum
+// NaN.
 struct RowStat {
   double sum;
   float top;
@@ -211,20 +216,30 @@ struct RowStat {
 };
 template <bool kWide>
 __device__ __forceinline__ RowStat join_chunks(const ChunkStat *c, int chunks, double k) {
-  constexpr int kLanes = kWide ? kWave : 16;
+  constexpr int kLanes = kWide ? kWave : 16, kHeld = 4;
   const int first = threadIdx.x & (kLanes - 1);
-  ChunkStat mine{0.0, -INFINITY, 0x7fffffff};
-  if (first < chunks) mine = c[first];
-  float top = mine.top;
-  int arg = mine.arg;
-  if constexpr (kWide)
-    for (int i = first + kLanes; i < chunks; i += kLanes) {
-      const ChunkStat x = c[i];
-      if (x.top > top) {  // (places ascend)
-        top = x.top;
-        arg = x.arg;
-      }
+  ChunkStat held[kHeld];
+  float top = -INFINITY;
+  int arg = 0x7fffffff;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const int i = first + j * kLanes;
+    held[j] = c[min(i, chunks - 1)];
+    if (i >= chunks) held[j] = ChunkStat{0.0, -INFINITY, 0x7fffffff};
+  }
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (held[j].top > top) {  // (places ascend)
+      top = held[j].top;
+      arg = held[j].arg;
     }
+  for (int i = first + kHeld * kLanes; i < chunks; i += kLanes) {
+    const ChunkStat x = c[i];
+    if (x.top > top) {
+      top = x.top;
+      arg = x.arg;
+    }
+  }
   const float mine_top = top;
   top = kWide ? wave_top(top) : row16_top(top);
   if (k == 0.0) {
@@ -232,13 +247,11 @@ __device__ __forceinline__ RowStat join_chunks(const ChunkStat *c, int chunks, d
 #pragma unroll
     for (int m = 1; m < kLanes; m <<= 1) arg = min(arg, __shfl_xor(arg, m, kWave));
   }
-  double sum = mine.sum * weight_of(mine.top, top, k);
-  if constexpr (kWide) {
-    for (int i = first + kLanes; i < chunks; i += kLanes) sum += c[i].sum * weight_of(c[i].top, top, k);
-    sum = wave_sum64(sum);
-  } else {
-    sum = row16_sum(sum);
-  }
+  double sum = 0.0;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) sum += held[j].sum * weight_of(held[j].top, top, k);
+  for (int i = first + kHeld * kLanes; i < chunks; i += kLanes) sum += c[i].sum * weight_of(c[i].top, top, k);
+  sum = kWide ? wave_sum64(sum) : row16_sum(sum);
   return RowStat{sum > 0.0 && sum < INFINITY ? sum : __builtin_nan(""), top, arg};
 }
 
@@ -603,14 +616,15 @@ int chunks_of(const moespec_verify &v) { return (v.vocab + kChunk - 1) / kChunk;
 template <typename T>
 hipError_t run_verify(const VerifyArgs &a, hipStream_t st) {
   const bool vec = a.logit_stride * sizeof(T) % 16 == 0 && (!a.draft || a.draft_stride * sizeof(T) % 16 == 0);
-  const dim3 grid(a.chunks, a.M, a.draft ? 2 : 1);
+  constexpr int kWaves = kStatThreads / kWave;
+  const dim3 grid((a.chunks + kWaves - 1) / kWaves, a.M, a.draft ? 2 : 1);
   if (vec) logit_stats_kernel<T, true><<<grid, kStatThreads, 0, st>>>(a);
   else logit_stats_kernel<T, false><<<grid, kStatThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int groups = a.chunks < kVerifyGroups ? a.chunks : kVerifyGroups;
   const size_t sums = (size_t)a.chunks * sizeof(double), smem = (size_t)a.max_tree * 40 + (a.draft ? (size_t)a.max_tree * 12 : sums);
-  const bool wide = a.chunks > 16;
+  const bool wide = a.chunks > 64;
   auto walk = a.draft ? (wide ? draft_walk_kernel<T, true, true> : draft_walk_kernel<T, true, false>)
                       : (wide ? draft_walk_kernel<T, false, true> : draft_walk_kernel<T, false, false>);
   if (smem > 60 * 1024) {
@@ -620,7 +634,12 @@ hipError_t run_verify(const VerifyArgs &a, hipStream_t st) {
   walk<<<dim3(a.draft ? groups : 1, a.n_seq), kWalkThreads, smem, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess || !a.draft) return e;
-  draft_draw_kernel<T><<<a.n_seq, kWalkThreads, sums, st>>>(a);
+  auto draw = draft_draw_kernel<T>;
+  if (sums > 60 * 1024) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(draw), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sums);
+    if (e != hipSuccess) return e;
+  }
+  draw<<<a.n_seq, kWalkThreads, sums, st>>>(a);
   return hipGetLastError();
 }
 

@@ -70,7 +70,7 @@ hipError_t launch_paged_attention(const moespec_attn_desc &ds, const moespec_pag
                                   int64_t q_stride, const int32_t *cache_len, int max_len, void *out, float *lse, void *ws,
                                   hipStream_t st);
 constexpr int kMaxVerifyTree = 2048;  // rows of a tree that the walk holds in LDS
-constexpr int kVerifyChunk = 8192;    // logits of a workgroup
+constexpr int kVerifyChunk = 2048;    // logits of a wave
 constexpr int kVerifyGroups = 32;     // workgroups of 1024 threads a sequence, at most, that sum p - q (sampled drafts)
 size_t draft_verify_ws(const moespec_verify &v, int n_seq, int M);
 hipError_t launch_draft_verify(const moespec_verify &v, const moespec_tree &tree, const int32_t *tokens, const double *u_accept,

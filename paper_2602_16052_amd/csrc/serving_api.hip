@@ -209,7 +209,7 @@ moespec_status moespec_draft_verify(const moespec_verify *verify, const moespec_
   const size_t need = draft_verify_ws(v, tree->n_seq, tree->n_tokens);
   if ((s = check_ws(ws, ws_bytes, need)) != MOESPEC_OK) return s;
   const double M = tree->n_tokens, n_seq = tree->n_seq, es = v.dtype == MOESPEC_BF16 ? 2 : 4;
-  if (M * ((v.vocab + kVerifyChunk - 1) / kVerifyChunk) * (v.draft_logits ? 2 : 1) * 256. > (double)kMaxThreads ||
+  if (M * ((v.vocab + kVerifyChunk - 1) / kVerifyChunk) * (v.draft_logits ? 2 : 1) * 64. + M * 2 * 192. > (double)kMaxThreads ||
       n_seq * kVerifyGroups * 1024. > (double)kMaxThreads)
     return MOESPEC_ERR_UNSUPPORTED_SHAPE;
   const double words = (tree->max_tree + 31) / 32;
