@@ -473,10 +473,10 @@ __global__ __launch_bounds__(kWalkThreads) void draft_walk_kernel(VerifyArgs a) 
           for (int i = lane; i < n_gone; i += kWave) again |= gone[i] == x;
           if (__ballot(again) != 0) continue;
           const double p = mine[t];
-          if (number[t] * (1.0 - left) < p) {
+          if (p > 0.0 && number[t] * (1.0 - left) < p) {
             step = t;
           } else {
-            if (greedy) continue;
+            if (greedy || x < 0 || x >= a.V) continue;  // (a token of no vocabulary leaves p as it is)
             left += p;
             if (lane == 0) gone[n_gone] = x;
             ++n_gone;

@@ -85,6 +85,19 @@ __device__ __forceinline__ void split(float (&v)[8], bf16x8 (&part)[N]) {
     }
 }
 
+// Eight weights in two parts that are both above 0 where the weight is, so that a value of infinity stays one: cut off, and the rest, which is
+// 2^-16 of the weight at least (off by 2^-15 of it at most).
+__device__ __forceinline__ void split_above_zero(const float (&v)[8], bf16x8 (&part)[2]) {
+  uint32_t cut[4];
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    cut[i / 2] = __builtin_amdgcn_perm(__float_as_uint(v[i + 1]), __float_as_uint(v[i]), 0x07060302u);
+#pragma unroll
+    for (int j = i; j < i + 2; ++j) part[1][j] = (__bf16)fmaxf(v[j] - __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u), v[j] * 0x1p-16f);
+  }
+  part[0] = __builtin_bit_cast(bf16x8, cut);
+}
+
 // v of the lanes that hold the same head, l ^ 16 and l ^ 32, combined.
 __device__ __forceinline__ float head_max(float v) {
   auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -305,15 +318,16 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
       }
     asm volatile("" ::: "memory");  // the wave's own rows: LDS keeps their order
     if constexpr (P::kBf16) {
-      // The matrix instructions take bf16 weights beside bf16 values: a weight goes in as its rounding and what that leaves (off by 2^-18 of
-      // it at most; fp32 layers: in three parts), so that outputs are as exact as their own rounding.  With the rounding alone they are 0.0023
-      // off (root of the mean square, relative) where that leaves 0.0017; the other products are hidden behind the stream of keys
-      // and values.
+      // The matrix instructions take bf16 weights beside bf16 values: a weight goes in as its rounding and what that leaves (off by 2^-16 of
+      // it at most; fp32 layers: in three parts, 2^-24), so that outputs are as exact as their own rounding.  With the rounding alone
+      // they are 0.0023 off (root of the mean square, relative) where that leaves 0.0017; the other products are hidden behind the
+      // stream of keys and values.
       bf16x8 p[P::kPParts];
       float weights[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) weights[i] = sc[i / 4][i % 4];
-      split<P::kPParts>(weights, p);
+      if constexpr (P::kCodes) split<P::kPParts>(weights, p);
+      else split_above_zero(weights, p);
       // lane i of 16 points at 4 elements of row i / 4 and receives element i of 4 rows
       typedef __attribute__((address_space(3))) bf16x4 lds4;
       const uint32_t at = my_lds + (4 * g4 + (n16 >> 2)) * P::kStride + 8 * (n16 & 3);

@@ -91,8 +91,9 @@ class Pool:
         D, n, u = q.shape[2], max(self.lens), HALF_STEP[self.dtype]
         # a score: products and sums of D terms (a whole step each in the matrix cores), the scales, the exponential's argument
         score = (2 * D + 10) * 2.0 ** -24 * spread
-        # weights: what the two halves of a bf16 weight leave, the value's scale, the scores above and below the line, sums over keys
-        rel = (2.0 ** -18 if self.dtype == "bf16" else 0.0) + 2.0 ** -23 + 2 * score + 2 * (n + 64) * 2.0 ** -24
+        # weights: what the two parts of a bf16 weight leave (the first is cut off: 2^-7; the second is rounded: 2^-8 of that), of an fp32 one
+        # over codes the three parts (2^-8 three times), the value's scale, the scores above and below the line, sums over keys
+        rel = (2.0 ** -15 if self.dtype == "bf16" else 2.0 ** -24) + 2.0 ** -23 + 2 * score + 2 * (n + 64) * 2.0 ** -24
         tol = u * np.abs(want) * (1 + 2.0 ** -6) + bound * rel[:, :, None] + 1e-37
         err = np.abs(f64(out) - want)
         assert np.all(err <= tol), f"out off by {np.nanmax(err / tol):.2f} of the bound"

@@ -130,6 +130,26 @@ def test_tokens_outside_of_the_vocabulary_are_rejected():
     b.tokens[[1, 7]] = [-1, 100]
     b.u_accept[:] = 0
     assert b.check(b.run()) == [1, 2]
+    for seed in range(8):  # sampled drafts: p as it is
+        b = Batch([3] * 6, 100, seed=seed, sampled=True)
+        b.tokens[[1, 4, 7, 10]] = [-5, 100, 2 ** 31 - 1, -2 ** 31]
+        b.check(b.run())
+
+
+def test_a_token_without_probability_is_never_accepted():
+    """Also where what is left of p is below 0 by a rounding, or the random number is."""
+    b = Batch([6], 40, seed=5)
+    b.sees = [A.ancestors([-1, 0, 0, 0, 0, 0])]
+    b.logits[:] = -float("inf")
+    b.logits[0, 3:6] = torch.tensor([0.3, 0.7, 0.2], device="cuda")
+    b.logits[1:] = 0
+    b.tokens = np.array([0, 3, 4, 5, 9, 10])
+    for u in (np.ones(6), np.full(6, -1.0), np.array([0, 1.0, 1.0, 1.0, 0.0, -1.0])):
+        b.u_accept = u
+        got = b.run()
+        assert int(got["n_path"][0]) == 1 or int(got["path"][0, 1]) in (1, 2, 3)
+        if int(got["n_path"][0]) == 1:
+            assert 3 <= int(got["next_token"][0]) <= 5
 
 
 @pytest.mark.parametrize("heat", [1.0, 0.0])

@@ -165,6 +165,21 @@ def test_scores_of_minus_infinity_and_nan(dtype):
     pool.check(q[1:2], out[1:2], lse[1:2], want)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_of_infinity_that_are_seen_stay_infinities(dtype):
+    """Under weights that bf16 holds exactly (a single key: 1) and under others."""
+    pool = Pool(dtype, "plain", 1, 64, [1, 70, 300], 16, seed=21, H=4)
+    v, inf = pool.cache.v_pages[0, :, 0], float("inf")
+    for s, e, d, x in ((0, 0, 3, inf), (0, 0, 9, -inf), (1, 69, 5, -inf), (2, 33, 60, inf)):
+        v[pool.rows[s][e // 16], e % 16, d] = x
+    q = queries(pool)
+    out, lse = run(pool, q)
+    for s, d, x in ((0, 3, inf), (0, 9, -inf), (1, 5, -inf), (2, 60, inf)):
+        assert torch.all(out[s, :, d] == x)
+        out[s, :, d] = 0
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
 def test_rows_whose_scale_is_nan_make_only_their_own_sequence_nan():
     pool = Pool("bf16", "i8", 1, 64, [40, 40], 16, seed=14, H=2)
     pool.cache.v_scale[0, pool.rows[0][1], 0, 3] = float("nan")
