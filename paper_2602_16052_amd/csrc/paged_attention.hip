@@ -462,9 +462,14 @@ __global__ __launch_bounds__(kGroups *D / 4) void paged_join_kernel(KeyArgs a, i
 constexpr int kMostGroups = 512;      // workgroups wanted, at most
 constexpr size_t kFirstBytes = 2048;  // first parts of up to kMaxShared sequences
 
+// Short caches and many sequences are not split: a unit of keys takes a workgroup 1.2 us, the launch that joins parts 2.5 to 6.  us whole and
+// in parts, bf16 heads of 128: 4 heads of one sequence (workgroups), 250 entries (2 units) 6.8 and 8.3, 500 entries 8.9 and 8.3; 64 of them, 500
+// 9.8 and 10.9, 1000 14.9 and 12.9; 160, 1000 16.4 and 20.6, 2000 34.7 and 38.3 (int8 31.4 and 24.6); 400, 2000 76 and 81 (int8 47 and
+// 54).
 // Parts of all sequences together: enough for `target` workgroups, none without a unit of keys; 0 where every sequence is one part.
 int slots_of(int64_t target, int64_t n_seq, int64_t Hk, int64_t head_tiles, int64_t max_len, int64_t unit) {
-  const int64_t units = (max_len + unit - 1) / unit;
+  const int64_t units = (max_len + unit - 1) / unit, groups = n_seq * Hk * head_tiles;
+  if (units <= 2 + groups / 26) return 0;
   int64_t n = target / (Hk * head_tiles);
   if (n > n_seq * units) n = n_seq * units;
   if (n_seq == 1 && n > kMaxParts) n = kMaxParts;
