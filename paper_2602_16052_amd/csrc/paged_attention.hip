@@ -465,11 +465,11 @@ constexpr size_t kFirstBytes = 2048;  // first parts of up to kMaxShared sequenc
 // Short caches and many sequences are not split: a unit of keys takes a workgroup 1.2 us, the launch that joins parts 2.5 to 6.  us whole and
 // in parts, bf16 heads of 128: 4 heads of one sequence (workgroups), 250 entries (2 units) 6.8 and 8.3, 500 entries 8.9 and 8.3; 64 of them, 500
 // 9.8 and 10.9, 1000 14.9 and 12.9; 160, 1000 16.4 and 20.6, 2000 34.7 and 38.3 (int8 31.4 and 24.6); 400, 2000 76 and 81 (int8 47 and
-// 54).
+// 54); rows of 256, 64 workgroups, 250 entries 10.8 and 11.5, 500 15.4 and 13.4.
 // Parts of all sequences together: enough for `target` workgroups, none without a unit of keys; 0 where every sequence is one part.
-int slots_of(int64_t target, int64_t n_seq, int64_t Hk, int64_t head_tiles, int64_t max_len, int64_t unit) {
+int slots_of(int64_t target, int64_t n_seq, int64_t Hk, int64_t head_tiles, int64_t max_len, int64_t unit, int64_t row_bytes) {
   const int64_t units = (max_len + unit - 1) / unit, groups = n_seq * Hk * head_tiles;
-  if (units <= 2 + groups / 26) return 0;
+  if (units * (row_bytes > 256 ? row_bytes : 256) <= (2 + groups / 26) * 256) return 0;
   int64_t n = target / (Hk * head_tiles);
   if (n > n_seq * units) n = n_seq * units;
   if (n_seq == 1 && n > kMaxParts) n = kMaxParts;
@@ -481,7 +481,7 @@ hipError_t run_paged(const PagedAttnArgs &args, void *out, float *lse, void *ws,
   typedef PagedShape<T, CODE, D> P;
   PagedAttnArgs a = args;
   const KeyArgs &k = a.keys;
-  a.slots = slots_of(P::kTarget, k.n_seq, k.Hk, a.head_tiles, k.max_len, P::kUnit);
+  a.slots = slots_of(P::kTarget, k.n_seq, k.Hk, a.head_tiles, k.max_len, P::kUnit, P::kRowBytes);
   auto kern = paged_attention_kernel<T, CODE, D>;
   static_assert(P::kLds <= 160 * 1024, "LDS of a compute unit");
   if (P::kLds > 64 * 1024) {
