@@ -41,34 +41,33 @@ struct PagedShape {
   static constexpr int kValueLanes = kRowBytes / 16;       // lanes that hold a row of values
   static constexpr int kValueRows = 64 / pow2_ceil(kValueLanes) < kKeys ? 64 / pow2_ceil(kValueLanes) : kKeys;  // rows of a load
   static constexpr int kValueLoads = kKeys / kValueRows;
-  // Workgroups wanted: one round of what the compute units hold by registers, two each, or one with long rows.  us with 512 and with 256:
-  // 48 requests over int8 rows of 128 135 and 214, one over 131071 e4m3 rows of 128 36.1 and 41.4; bf16 rows of 192 46.5 and 41.5, fp32
+  // Workgroups wanted: one round of what the compute units hold by registers (up to three each, or one with long rows), two each where
+  // parts are short, which then have as many again to join.  us with 512 and with 768: 48 requests over int8 rows of 128 123 and 116, 64
+  // over bf16 ones 266 and 263, one over 131071 e4m3 rows 29.2 and 31.9; with 512 and with 256: bf16 rows of 192 46.5 and 41.5, fp32
   // ones of 256 36.5 and 30.9, int8 ones of 256 56.2 and 51.6.
-  static constexpr int kTarget = D >= 192 || kRowBytes >= 512 ? 256 : 512;
+  static constexpr bool kLong = D >= 192 || kRowBytes >= 512;
+  static int target(int64_t all_units) { return kLong ? 256 : all_units >= 16 * 768 ? 768 : 512; }
   static constexpr int kJoinRow = D + 4;  // floats; the pad keeps the 16 heads of a store off each other's banks
   static constexpr int kJoin = kWaves * 16 * (kJoinRow + 2) * (int)sizeof(float);
   static constexpr int kLds = kWaves * kTileLds > kJoin ? kWaves * kTileLds : kJoin;
 };
 
-// Two bytes' worth of codes, and four, as values.
-template <int CODE>
-__device__ __forceinline__ float code_value(uint32_t w, int e) {
-  if (CODE == MOESPEC_CACHE_I8) return (float)(int8_t)(w >> (8 * e));
-  switch (e) {
-    case 0: return __builtin_amdgcn_cvt_f32_fp8(w, 0);
-    case 1: return __builtin_amdgcn_cvt_f32_fp8(w, 1);
-    case 2: return __builtin_amdgcn_cvt_f32_fp8(w, 2);
-    default: return __builtin_amdgcn_cvt_f32_fp8(w, 3);
-  }
-}
-// Eight codes as bf16 (exact: both have no more bits).
+// Eight codes as bf16 (exact: bf16 has no fewer bits).
 template <int CODE>
 __device__ __forceinline__ bf16x8 codes_bf16(uint32_t a, uint32_t b) {
   bf16x8 v;
+  if constexpr (CODE == MOESPEC_CACHE_I8) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    v[e] = (__bf16)code_value<CODE>(a, e);
-    v[4 + e] = (__bf16)code_value<CODE>(b, e);
+    for (int e = 0; e < 4; ++e) {
+      v[e] = (__bf16)(float)(int8_t)(a >> (8 * e));
+      v[4 + e] = (__bf16)(float)(int8_t)(b >> (8 * e));
+    }
+  } else {  // two at a time
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    const bf16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true)};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = p[e / 2][e % 2];
   }
   return v;
 }
@@ -98,6 +97,13 @@ __device__ __forceinline__ void split_above_zero(const float (&v)[8], bf16x8 (&p
   part[0] = __builtin_bit_cast(bf16x8, cut);
 }
 
+// 16 bytes that nobody reads again soon.  Values come in whole lines and are requested so: 64 requests 293 -> 266 us (6.1 TB/s), int8 130 ->
+// 123, one over 131071 e4m3 entries 33.1 -> 29.3.  A load of keys takes half a line of every row, and the other half has to stay until
+// the next one: with keys requested so too, 284, 122 and 30.8.
+__device__ __forceinline__ uint4 stream_load(const unsigned char *p) {
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p)));
+}
+
 // v of the lanes that hold the same head, l ^ 16 and l ^ 32, combined.
 __device__ __forceinline__ float head_max(float v) {
   auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -111,7 +117,7 @@ __device__ __forceinline__ float head_sum(float v) {
 }
 
 template <typename T, int CODE, int D>
-__global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T *__restrict__ out, float *__restrict__ lse,
+__global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kernel(PagedAttnArgs a, T *__restrict__ out, float *__restrict__ lse,
                                                               float *__restrict__ part, float2 *__restrict__ part_ml,
                                                               int32_t *__restrict__ first_of) {
   typedef PagedShape<T, CODE, D> P;
@@ -208,7 +214,7 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, T
       const unsigned char *at = pg.v + row * P::kRowBytes;
 #pragma unroll
       for (int j = 0; j < P::kValueLoads / P::kHalves; ++j)
-        vr[x * (P::kValueLoads / P::kHalves) + j] = *reinterpret_cast<const uint4 *>(at + vat + j * P::kValueRows * P::kRowBytes);
+        vr[x * (P::kValueLoads / P::kHalves) + j] = stream_load(at + vat + j * P::kValueRows * P::kRowBytes);
       if (P::kCodes) vs[x] = *reinterpret_cast<const f32x4 *>(pg.v_scale + row + 4 * g4);
     }
   };
@@ -459,7 +465,7 @@ __global__ __launch_bounds__(kGroups *D / 4) void paged_join_kernel(KeyArgs a, i
   if (lse && col == 0) lse[row] = l == 0.f ? -INFINITY : (top + __log2f(l)) * 0.69314718055994531f;
 }
 
-constexpr int kMostGroups = 512;      // workgroups wanted, at most
+constexpr int kMostGroups = 768;      // workgroups wanted, at most
 constexpr size_t kFirstBytes = 2048;  // first parts of up to kMaxShared sequences
 
 // Short caches and many sequences are not split: a unit of keys takes a workgroup 1.2 us, the launch that joins parts 2.5 to 6.  us whole and
@@ -481,7 +487,8 @@ hipError_t run_paged(const PagedAttnArgs &args, void *out, float *lse, void *ws,
   typedef PagedShape<T, CODE, D> P;
   PagedAttnArgs a = args;
   const KeyArgs &k = a.keys;
-  a.slots = slots_of(P::kTarget, k.n_seq, k.Hk, a.head_tiles, k.max_len, P::kUnit, P::kRowBytes);
+  const int64_t units = ((int64_t)k.max_len + P::kUnit - 1) / P::kUnit * k.n_seq * k.Hk * a.head_tiles;
+  a.slots = slots_of(P::target(units), k.n_seq, k.Hk, a.head_tiles, k.max_len, P::kUnit, P::kRowBytes);
   auto kern = paged_attention_kernel<T, CODE, D>;
   static_assert(P::kLds <= 160 * 1024, "LDS of a compute unit");
   if (P::kLds > 64 * 1024) {
