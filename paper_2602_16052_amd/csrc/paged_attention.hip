@@ -9,6 +9,11 @@
 // same order of elements.  A lane's scores, key 4 (l / 16) + i of head l % 16, are already the right operand of O^T = V^T P^T.
 // Values lie in rows and are needed in columns: a wave lays its own through LDS (rows of D elements and a pad that keeps the
 // transposing reads off each other's banks).  Waves share nothing until their results are joined at the end.
+// A wave requests the next tile's keys when the products have used up their registers, and its values when these lie in LDS, so that
+// one of the two is always under way.
+// 64 requests x 8 heads of 128, up to 8189 bf16 entries: 264 us, 6.1 TB/s (a read-only stream reaches 6.4); int8, 48 x 4 heads, up to 16381: 116
+// us, 5.4 TB/s (the vector ALU, which widens the codes, is busy for half of the cycles); e4m3, one request over 131071: 29 us, 4.8 TB/s (start,
+// joining of 128 parts); one over 1021 bf16 entries: 8.9 us, two launches.
 #include "serving.h"
 
 namespace moespec {

@@ -249,3 +249,10 @@ def test_bit_identical_runs_and_graph_replays():
     keys, values = pool.values("k"), pool.values("v")
     keys[3], values[3] = keys[3][:, :0], values[3][:, :0]  # (that sequence has no page)
     pool.check(q, out, lse, V.attention(f64(q), keys, values, float(np.float32(pool.scale))))
+
+
+def test_the_most_query_heads():
+    for dtype, H, Hk in (("bf16", 1024, 1), ("f32", 1024, 512)):
+        pool = Pool(dtype, "plain", Hk, 64, [40, 3], 16, seed=22, H=H).poison()
+        q = queries(pool)
+        pool.check(q, *run(pool, q))
