@@ -559,7 +559,8 @@ typedef struct {
  *   path, n_path, max_path                          as for moespec_cache_commit; path and n_path NULL: all tokens of the tree in order
  *   new_len  [n_seq] int32 out                      min(cache_len + n_path, max_pages * page_size); may be NULL
  * A row's scale and codes, with amax its largest magnitude:
- *   I8    scale = amax / 127, code = x * (127 / amax) to the nearest integer (ties to even; quotients in fp32, the product unrounded)
+ *   I8    scale = amax / 127, code = x * (127 / amax) to the nearest integer (ties to even; quotients in fp32, the product unrounded;
+ *         127 / amax no larger than the largest fp32 number, so that rows with amax < 127 / 3.4e38 = 3.7e-37 read as smaller ones, or 0)
  *   E4M3  scale = 2^e, the smallest with amax <= 448 * 2^e and e >= -126, code = x / scale to the nearest
  * A row with a value that is not finite has the scale NaN and reads as NaN throughout.  Entries whose page is outside of the pool are
  * dropped.  No two entries that are written may lie in the same place (pages that sequences share hold entries in front of

@@ -156,6 +156,38 @@ __device__ __forceinline__ void arrived(F &f) {
   asm volatile("" : "+v"(f));
 }
 
+// 16 bytes of a row as floats and back.
+template <typename T> struct Piece;
+template <> struct Piece<uint16_t> {
+  static constexpr int kElems = 8;
+  static __device__ __forceinline__ void load(const uint16_t *p, float (&v)[8]) {
+    const uint4 b = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ void store(uint16_t *p, const float (&v)[8]) {
+    bf16x8 o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
+    *reinterpret_cast<bf16x8 *>(p) = o;
+  }
+};
+template <> struct Piece<float> {
+  static constexpr int kElems = 4;
+  static __device__ __forceinline__ void load(const float *p, float (&v)[4]) {
+    const f32x4 b = *reinterpret_cast<const f32x4 *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = b[i];
+  }
+  static __device__ __forceinline__ void store(float *p, const float (&v)[4]) {
+    *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]};
+  }
+};
+
 // Row (of 32) of element i of a lane's 32 x 32 result; half = lane >> 5.  The column is lane & 31.
 __device__ __forceinline__ int acc_row(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
 

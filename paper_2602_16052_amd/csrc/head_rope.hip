@@ -22,40 +22,6 @@ struct RopeArgs {
   float eps;
 };
 
-template <typename T>
-struct Piece16;
-template <>
-struct Piece16<uint16_t> {
-  static constexpr int kElems = 8;
-  static __device__ __forceinline__ void load(const uint16_t *p, float (&v)[8]) {
-    const uint4 b = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ void store(uint16_t *p, const float (&v)[8]) {
-    bf16x8 o;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
-    *reinterpret_cast<bf16x8 *>(p) = o;
-  }
-};
-template <>
-struct Piece16<float> {
-  static constexpr int kElems = 4;
-  static __device__ __forceinline__ void load(const float *p, float (&v)[4]) {
-    const f32x4 b = *reinterpret_cast<const f32x4 *>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = b[i];
-  }
-  static __device__ __forceinline__ void store(float *p, const float (&v)[4]) {
-    *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]};
-  }
-};
-
 // Cosine and sine of place * freq.  The angle is reduced to a quarter turn in 64 bits, so that far places lose nothing; what is left
 // is at most pi / 4 and rounded to fp32 once (2.4e-8 at most).
 __device__ __forceinline__ float2 turn(double place, float freq) {
@@ -74,7 +40,7 @@ __device__ __forceinline__ float2 turn(double place, float freq) {
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void head_rope_kernel(RopeArgs a) {
-  typedef Piece16<T> P;
+  typedef Piece<T> P;
   constexpr int E = P::kElems, kPieces = D / E, kLanes = kPieces / 2, W = pow2_ceil(kLanes), kHeads = 256 / W;
   __shared__ float2 cs[D / 2];
   const int row = blockIdx.x, lane = threadIdx.x & 63, j = threadIdx.x % W;
