@@ -182,19 +182,27 @@ __global__ __launch_bounds__(kStatThreads) void logit_stats_kernel(VerifyArgs a)
   int arg = 0x7fffffff;
   if (k > 0.0) {
     if (top > -INFINITY && top < INFINITY) {
-      // 2^(x k - c) with c = top k rounded, one instruction less than from x - top; what c has lost is the same for all
+      // 2^(x k - c) with c = top k rounded, one instruction less than from x - top; what c has lost is the same for all.  From |c| = 2^40 on
+      // (a row of the type's lowest value) that could be anything, and the floats next to top are 2^16 away: only top itself weighs.
       const double c = (double)top * k;
-      constexpr int kSide = 4;  // in flight at a time; more of them, and their registers cost waves
+      if (fabs(c) < 0x1p40) {
+        constexpr int kSide = 4;  // in flight at a time; more of them, and their registers cost waves
 #pragma unroll
-      for (int i = 0; i < kEach; i += kSide) {
-        double w[kSide];
+        for (int i = 0; i < kEach; i += kSide) {
+          double w[kSide];
 #pragma unroll
-        for (int j = 0; j < kSide; ++j) w[j] = fma((double)v[i + j], k, -c);
-        exp2_of(w);
-        sum += (w[0] + w[1]) + (w[2] + w[3]);
-        __builtin_amdgcn_sched_barrier(0);
+          for (int j = 0; j < kSide; ++j) w[j] = fma((double)v[i + j], k, -c);
+          exp2_of(w);
+          sum += (w[0] + w[1]) + (w[2] + w[3]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        sum *= exp2_sum(-fma((double)top, k, -c));
+      } else {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) n += v[i] == top ? 1 : 0;
+        sum = n;
       }
-      sum *= exp2_sum(-fma((double)top, k, -c));
     }
   } else {
 #pragma unroll

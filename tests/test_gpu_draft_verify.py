@@ -197,6 +197,32 @@ def test_numbers_and_temperatures_out_of_range():
     assert np.all((got >= 0) & (got < 700))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sampled", [False, True])
+def test_logits_of_the_types_lowest_value_and_other_far_ones(dtype, sampled):
+    """Rows of the lowest value alone (every token weighs the same), rows of it but for one part of the vocabulary, logits of 1e30, and ordinary
+    ones at the lowest temperature: logit / temperature is far past the bits of a float64's fraction, their differences are not."""
+    low = torch.finfo(TORCH[dtype]).min
+    lengths = []
+    for seed in range(6):
+        b = Batch([6, 1, 9, 4, 12], 5000, dtype, sampled, seed=40 + seed, heat=[1.0, 0.7, 1.3, 1e-30, 3e-18], chain=seed % 2 == 0, lift=6.0)
+        rng = np.random.default_rng(seed)
+        kinds = rng.integers(0, 5, b.M)
+        for t in (b.logits, b.draft):
+            if t is None:
+                continue
+            for row, kind in enumerate(kinds):
+                if kind == 1:
+                    t[row] = low
+                elif kind == 2:
+                    t[row, 2048:] = low
+                elif kind == 3:
+                    t[row] = torch.where(t[row] > 1.0, torch.tensor(1e30, dtype=t.dtype, device="cuda"), -t[row].abs() * 1e29)
+        b.u_accept = np.where(rng.random(b.M) < 0.5, b.u_accept, 1e-4)  # (a token of 5000: 2e-4)
+        lengths += b.check(b.run())
+    assert max(lengths) > 2
+
+
 def test_large_trees_and_their_limit():
     b = Batch([2048, 300], 300, seed=12, lift=1.0, back=40)
     b.check(b.run(64), 64)
