@@ -1,7 +1,7 @@
 // Attention of one new token of every sequence over its pages of keys and values, which may be held in 8 bits.
 //
 // Bound by the stream of keys and values: each is read once for all query heads that share it.  One pass with a running maximum m and
-// sum l for each head (in units of log 2): p = 2^(c q.k - m), l += p, O += p V, out = O / l; the scale of a key's row multiplies its
+// sum l for each head: p = 2^(c (q.k - m)), l += p, O += p V, out = O / l; the scale of a key's row multiplies its
 // score, that of a value's row its weight.  The keys are split into parts (few sequences) that a second kernel joins.
 //
 // The query heads of a KV head are the 16 columns of matrix instructions (unused ones repeat a head and are not written).  S = K Q^T
@@ -306,11 +306,12 @@ __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kerne
     for (int x = 0; x < P::kHalves; ++x)
 #pragma unroll
       for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[x][i]);
-    mx = head_max(mx) * ka.c;
-    // raised only when it is passed by more than 2^8: until then weights stay below 2^8, as exact as below 1, and O is not rescaled
-    const bool raise = mx > m + 8.f;
+    mx = head_max(mx);
+    // raised only when it is passed by more than 2^8: until then weights stay below 2^8, as exact as below 1, and O is not rescaled.  Scores are
+    // subtracted before they are scaled, so that the largest weighs 1 however large it is.
+    const bool raise = (mx - m) * ka.c > 8.f;
     if (__ballot(raise) != 0) {
-      const float alpha = raise ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
+      const float alpha = raise ? __builtin_amdgcn_exp2f((m - mx) * ka.c) : 1.f;
       m = raise ? mx : m;
       l *= alpha;
 #pragma unroll
@@ -323,7 +324,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kerne
     for (int x = 0; x < P::kHalves; ++x)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        sc[x][i] = __builtin_amdgcn_exp2f(fmaf(sc[x][i], ka.c, -mu));
+        sc[x][i] = __builtin_amdgcn_exp2f((sc[x][i] - mu) * ka.c);
         l += sc[x][i];
         if (P::kCodes) sc[x][i] *= vscale[x][i];
       }
@@ -362,7 +363,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kerne
     asm volatile("" ::: "memory");
   }
   l = head_sum(l);
-  if (m == -INFINITY && l != 0.f) m = 0.f;  // scores that are all NaN: so is the row
+  m = m == -INFINITY && l != 0.f ? 0.f : m * ka.c;  // scores that are all NaN: so is the row
 
   // the waves' results joined: [wave][head]{m, l}, then [wave][head][D]
   __syncthreads();

@@ -5,7 +5,7 @@ import torch
 
 from oracle import serving_oracle as V
 from paper_2602_16052_amd import binding as mb
-from attention_common import TORCH, f64, i32
+from attention_common import HALF_STEP, TORCH, f64, i32
 from serving_common import Pool
 
 pytestmark = pytest.mark.gpu
@@ -142,6 +142,36 @@ def test_large_scores_and_a_maximum_that_rises_late():
         flat[pool.rows[0][e // 16], e % 16] *= 6
     q = queries(pool, scale=3.0)
     pool.check(q, *run(pool, q))
+
+
+@pytest.mark.parametrize("lens", [[5000], [700, 33, 1]])
+@pytest.mark.parametrize("dtype,code", [("bf16", "plain"), ("f32", "plain"), ("bf16", "i8"), ("f32", "e4m3")])
+def test_scores_whose_rounding_is_larger_than_any_exponent(dtype, code, lens):
+    """Scores up to 1.8e10 and down to -1.8e10 (their last bit: 2^11) leave the keys with the largest one alone, which share the row.  Keys are a power of
+    two a times a row of signs and queries another times the same signs, so that every product and sum is exact."""
+    D, b = 64, 2.0 ** 20
+    pool = Pool(dtype, code, 1, D, lens, 16, seed=len(lens), H=4, scale=0.27)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    sign = torch.where(torch.rand((D,), generator=gen, device="cuda") < 0.5, -1.0, 1.0)
+    c = pool.cache
+    a = torch.exp2(torch.randint(0, 11, c.k_pages.shape[:-1], generator=gen, device="cuda").float())
+    if code == "plain":
+        c.k_pages.copy_(a[..., None] * sign)
+    else:
+        c.k_pages.copy_(sign.expand(c.k_pages.shape).to(c.k_pages.dtype))
+        c.k_scale.copy_(a)
+    q = (sign * b).expand((len(lens), 4, D)).clone()
+    q[:, 1] *= -1.0
+    q[:, 2] *= 2.0 ** -20
+    q = q.to(TORCH[dtype])
+    out, lse = run(pool, q)
+    want, want_lse, bound, _ = V.attention(f64(q), pool.values("k"), pool.values("v"), float(np.float32(0.27)))
+    # weights are 1 or below 2^-24 of it (head 2: scores of up to 17695, two of which are 17 apart at least)
+    rel = (2.0 ** -15 if dtype == "bf16" else 2.0 ** -24) + 2.0 ** -23 + 2 * (max(lens) + 64) * 2.0 ** -24
+    u = HALF_STEP[dtype]
+    assert np.all(np.abs(f64(out) - want) <= u * np.abs(want) * (1 + 2.0 ** -6) + bound * rel)
+    # the scale in units of log 2, its product with a score, the sum with log2 l, ln 2, the product with it: half a step each
+    assert np.all(np.abs(f64(lse) - want_lse) <= np.abs(want_lse) * 5 * 2.0 ** -24 * 1.01 + 2.0 ** -15)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
