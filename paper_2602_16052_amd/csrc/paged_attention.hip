@@ -363,9 +363,10 @@ __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kerne
     asm volatile("" ::: "memory");
   }
   l = head_sum(l);
-  m = m == -INFINITY && l != 0.f ? 0.f : m * ka.c;  // scores that are all NaN: so is the row
+  if (m == -INFINITY && l != 0.f) m = 0.f;  // scores that are all NaN: so is the row
 
-  // the waves' results joined: [wave][head]{m, l}, then [wave][head][D]
+  // the waves' results joined: [wave][head]{m, l}, then [wave][head][D].  Here and between parts m stays a score: maxima are subtracted before they are
+  // scaled, so that a key weighs the same whichever wave or part it falls to.  (Scaled ones, rounded, would be off by half a unit of log 2 at 2^23.)
   __syncthreads();
   float2 *ml = reinterpret_cast<float2 *>(lds);
   float *op = reinterpret_cast<float *>(lds + P::kWaves * 16 * sizeof(float2));
@@ -384,7 +385,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kerne
 #pragma unroll
     for (int w = 0; w < P::kWaves; ++w) {
       const float2 x = ml[w * 16 + n];
-      const float f = __builtin_amdgcn_exp2f(x.x - mu);
+      const float f = __builtin_amdgcn_exp2f((x.x - mu) * ka.c);
       lt = fmaf(x.y, f, lt);
       const f32x4 y = *reinterpret_cast<const f32x4 *>(op + (w * 16 + n) * P::kJoinRow + d);
       if (x.x != -INFINITY) {  // a wave without keys has no values
@@ -397,7 +398,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kerne
       const size_t row = (size_t)s * ka.H + head;
       const float inv = lt == 0.f ? 0.f : 1.f / lt;
       Elem<T>::store4(out + row * D + d, lt == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
-      if (lse && d == 0) lse[row] = lt == 0.f ? -INFINITY : (mt + __log2f(lt)) * 0.69314718055994531f;
+      if (lse && d == 0) lse[row] = lt == 0.f ? -INFINITY : (mt * ka.c + __log2f(lt)) * 0.69314718055994531f;
     } else {
       const size_t row = (size_t)index * ka.H + head;
       *reinterpret_cast<f32x4 *>(part + row * D + d) = v;
@@ -432,14 +433,14 @@ __global__ __launch_bounds__(kGroups *D / 4) void paged_join_kernel(KeyArgs a, i
     float top = m;
 #pragma unroll
     for (int j = 0; j < 4; ++j) top = fmaxf(top, i0 + j * kGroups < n ? x[j].x : -INFINITY);
-    const float mu = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f(m - mu);
+    const float mu = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f((m - mu) * a.c);
     l *= f0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] *= f0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (i0 + j * kGroups >= n || x[j].x == -INFINITY) continue;
-      const float f = __builtin_amdgcn_exp2f(x[j].x - mu);
+      const float f = __builtin_amdgcn_exp2f((x[j].x - mu) * a.c);
       l = fmaf(f, x[j].y, l);
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = fmaf(f, v[j][e], o[e]);
@@ -453,13 +454,13 @@ __global__ __launch_bounds__(kGroups *D / 4) void paged_join_kernel(KeyArgs a, i
   float top = m;
 #pragma unroll
   for (int g = 1; g < kGroups; ++g) top = fmaxf(top, ml[g].x);
-  const float mu = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f(m - mu);
+  const float mu = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f((m - mu) * a.c);
   l *= f0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] *= f0;
 #pragma unroll
   for (int g = 1; g < kGroups; ++g) {
-    const float f = __builtin_amdgcn_exp2f(ml[g].x - mu);
+    const float f = __builtin_amdgcn_exp2f((ml[g].x - mu) * a.c);
     l = fmaf(f, ml[g].y, l);
     const f32x4 v = po[g][col];
 #pragma unroll
@@ -468,7 +469,7 @@ __global__ __launch_bounds__(kGroups *D / 4) void paged_join_kernel(KeyArgs a, i
   const size_t row = (size_t)s * a.H + head;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   Elem<T>::store4(out + row * D + 4 * col, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
-  if (lse && col == 0) lse[row] = l == 0.f ? -INFINITY : (top + __log2f(l)) * 0.69314718055994531f;
+  if (lse && col == 0) lse[row] = l == 0.f ? -INFINITY : (top * a.c + __log2f(l)) * 0.69314718055994531f;
 }
 
 constexpr int kMostGroups = 768;      // workgroups wanted, at most

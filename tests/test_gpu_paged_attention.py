@@ -286,3 +286,38 @@ def test_the_most_query_heads():
         pool = Pool(dtype, "plain", Hk, 64, [40, 3], 16, seed=22, H=H).poison()
         q = queries(pool)
         pool.check(q, *run(pool, q))
+
+
+FAR = {"plain": (2.0 ** 12, 2.0 ** 11), "i8": (2.0 ** 16, 127.0), "e4m3": (2.0 ** 15, 256.0)}  # element 0 of queries and of the two keys
+
+
+@pytest.mark.parametrize("lens,pairs", [([128] * 4, [(5, 9), (5, 40), (69, 120), (3, 69)]),             # one part: a wave's tile, two waves, two tiles
+                                        ([5000, 2000, 700], [(5, 4990), (1990, 40), (100, 690)]),       # parts that sequences share
+                                        ([5000], [(4000, 2)])])                                         # parts of one sequence
+@pytest.mark.parametrize("dtype,code", [("bf16", "plain"), ("f32", "plain"), ("bf16", "i8"), ("f32", "i8"), ("bf16", "e4m3"), ("f32", "e4m3")])
+def test_neighbouring_scores_far_from_zero_weigh_what_their_difference_says(dtype, code, lens, pairs):
+    """Two keys of every sequence have scores around 2^23 that are 0, 1, 2 and 5 apart, whole numbers throughout, so that scores are exact; the
+    others have the score 0, and no weight.  Wherever the two fall, the rest follows from the difference alone: a bound that does not grow with
+    the scores."""
+    D, diffs = 64, [0.0, 1.0, 2.0, 5.0]
+    pool = Pool(dtype, code, 1, D, lens, 16, seed=7, H=4, scale=1.0)
+    a, b = FAR[code]
+    k = torch.zeros((pool.cache.k_pages.shape[1], 16, D), device="cuda")
+    for s, (e0, e1) in enumerate(pairs):
+        for e, one in ((e0, 1.0), (e1, 0.0)):
+            k[int(pool.rows[s][e // 16]), e % 16, 0] = b
+            k[int(pool.rows[s][e // 16]), e % 16, 1] = one
+    pool.cache.k_pages.copy_(k.to(pool.cache.k_pages.dtype)[None, :, None])
+    if code != "plain":
+        pool.cache.k_scale.fill_(1.0)
+    q = torch.zeros((len(lens), 4, D), device="cuda")
+    q[:, :, 0], q[:, :, 1] = a, torch.tensor(diffs, device="cuda")
+    q = q.to(TORCH[dtype])
+    out, lse = run(pool, q)
+    want, want_lse, bound, _ = V.attention(f64(q), pool.values("k"), pool.values("v"), 1.0)
+    # the scale in units of log 2 and its product with the difference: half a step each of 5 / ln 2, times ln 2; two exponentials, sums and quotients
+    # of two keys; the parts of a weight
+    rel = 2 * 5 * 2.0 ** -24 + 16 * 2.0 ** -24 + (2.0 ** -15 if dtype == "bf16" else 2.0 ** -23)
+    assert np.all(np.abs(f64(out) - want) <= HALF_STEP[dtype] * np.abs(want) * (1 + 2.0 ** -6) + bound * rel)
+    # the scale in units of log 2, its product with a score, the sum with log2 l, ln 2, the product with it: half a step each
+    assert np.all(np.abs(f64(lse) - want_lse) <= np.abs(want_lse) * 5 * 2.0 ** -24 * 1.01)
