@@ -121,6 +121,13 @@ __device__ __forceinline__ float head_sum(float v) {
   return half_swap(v, false);
 }
 
+// log sum exp of a row from its largest score, the sum of 2^(c (score - largest)), and c.  (c and the logarithm are brought to natural units
+// first: finite wherever the result is.)
+__device__ __forceinline__ float lse_of(float m, float l, float c) {
+  constexpr float kLn2 = 0.69314718055994531f;
+  return l == 0.f ? -INFINITY : fmaf(m, c * kLn2, __log2f(l) * kLn2);
+}
+
 template <typename T, int CODE, int D>
 __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kernel(PagedAttnArgs a, T *__restrict__ out, float *__restrict__ lse,
                                                               float *__restrict__ part, float2 *__restrict__ part_ml,
@@ -398,7 +405,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kerne
       const size_t row = (size_t)s * ka.H + head;
       const float inv = lt == 0.f ? 0.f : 1.f / lt;
       Elem<T>::store4(out + row * D + d, lt == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
-      if (lse && d == 0) lse[row] = lt == 0.f ? -INFINITY : (mt * ka.c + __log2f(lt)) * 0.69314718055994531f;
+      if (lse && d == 0) lse[row] = lse_of(mt, lt, ka.c);
     } else {
       const size_t row = (size_t)index * ka.H + head;
       *reinterpret_cast<f32x4 *>(part + row * D + d) = v;
@@ -469,7 +476,7 @@ __global__ __launch_bounds__(kGroups *D / 4) void paged_join_kernel(KeyArgs a, i
   const size_t row = (size_t)s * a.H + head;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   Elem<T>::store4(out + row * D + 4 * col, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
-  if (lse && col == 0) lse[row] = l == 0.f ? -INFINITY : (top * a.c + __log2f(l)) * 0.69314718055994531f;
+  if (lse && col == 0) lse[row] = lse_of(top, l, a.c);
 }
 
 constexpr int kMostGroups = 768;      // workgroups wanted, at most

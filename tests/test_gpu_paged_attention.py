@@ -321,3 +321,19 @@ def test_neighbouring_scores_far_from_zero_weigh_what_their_difference_says(dtyp
     assert np.all(np.abs(f64(out) - want) <= HALF_STEP[dtype] * np.abs(want) * (1 + 2.0 ** -6) + bound * rel)
     # the scale in units of log 2, its product with a score, the sum with log2 l, ln 2, the product with it: half a step each
     assert np.all(np.abs(f64(lse) - want_lse) <= np.abs(want_lse) * 5 * 2.0 ** -24 * 1.01)
+
+
+def test_the_logarithm_of_a_row_whose_scores_are_near_the_largest_number():
+    """lse is the score itself (3e38), though log2(e) times it is no number."""
+    pool = Pool("f32", "plain", 1, 64, [1, 700], 16, seed=13, H=4, scale=1.0)
+    pool.cache.k_pages.zero_()
+    for s in range(2):
+        pool.cache.k_pages[0, int(pool.rows[s][0]), 0, 0, 0] = 1.5 * 2.0 ** 63
+    q = torch.zeros((2, 4, 64), device="cuda")
+    q[:, :, 0] = 2.0 ** 64
+    out, lse = run(pool, q)
+    values = pool.values("v")
+    for s in range(2):
+        assert np.array_equal(f64(out[s]), np.broadcast_to(values[s][0, :1], (4, 64)))
+    # c, ln 2, their product, the score's with it: half a step each
+    assert np.all(np.abs(f64(lse) / (1.5 * 2.0 ** 127) - 1) <= 4 * 2.0 ** -24 * 1.01)
