@@ -323,6 +323,49 @@ def test_neighbouring_scores_far_from_zero_weigh_what_their_difference_says(dtyp
     assert np.all(np.abs(f64(lse) - want_lse) <= np.abs(want_lse) * 5 * 2.0 ** -24 * 1.01)
 
 
+@pytest.mark.parametrize("n", [300, 3000])  # a part, and parts
+@pytest.mark.parametrize("dtype,code", [("bf16", "plain"), ("f32", "plain"), ("bf16", "i8"), ("f32", "i8"), ("bf16", "e4m3"), ("f32", "e4m3")])
+def test_large_values_under_a_maximum_that_rises_a_little(dtype, code, n):
+    """Results are finite, so they are computed: values of 2^117 and more under weights that a later key passes by e^5, hundreds of them under the
+    same weight (the head of negative queries), whose plain sum is beyond the largest number, and a single value of 96 * 2^121."""
+    D = 64
+    pool = Pool(dtype, code, 1, D, [n, n], 16, seed=11, H=4, scale=1.0)
+    c, gen = pool.cache, torch.Generator(device="cuda").manual_seed(12)
+    top = [[e % n for e in (133, 134, n - 5, n - 133)], [133]]
+    k = torch.zeros((c.k_pages.shape[1], 16, D), device="cuda")
+    v = torch.zeros_like(k)
+    size = 2.0 ** 120 * (1.0 if n == 300 else 2.0 ** -3)
+    v[torch.from_numpy(pool.rows[0][: -(-n // 16)].astype(np.int64)).cuda()] = torch.randint(64, 128, (-(-n // 16), 16, D), generator=gen,
+                                                                                           device="cuda").float() / 64
+    if code == "e4m3":
+        v = v.to(torch.float8_e4m3fn).float()
+    for s in range(2):
+        for e in top[s]:
+            k[int(pool.rows[s][e // 16]), e % 16, 0] = 5.0
+    scale = torch.full((c.k_pages.shape[1], 16), size, device="cuda")
+    p, i = int(pool.rows[1][133 // 16]), 133 % 16
+    v[p, i], scale[p, i] = 96.0, 2.0 ** 121
+    q = torch.zeros((2, 4, D), device="cuda")
+    q[:, :, 0] = torch.tensor([1.0, 0.5, -1.0, 0.75], device="cuda")
+    q = q.to(TORCH[dtype])
+    if code == "plain":
+        c.k_pages.copy_(k[None, :, None])
+        c.v_pages.copy_((v * scale[..., None])[None, :, None])
+    else:
+        held = 64.0 if code == "i8" else 1.0  # (96 * 64 is no int8: the single value's code stays 96)
+        wide = v * held
+        wide[p, i] = 96.0
+        scale = scale / held
+        scale[p, i] = 2.0 ** 121
+        c.k_pages.copy_(k.to(c.k_pages.dtype)[None, :, None])
+        c.v_pages.copy_(wide.to(c.v_pages.dtype)[None, :, None])
+        c.k_scale.fill_(1.0)
+        c.v_scale.copy_(scale[None, :, None])
+    out, lse = run(pool, q)
+    assert torch.isfinite(out.float()).all()
+    pool.check(q, out, lse)
+
+
 def test_the_logarithm_of_a_row_whose_scores_are_near_the_largest_number():
     """lse is the score itself (3e38), though log2(e) times it is no number."""
     pool = Pool("f32", "plain", 1, 64, [1, 700], 16, seed=13, H=4, scale=1.0)
