@@ -22,13 +22,17 @@ struct RopeArgs {
   float eps;
 };
 
-// Cosine and sine of place * freq.  The angle is reduced to a quarter turn in 64 bits, so that far places lose nothing; what is left
-// is at most pi / 4 and rounded to fp32 once (2.4e-8 at most).
+// Cosine and sine of place * freq.  The angle is reduced to a quarter turn in 64 bits, with what the products round off carried along (a
+// product rounded once is off by 2.4e-7 at place 2^31): what is left is at most pi / 4 and rounded to fp32 once (2.4e-8 at
+// most), up to 2^50 quarter turns.
 __device__ __forceinline__ float2 turn(double place, float freq) {
-  const double quarters = place * (double)freq * 0.63661977236758134;
+#pragma clang fp contract(off)  // (a difference that took the place of its rounded product would count the rest twice)
+  constexpr double kQuarters = 0.63661977236758134, kQuartersRest = -3.935735335036497e-17;  // 2 / pi
+  const double x = place * (double)freq, x_rest = fma(place, (double)freq, -x);
+  const double quarters = x * kQuarters, rest = fma(x, kQuarters, -quarters) + fma(x, kQuartersRest, x_rest * kQuarters);
   const double n = rint(quarters);
   float s, c;
-  sincospif(0.5f * (float)(quarters - n), &s, &c);
+  sincospif(0.5f * (float)((quarters - n) + rest), &s, &c);
   const int k = (int)(n - 4.0 * floor(0.25 * n));
   if (k & 1) {
     const float x = s;

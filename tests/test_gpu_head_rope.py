@@ -1,5 +1,7 @@
 """Norm and rotation of queries and keys against the fp64 oracle: types, head sizes, partial and interleaved rotation, places from
 trees and given ones, strides and in place, rows that are not touched."""
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -172,3 +174,23 @@ def test_a_captured_call_follows_the_lengths():
             check(q, None, place, fr, 128, qo, "bf16")
             check(k, None, place, fr, 128, ko, "bf16")
             lens += i32([1, 7])
+
+
+TWO_OVER_PI = Fraction(63661977236758134307553505349005744813783858296182579499066937623558719053690614036045521106501234, 10 ** 98)
+
+
+def test_angles_of_far_places_against_exact_ones():
+    """Cosine and sine themselves (pairs of 1 and 0) at places up to 2^31 and frequencies up to a thousand, against angles that were reduced as
+    fractions: as exact at the last place as at the first."""
+    place = [0, 1, -7, 2 ** 20 + 1, 2 ** 24 + 1, 123456789, 2 ** 28 + 3, 2 ** 31 - 1, 2 ** 31 - 10007]
+    freq = torch.cat([freqs(128), torch.tensor([3.0, 17.3, 0.9999, 1000.3, 999.7, 2.5, 1.5707964, 0.1], device="cuda")])
+    D = 256
+    q = torch.zeros((len(place), 1, D), device="cuda")
+    q[:, :, :72] = 1.0
+    out, _ = mb.moespec_head_rope(mb.AttnDesc(1, 1, D, 1, mb.F32), q, None, freq=freq, rot_dim=144, positions=i32(place))
+    turns = [[Fraction(p) * Fraction(float(f)) * TWO_OVER_PI for f in freq.tolist()] for p in place]
+    angle = np.array([[float(t - 4 * round(t / 4)) for t in row] for row in turns]) * (np.pi / 2)
+    # the angle: half a step of a quarter turn's half; sine and cosine: two steps below 1 (the products with 1 and 0 are exact)
+    tol = 2.4e-8 + 2 * 2.0 ** -24
+    assert np.max(np.abs(f64(out[:, 0, :72]) - np.cos(angle))) <= tol
+    assert np.max(np.abs(f64(out[:, 0, 72:144]) - np.sin(angle))) <= tol
