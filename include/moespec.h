@@ -609,7 +609,8 @@ typedef struct {
   int64_t logit_stride;     /* elements from a row of logits to the next one; 0: V                        */
   int64_t draft_stride;     /* the same for draft_logits                                                  */
   const void *logits;       /* [M, V] the target's, row t for what follows token t                        */
-  const void *draft_logits; /* [M, V] the drafter's, from which the token behind t was drawn; or NULL     */
+  const void *draft_logits; /* [M, V] the drafter's, from which the token behind t was drawn at the same
+                               temperature (drawn at another one, t': the logits times temperature / t'); or NULL */
   const float *temperature; /* [n_seq] or NULL (1); not above 0: greedy.  Taken within 2^-60 .. 2^60      */
 } moespec_verify;
 
@@ -623,9 +624,10 @@ size_t moespec_verify_workspace_bytes(const moespec_verify *verify, int32_t n_se
  * front of it that its mask shows (chains: the one in front).  From the root on, with p the target's distribution behind the last
  * accepted token (softmax of logits / temperature), its children in order:
  *   accept child c of token x if u_accept[c] q(x) < p(x);  else p <- max(p - q, 0) / sum max(p - q, 0), and the next child
- * where q is the drafter's distribution (with draft_logits; chains only), or 1 at x and 0 elsewhere.  Where no child is
+ * where q is the drafter's distribution (softmax of draft_logits / temperature, the sequence's own as for p; chains only), or, without
+ * draft_logits, 1 at x and 0 elsewhere.  Where no child is
  * accepted the path ends, and the next token is the first whose running sum of p exceeds u_sample times the whole sum.  Greedy: p is 1 at the
- * largest logit (ties to the lowest token), and no number is drawn.
+ * largest logit (ties to the lowest token), no number is drawn, and the drafter's distribution does not matter.
  *   tokens   [M] int32 in     outside of 0 .. V - 1: rejected
  *   u_accept [M] double in, u_sample [n_seq] double in   uniform in [0, 1)
  *   path     [n_seq, max_path] int32 out   places of the accepted tokens in the tree, the root's 0 first; -1 behind n_path

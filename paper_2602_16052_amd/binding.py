@@ -1147,7 +1147,8 @@ class DraftVerifyCall(_Call):
     """moespec_draft_verify: from the target's logits [M, vocab] (and, for drafts sampled in chains, the drafter's draft_logits [M,
     vocab]; rows of both may be longer in memory) and the uniform numbers u_accept [M], u_sample [n_seq] float64 to the accepted
     path [n_seq, max_path] int32, n_path and next_token [n_seq] int32, and accepted [M] float32 (1 or 0) or None.  tokens [M] int32;
-    temperature [n_seq] float32 or None (1); tree_off, tree_mask, max_tree as in TreeAttentionCall, row 0 of a tree its root."""
+    temperature [n_seq] float32 or None (1), of both distributions: a drafter that samples at another one, t', passes its logits times
+    temperature / t'; tree_off, tree_mask, max_tree as in TreeAttentionCall, row 0 of a tree its root."""
 
     def __init__(self, desc: VerifyDesc, logits: torch.Tensor, tokens: torch.Tensor, u_accept: torch.Tensor, u_sample: torch.Tensor,
                  path: torch.Tensor, n_path: torch.Tensor, next_token: torch.Tensor, ws: torch.Tensor,

@@ -295,3 +295,24 @@ def test_graph_replays_and_a_shared_workspace():
             stream.synchronize()
             for x, (_, out, _) in zip((b, c), calls):
                 x.check(out, 8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_drafter_that_samples_at_another_temperature(dtype):
+    """One temperature divides both rows of logits; a drafter with its own passes its logits times the quotient (powers of two here, so that nothing
+    is rounded)."""
+    told_apart = 0
+    for heat, own in ((0.5, 1.0), (2.0, 0.5), (1.0, 4.0)):
+        b = Batch([6] * 12, 700, dtype, sampled=True, seed=int(8 * heat), heat=[heat] * 12)
+        drafted = b.draft.clone()
+        b.draft = drafted * (heat / own)
+        got = b.run()
+        # the same walk over logits that each were divided by their own temperature beforehand
+        target, draft = f64(b.logits) / heat, f64(drafted) / own
+        for s in range(12):
+            rows = slice(b.off[s], b.off[s + 1])
+            want, follows = V.verify(target[rows], b.tokens[rows], b.sees[s], b.u_accept[rows], b.u_sample[s], 16, 1.0, draft[rows])
+            assert got["path"][s].tolist() == want + [-1] * (16 - len(want)) and int(got["next_token"][s]) == follows
+            wrong = V.verify(target[rows], b.tokens[rows], b.sees[s], b.u_accept[rows], b.u_sample[s], 16, 1.0, f64(drafted)[rows] / heat)
+            told_apart += wrong != (want, follows)
+    assert told_apart == 17  # sequences in which the drafter at the target's temperature would have led elsewhere
