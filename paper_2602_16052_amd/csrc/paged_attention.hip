@@ -11,9 +11,11 @@
 // transposing reads off each other's banks).  Waves share nothing until their results are joined at the end.
 // A wave requests the next tile's keys when the products have used up their registers, and its values when these lie in LDS, so that
 // one of the two is always under way.
-// 64 requests x 8 heads of 128, up to 8189 bf16 entries: 264 us, 6.1 TB/s (a read-only stream reaches 6.4); int8, 48 x 4 heads, up to 16381: 116
-// us, 5.4 TB/s (the vector ALU, which widens the codes, is busy for half of the cycles); e4m3, one request over 131071: 29 us, 4.8 TB/s (start,
-// joining of 128 parts); one over 1021 bf16 entries: 8.9 us, two launches.
+// 64 requests x 8 heads of 128, up to 8189 bf16 entries: 262 us, 6.2 TB/s (a read-only stream reaches 6.4); int8, 48 x 4 heads, up to 16381: 117
+// us, 5.4 TB/s (the vector ALU, which widens the codes, is busy for 45 % of the cycles, and 38 % of the LDS cycles are bank conflicts: the stores of
+// widened values, pieces of 16 bytes 32 apart); e4m3, one request over 131071: 30 us, 4.6 TB/s (2 us of start, 5.5 of joining 128 parts); one
+// over 1021 bf16 entries: 8.6 us, two launches.
+// fp32 layers over codes with heads of 128 keep 60 bytes a lane in scratch (168 registers, for three workgroups a compute unit).
 #include "serving.h"
 
 namespace moespec {
@@ -49,7 +51,8 @@ struct PagedShape {
   // Workgroups wanted: one round of what the compute units hold by registers (up to three each, or one with long rows), two each where
   // parts are short, which then have as many again to join.  us with 512 and with 768: 48 requests over int8 rows of 128 123 and 116, 64
   // over bf16 ones 266 and 263, one over 131071 e4m3 rows 29.2 and 31.9; with 512 and with 256: bf16 rows of 192 46.5 and 41.5, fp32
-  // ones of 256 36.5 and 30.9, int8 ones of 256 56.2 and 51.6.
+  // ones of 256 36.5 and 30.9, int8 ones of 256 56.2 and 51.6.  8-bit rows of 192 in bf16 layers, of which two fit, are the exception: 30 requests x 4
+  // heads over 5000 int8 entries 51.6 and 62.5, e4m3 48.8 and 56.4.
   static constexpr bool kLong = D >= 192 || kRowBytes >= 512;
   static int target(int64_t all_units) { return kLong ? 256 : all_units >= 16 * 768 ? 768 : 512; }
   static constexpr int kJoinRow = D + 4;  // floats; the pad keeps the 16 heads of a store off each other's banks
@@ -494,9 +497,14 @@ constexpr int kMostGroups = 768;      // workgroups wanted, at most
 constexpr size_t kFirstBytes = 2048;  // first parts of up to kMaxShared sequences
 
 // Short caches and many sequences are not split: a unit of keys takes a workgroup 1.2 us, the launch that joins parts 2.5 to 6.  us whole and
-// in parts, bf16 heads of 128: 4 heads of one sequence (workgroups), 250 entries (2 units) 6.8 and 8.3, 500 entries 8.9 and 8.3; 64 of them, 500
-// 9.8 and 10.9, 1000 14.9 and 12.9; 160, 1000 16.4 and 20.6, 2000 34.7 and 38.3 (int8 31.4 and 24.6); 400, 2000 76 and 81 (int8 47 and
-// 54); rows of 256, 64 workgroups, 250 entries 10.8 and 11.5, 500 15.4 and 13.4.
+// in parts, heads of 128 (of 256 where it says so), bf16, with int8 behind them: 4 heads of one sequence (workgroups), 250 entries (2 units) 6.9 and 8.4, 500
+// entries 9.7 and 8.5; 64 of them, 500 10.7 and 11.4, 1000 17.0 and 13.9; 160, 1000 19.8 and 23.1 (19.8 and 19.2), 2000 34.1 and 36.4 (34.3 and
+// 26.6), 4000 62.1 and 59.3 (63.2 and 39.4); 400, 2000 69.9 and 74.2 (44.6 and 52.6), 4000 132 and 141 (82 and 89); rows of 256, 64
+// workgroups, 250 entries 12.7 and 14.1, 500 18.9 and 16.5.  The rule counts rows of 128 and of 256 bytes alike, which suits int8 at 160
+// workgroups and costs bf16 7 % there (2000 entries), and it takes the parts, 6 to 9 % slower, at 400 workgroups and 4000 entries.
+// Parts are what cuts a sequence that is much longer than the others: as many sequences as target / (Hk * head_tiles), or more, have none
+// to spare.  A request of 131071 bf16 entries (8 KV heads; alone 87 us) among 63 of 100 entries takes 93 us, among 94 834, among 95 1635,
+// among 127 4250 (its eight workgroups are then on one XCD).
 // Parts of all sequences together: enough for `target` workgroups, none without a unit of keys; 0 where every sequence is one part.
 int slots_of(int64_t target, int64_t n_seq, int64_t Hk, int64_t head_tiles, int64_t max_len, int64_t unit, int64_t row_bytes) {
   const int64_t units = (max_len + unit - 1) / unit, groups = n_seq * Hk * head_tiles;

@@ -8,7 +8,8 @@
 namespace moespec {
 
 // The sequence that owns a token row (the number of sequences that end at or in front of it), the same in every lane of a wave; n_seq
-// for rows of none.  One trip to memory for every 64 sequences.
+// for rows of none.  One trip to memory for every 64 sequences, in each wave: right for some hundreds.  (Rotation of one token of each of 256 sequences 4.5
+// us, of 4096 31, of 65535 5522; the same tokens as one sequence with given places 5.0, 6.8 and 86.)
 __device__ __forceinline__ int seq_of_row(const int32_t *tree_off, int n_seq, int row) {
   if (!tree_off) return 0;
   const int lane = threadIdx.x & 63;
