@@ -595,7 +595,7 @@ size_t moespec_paged_attention_workspace_bytes(const moespec_attn_desc *desc, co
  *   out  [n_seq, H, D] dtype out, lse [n_seq, H] float out (natural logarithm; may be NULL)
  * Entries whose page is outside of the pool are not seen, nor those from cache_len on, whatever they hold.  A token that sees no
  * key, or whose every score is -inf, gets out = 0 and lse = -inf.  Results are finite wherever the formula's are; values (codes: scales) below
- * cache_len * 2^-102 may lose bits.  Weights (times the values' scale) enter to 2^-15 in a bf16 layer,
+ * max_len * 2^-102 may lose bits.  Weights (times the values' scale) enter to 2^-15 in a bf16 layer,
  * everything else is fp32 (in an fp32 layer over codes, queries and weights as the sum of three bf16 numbers, which are finite).  desc.capacity does not matter here.
  */
 moespec_status moespec_paged_attention(const moespec_attn_desc *desc, const moespec_paged_cache *cache, int32_t n_seq,

@@ -12,8 +12,8 @@
 // A wave requests the next tile's keys when the products have used up their registers, and its values when these lie in LDS, so that
 // one of the two is always under way.
 // 64 requests x 8 heads of 128, up to 8189 bf16 entries: 262 us, 6.2 TB/s (a read-only stream reaches 6.4); int8, 48 x 4 heads, up to 16381: 117
-// us, 5.4 TB/s (the vector ALU, which widens the codes, is busy for 45 % of the cycles, and 38 % of the LDS cycles are bank conflicts: the stores of
-// widened values, pieces of 16 bytes 32 apart); e4m3, one request over 131071: 30 us, 4.6 TB/s (2 us of start, 5.5 of joining 128 parts); one
+// us, 5.4 TB/s (the vector ALU, which widens the codes, is busy for over 40 % of the cycles, and 38 % of the LDS cycles are bank conflicts: the stores of
+// widened values, pieces of 16 bytes 32 apart); e4m3, one request over 131071: 30 us, 4.6 TB/s (2 us of start, 5 to 6 of joining 128 parts); one
 // over 1021 bf16 entries: 8.6 us, two launches.
 // fp32 layers over codes with heads of 128 keep 60 bytes a lane in scratch (168 registers, for three workgroups a compute unit).
 #include "serving.h"
@@ -26,6 +26,12 @@ struct PagedAttnArgs {
   KeyArgs keys;  // q, cache_len, lengths and heads (one token of every sequence)
   Pages pages;
   int head_tiles, slots;  // tiles of 16 query heads; parts of all sequences together, 0: every sequence is one part
+  // 2^-8 / 2^k with 2^k >= max_len: what weights of 1 enter the products as (exactly).  Weights are up to 2^8 before the maximum is raised, and so the
+  // sum over a sequence's keys is no larger than the largest value: finite wherever that is, as the result is.  (Without it values from 2^-8
+  // of the largest number on, or many keys of the same score, are infinities.)  us without and with it: 48 requests over int8 rows of 128 117.9 and 117.5, 30 over ones of
+  // 192 61.0 and 63.2, 64 over bf16 ones 263.6 and 263.5, four of fp32 12.2 and 12.3; by each sequence's own length, which joining then has to
+  // load, 118.2, 61.3, 263.9 and 12.6.
+  float unit;
 };
 
 template <typename T, int CODE, int D>
@@ -124,12 +130,6 @@ __device__ __forceinline__ float head_sum(float v) {
   return half_swap(v, false);
 }
 
-// 2^-8 / 2^k with 2^k >= len: what weights of 1 enter the products as (exactly).  Weights are up to 2^8 before the maximum is raised, and so the sum over a
-// sequence's keys is no larger than the largest value: finite wherever that is, as the result is.  (Without it 2^8 times as large values, or that
-// many keys of the same score, are infinities.)  us without and with it: 48 requests over int8 rows of 128 117.5 and 118.1, 30 over ones of 192
-// 60.8 and 61.2, 64 over bf16 ones 262.4 and 263.0, four of fp32 12.2 and 12.6.
-__device__ __forceinline__ float weight_unit(int len) { return __uint_as_float((uint32_t)(87 + __clz(max(len, 2) - 1)) << 23); }
-
 // log sum exp of a row from its largest score, the sum of 2^(c (score - largest)), and c.  (c and the logarithm are brought to natural units
 // first: finite wherever the result is.)
 __device__ __forceinline__ float lse_of(float m, float l, float c) {
@@ -157,7 +157,6 @@ __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kerne
   if (s < 0) return;
   const int len = seq_geom(ka, s).len, all = (len + P::kUnit - 1) / P::kUnit;
   const int u0 = share.first(all), u1 = share.last(all);
-  const float unit = weight_unit(len);
   const int h = hk * ka.G + min(tile * 16 + n16, ka.G - 1);
 
   // queries, in the order of a lane's keys
@@ -287,7 +286,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kerne
 #pragma unroll
     for (int x = 0; x < P::kHalves; ++x)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) vscale[x][i] = P::kCodes ? vs[x][i] * unit : 0.f;
+      for (int i = 0; i < 4; ++i) vscale[x][i] = P::kCodes ? vs[x][i] * a.unit : 0.f;
     if (!whole) {  // what is not seen has no score, and must meet weights of 0 as numbers
 #pragma unroll
       for (int x = 0; x < P::kHalves; ++x) {
@@ -346,7 +345,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kerne
       for (int i = 0; i < 4; ++i) {
         sc[x][i] = __builtin_amdgcn_exp2f((sc[x][i] - mu) * ka.c);
         l += sc[x][i];
-        sc[x][i] *= P::kCodes ? vscale[x][i] : unit;
+        sc[x][i] *= P::kCodes ? vscale[x][i] : a.unit;
       }
     asm volatile("" ::: "memory");  // the wave's own rows: LDS keeps their order
     if constexpr (P::kBf16) {
@@ -416,7 +415,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kerne
     const int head = hk * ka.G + tile * 16 + n;
     if (a.slots == 0) {
       const size_t row = (size_t)s * ka.H + head;
-      const float inv = lt == 0.f ? 0.f : 1.f / (lt * unit);
+      const float inv = lt == 0.f ? 0.f : 1.f / (lt * a.unit);
       Elem<T>::store4(out + row * D + d, lt == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
       if (lse && d == 0) lse[row] = lse_of(mt, lt, ka.c);
     } else {
@@ -430,7 +429,7 @@ __global__ __launch_bounds__(256, (D <= 128 ? 3 : 1)) void paged_attention_kerne
 // The parts of a token's keys joined: a workgroup of D / 4 x kGroups threads per head, the parts shared out to the groups.
 constexpr int kGroups = 8;
 template <typename T, int D>
-__global__ __launch_bounds__(kGroups *D / 4) void paged_join_kernel(KeyArgs a, int slots, const float *__restrict__ part,
+__global__ __launch_bounds__(kGroups *D / 4) void paged_join_kernel(KeyArgs a, int slots, float unit, const float *__restrict__ part,
                                                                    const float2 *__restrict__ part_ml,
                                                                    const int32_t *__restrict__ first_of, T *__restrict__ out,
                                                                    float *__restrict__ lse) {
@@ -439,7 +438,6 @@ __global__ __launch_bounds__(kGroups *D / 4) void paged_join_kernel(KeyArgs a, i
   __shared__ f32x4 po[kGroups][kCols];
   const int col = threadIdx.x % kCols, grp = threadIdx.x / kCols, head = blockIdx.x, s = blockIdx.y;
   const int p0 = a.n_seq == 1 ? 0 : first_of[s], n = a.n_seq == 1 ? slots : first_of[s + 1] - p0;
-  const float unit = weight_unit(seq_geom(a, s).len);
   float m = -INFINITY, l = 0.f;
   f32x4 o{0.f, 0.f, 0.f, 0.f};
   for (int i0 = grp; i0 < n; i0 += 4 * kGroups) {
@@ -535,7 +533,8 @@ hipError_t run_paged(const PagedAttnArgs &args, void *out, float *lse, void *ws,
   kern<<<(unsigned)((groups + 7) / 8 * 8 * a.head_tiles), 256, P::kLds, st>>>(a, static_cast<T *>(out), lse, part, ml, first_of);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.slots == 0) return e;
-  paged_join_kernel<T, D><<<dim3(k.H, k.n_seq), kGroups * D / 4, 0, st>>>(k, a.slots, part, ml, first_of, static_cast<T *>(out), lse);
+  paged_join_kernel<T, D>
+      <<<dim3(k.H, k.n_seq), kGroups * D / 4, 0, st>>>(k, a.slots, a.unit, part, ml, first_of, static_cast<T *>(out), lse);
   return hipGetLastError();
 }
 
@@ -582,6 +581,8 @@ hipError_t launch_paged_attention(const moespec_attn_desc &ds, const moespec_pag
   a.keys.c = (float)((double)ds.scale * 1.4426950408889634);
   a.pages = pages_of(ds, cache);
   a.head_tiles = (a.keys.G + 15) / 16;
+  a.unit = 0x1p-8f;
+  for (int64_t n = 1; n < max_len; n *= 2) a.unit *= 0.5f;
   return ds.dtype == MOESPEC_BF16 ? run_code<uint16_t>(cache.code, ds.head_dim, a, out, lse, ws, st)
                                   : run_code<float>(cache.code, ds.head_dim, a, out, lse, ws, st);
 }
