@@ -380,3 +380,16 @@ def test_the_logarithm_of_a_row_whose_scores_are_near_the_largest_number():
         assert np.array_equal(f64(out[s]), np.broadcast_to(values[s][0, :1], (4, 64)))
     # c, ln 2, their product, the score's with it: half a step each
     assert np.all(np.abs(f64(lse) / (1.5 * 2.0 ** 127) - 1) <= 4 * 2.0 ** -24 * 1.01)
+
+
+@pytest.mark.parametrize("lens", [[3000, 40], [120]])
+@pytest.mark.parametrize("dtype,code", [("bf16", "plain"), ("f32", "plain"), ("bf16", "i8"), ("f32", "i8"), ("bf16", "e4m3"), ("f32", "e4m3")])
+def test_small_values_keep_their_bits(dtype, code, lens):
+    """Values (codes: scales) down to about 3000 * 2^-102."""
+    pool = Pool(dtype, code, 2, 64, lens, 16, seed=17, H=8)
+    if code == "plain":
+        pool.cache.v_pages.mul_(2.0 ** -86)
+    else:
+        pool.cache.v_scale.mul_(2.0 ** -82)
+    q = queries(pool)
+    pool.check(q, *run(pool, q))
