@@ -6,7 +6,7 @@
 // a drafter's distribution the difference p - q of the last row is summed over its chunks by workgroups side by side, and a third
 // launch draws from it.
 // Probabilities are in fp64: accepting and drawing are decisions, and have to fall the same way whatever the order of the sums.  So the
-// exponentials, 20 instructions each, bound the first launch (16 trees of 63 x 50001 bf16 logits: 41 us of 53, where the bytes take 16; one tree
+// exponentials, 20 instructions each, bound the first launch (16 trees of 63 x 50001 bf16 logits: 41 us of 52, where the bytes take 16; one tree
 // x 131071: 10 of 20) and trips to memory the second (9 to 15 us).  A table of 2^x for bf16 logits in LDS was tried: 34 us for the 41, nothing
 // for one tree, for a hundred lines more.
 #include "serving.h"

@@ -3,7 +3,7 @@
 // are its own: nothing is exchanged between lanes but the sum of squares.  The angles of a token are the same for all of its heads:
 // a workgroup takes one token, and its first rot_dim / 2 threads leave sine and cosine in LDS.
 // 2044 rows of 32/8 heads of 128, bf16, out of a projection: 10.0 us, 4.2 TB/s (a workgroup makes one trip to memory for what says
-// where the token stands, one for its row, and the write); one token of 32/4 heads: 4.0 to 4.7 us, the launch.
+// where the token stands, one for its row, and the write); one token of 32/4 heads: 4.0 to 4.8 us, the launch.
 #include "serving.h"
 
 namespace moespec {

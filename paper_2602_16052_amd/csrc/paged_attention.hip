@@ -11,10 +11,10 @@
 // transposing reads off each other's banks).  Waves share nothing until their results are joined at the end.
 // A wave requests the next tile's keys when the products have used up their registers, and its values when these lie in LDS, so that
 // one of the two is always under way.
-// 64 requests x 8 heads of 128, up to 8189 bf16 entries: 262 us, 6.2 TB/s (a read-only stream reaches 6.4); int8, 48 x 4 heads, up to 16381: 117
+// 64 requests x 8 heads of 128, up to 8189 bf16 entries: 263 us, 6.2 TB/s (a read-only stream reaches 6.4); int8, 48 x 4 heads, up to 16381: 117
 // us, 5.4 TB/s (the vector ALU, which widens the codes, is busy for over 40 % of the cycles, and 38 % of the LDS cycles are bank conflicts: the stores of
-// widened values, pieces of 16 bytes 32 apart); e4m3, one request over 131071: 30 us, 4.6 TB/s (2 us of start, 5 to 6 of joining 128 parts); one
-// over 1021 bf16 entries: 8.6 us, two launches.
+// widened values, pieces of 16 bytes 32 apart); e4m3, one request over 131071: 29 us, 4.7 TB/s (2 us of start, 5.5 of joining 128 parts); one
+// over 1021 bf16 entries: 8.7 us, two launches.
 // fp32 layers over codes with heads of 128 keep 60 bytes a lane in scratch (168 registers, for three workgroups a compute unit).
 #include "serving.h"
 
